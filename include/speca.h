@@ -542,6 +542,137 @@ speca_status_t speca_cache_check(speca_cache_t* cache, void* stream);
 /* How many kernels the handle has launched since it was created. */
 speca_status_t speca_cache_launch_count(const speca_cache_t* cache, uint64_t* out);
 
+/* ---------------------------------------------------------------------------------------------------
+ * The verification layer itself.
+ *
+ * A speculative step computes one block for real -- the verification layer, whose fresh feature
+ * speca_verify compares with the forecast -- and a rejected sample computes all of them. The calls
+ * below are the parts of such a block that are not plain matrix products: the adaptive layer norm at
+ * its entry, the rotary positions of its queries and keys, and its attention. They work on packed
+ * sequences: the samples of a batch lie one after another in one [rows, ...] tensor, sequence s in rows
+ * host_q_start[s] .. host_q_start[s + 1] - 1, each of its own length (zero included). As everywhere in
+ * this library a device mask says per sequence whether it is active (dev_active_mask, n_seqs bytes, NULL =
+ * all): the rows of an inactive sequence are neither computed nor written, so rejected samples of a batch
+ * are recomputed alone.
+ *
+ * speca_layer_t holds the packing and, if the workspace is given, everything the calls need on the
+ * device. Strides are counted in elements; the last dimension is always dense. All arithmetic is fp32,
+ * rounded once to the storage type on the way out (the bf16 attention also rounds the softmax weights to
+ * bf16, the operand type of the tensor cores, and divides by the sum of the rounded weights).
+ */
+#define SPECA_MAX_SEQS     512 /* most packed sequences of one layer */
+#define SPECA_MAX_HEAD_DIM 128
+#define SPECA_MAX_GROUP    128 /* most query heads that share one key / value head */
+#define SPECA_MAX_AXES     4   /* most position axes of the rotary embedding */
+
+/* Which two elements of a head form a rotated pair; R = sum of axis_dims, elements from R on are kept.
+ * INTERLEAVED: pair p = elements 2p and 2p + 1. HALVES: pair p = elements p and p + R / 2. */
+typedef enum { SPECA_ROPE_INTERLEAVED = 0, SPECA_ROPE_HALVES = 1 } speca_rope_pairing_t;
+
+typedef struct speca_layer speca_layer_t; /* opaque, owned by the library */
+
+typedef struct {
+    int32_t n_seqs;              /* 1 .. SPECA_MAX_SEQS */
+    const int64_t* host_q_start; /* n_seqs + 1 row offsets, ascending from 0; rows in total below 2^31 */
+    const int64_t* host_kv_start; /* the same for keys and values; NULL = as the queries */
+    int32_t dtype;               /* speca_dtype_t of every tensor */
+    int32_t n_heads, n_kv_heads; /* n_kv_heads divides n_heads; query head h reads key head h * n_kv_heads / n_heads.
+                                    Both 0: a layer for speca_layer_modulate alone */
+    int32_t head_dim;            /* 1 .. SPECA_MAX_HEAD_DIM; for the attention in bf16 a multiple of 8 */
+    int32_t causal;              /* nonzero: query i of a sequence sees keys j <= i + kv_len - q_len */
+    float scale;                 /* of the scores; <= 0: 1 / sqrt(head_dim) */
+    float norm_eps;              /* of both norms; <= 0: 1e-6 */
+    int32_t n_axes;              /* rotary axes, 0 = none */
+    int32_t axis_dims[SPECA_MAX_AXES]; /* elements of a head per axis: even, in sum at most head_dim */
+    double theta;                /* pair i of an axis of d elements turns by position * theta^(-2 i / d) */
+    int32_t pairing;             /* speca_rope_pairing_t */
+    void* workspace;             /* device, 256-byte aligned, speca_layer_workspace_bytes; kept alive by the caller */
+    size_t workspace_bytes;
+    int32_t device;
+} speca_layer_config_t;
+
+/* Bytes of device workspace for this configuration (workspace, workspace_bytes, device are not read).
+ * Host only. Errors: INVALID_ARG, SHAPE, NOMEM. */
+speca_status_t speca_layer_workspace_bytes(const speca_layer_config_t* cfg, size_t* out_bytes);
+
+/* Builds the handle and fills the workspace (this call copies to the device and waits for it). A layer
+ * serves one stream at a time: the calls of one handle share its workspace.
+ * Errors: as above, ALIGNMENT (workspace), NOMEM (workspace too small), UNSUPPORTED (not sm_100), CUDA. */
+speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t** out);
+
+/* Waits for the device and releases the handle (the workspace is the caller's). CUDA if a kernel of this
+ * layer had given up on a bounded wait and speca_layer_check has not reported it yet. NULL is ok. */
+speca_status_t speca_layer_destroy(speca_layer_t* layer);
+
+/*
+ * Adaptive layer norm over rows of `dim` elements (any dim >= 1):
+ *   x' = x + gate_s * branch      (x' = x when branch is NULL)
+ *   y  = (x' - mean(x')) / sqrt(var(x') + norm_eps) * (1 + scale_s) + shift_s
+ * with s the row's sequence. y is computed from the unrounded x'.
+ *   x, branch, x_out, y   device, [rows, dim], row strides in elements. branch may be NULL; x_out may be
+ *                         NULL (x' is then not stored) and may be x itself; y may be x or branch unless
+ *                         x_out names that tensor too.
+ *   gate, scale, shift    device, [n_seqs, dim], row stride mod_stride; each may be NULL (gate: 1; scale,
+ *                         shift: 0). gate needs branch.
+ * Rows whose addresses and strides are multiples of 16 bytes take the vector path.
+ * Errors: INVALID_ARG, SHAPE (dim, a stride below dim), ALIGNMENT (to the element), CUDA.
+ */
+speca_status_t speca_layer_modulate(speca_layer_t* layer, int32_t dim, const void* x, int64_t x_stride, const void* branch,
+                                    int64_t branch_stride, const void* gate, const void* scale, const void* shift,
+                                    int64_t mod_stride, const uint8_t* dev_active_mask, void* x_out, int64_t x_out_stride,
+                                    void* y, int64_t y_stride, void* stream);
+
+/*
+ * Rotary positions over several axes for the queries and keys of the layer's query rows (in one launch),
+ * with the RMS norm over the head that such blocks put before it:
+ *   u = x * rsqrt(mean(x^2) + norm_eps) * weight   (u = x when the weight is NULL)
+ *   (a, b) -> (a cos w - b sin w, a sin w + b cos w) for every pair, w = position[axis of the pair] * its frequency.
+ * Axes take the pairs in order: the first axis_dims[0] / 2 pairs, and so on. The angle is reduced in fp64, so a
+ * position of any size costs no accuracy.
+ *   q, q_out, k, k_out  device, [rows, n_heads (k: n_kv_heads), head_dim], strides of rows and heads in
+ *                       elements. k and k_out may both be NULL. q_out may be q, k_out may be k, with the same strides.
+ *   (head_dim must be even.)
+ *   positions           device fp32 [rows, n_axes], dense.
+ *   q_weight, k_weight  device, head_dim elements, or NULL.
+ * Errors: INVALID_ARG, STATE (a layer without axes), SHAPE (a stride below head_dim where there is more than
+ * one head or row), ALIGNMENT (to the element), CUDA.
+ */
+speca_status_t speca_layer_rope(speca_layer_t* layer, const void* q, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
+                                int64_t q_out_row_stride, int64_t q_out_head_stride, const void* k, int64_t k_row_stride,
+                                int64_t k_head_stride, void* k_out, int64_t k_out_row_stride, int64_t k_out_head_stride,
+                                const float* positions, const void* q_weight, const void* k_weight,
+                                const uint8_t* dev_active_mask, void* stream);
+
+/*
+ * Attention of every query row over the keys of its own sequence:
+ *   o_i = sum_j p_ij v_j,  p_i = softmax over the visible j of scale * <q_i, k_j>.
+ * Visible are the first kv_len keys of the sequence, and with `causal` only j <= i + kv_len - q_len (the
+ * queries are the sequence's last rows, so one query per sequence is a decoding step). A row that sees nothing gets
+ * zeros (and lse = -inf). Keys and values behind kv_len are never used, whatever they hold; a value that
+ * is visible to some rows of a tile but not to others must be finite to leave the others alone (0 * inf).
+ *   q, o          device, [query rows, n_heads, head_dim];  k, v: [key rows, n_kv_heads, head_dim]. Strides of
+ *                 rows and heads in elements. o may not overlap an input.
+ *   dev_kv_len    device, n_seqs int32, or NULL: keys that hold data, per sequence (clamped to
+ *                 0 .. the sequence's rows in host_kv_start). Read on the device, so a captured call follows a growing cache.
+ *   dev_lse       device fp32 [n_heads, query rows] or NULL: natural log of the sum of exp(scale * <q, k>).
+ * bf16 runs on the tensor cores and needs q, k, v and o on 16-byte boundaries with strides of multiples
+ * of 8 elements. Results do not depend on the launch: no atomics on values, a fixed order of sums.
+ * Errors: INVALID_ARG, STATE (a layer without heads), SHAPE, ALIGNMENT, UNSUPPORTED (a stride the copy
+ * engine cannot address: 2^40 bytes or more), CUDA.
+ */
+speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
+                                     const void* k, int64_t k_row_stride, int64_t k_head_stride, const void* v,
+                                     int64_t v_row_stride, int64_t v_head_stride, void* o, int64_t o_row_stride,
+                                     int64_t o_head_stride, const int32_t* dev_kv_len, const uint8_t* dev_active_mask,
+                                     float* dev_lse, void* stream);
+
+/* Waits for `stream` and reports (and clears) a bounded wait that a kernel of this layer gave up on, in which
+ * case results since the last check are incomplete: CUDA. Errors: INVALID_ARG, CUDA. */
+speca_status_t speca_layer_check(speca_layer_t* layer, void* stream);
+
+/* Human-readable detail of the most recent error on this handle ("" if none). */
+const char* speca_layer_last_error(const speca_layer_t* layer);
+
 const char* speca_status_string(speca_status_t status);
 /* Human-readable detail of the most recent error on this handle ("" if none). */
 const char* speca_last_error(const speca_cache_t* cache);

@@ -26,6 +26,8 @@ SPECA_PATH_AUTO, SPECA_PATH_DIRECT, SPECA_PATH_BULK, SPECA_PATH_WIDE = 0, 1, 2, 
 SPECA_LAYOUT_TABLES, SPECA_LAYOUT_HISTORY = 0, 1
 SPECA_FEATURE_IN_PLACE = 1   # as feats[entry]: the features already sit in the planes speca_cache_next_slot names
 SPECA_MAX_ORDER, SPECA_MAX_BATCH, SPECA_MAX_ENTRIES, SPECA_MAX_HORIZON = 4, 64, 512, 8
+SPECA_ROPE_INTERLEAVED, SPECA_ROPE_HALVES = 0, 1
+SPECA_MAX_SEQS, SPECA_MAX_HEAD_DIM, SPECA_MAX_GROUP, SPECA_MAX_AXES = 512, 128, 128, 4
 
 EXPORTS = [
     "speca_cache_arena_bytes", "speca_cache_create", "speca_cache_destroy", "speca_cache_reset",
@@ -35,6 +37,8 @@ EXPORTS = [
     "speca_verify_pred_static", "speca_forecast_multi", "speca_verify_metric",
     "speca_verify_partial", "speca_verify_decide", "speca_cache_get_history", "speca_cache_set_history",
     "speca_forecast_sum", "speca_verify_select",
+    "speca_layer_workspace_bytes", "speca_layer_create", "speca_layer_destroy", "speca_layer_modulate", "speca_layer_rope",
+    "speca_layer_attention", "speca_layer_check", "speca_layer_last_error",
 ]
 
 
@@ -63,6 +67,17 @@ class CacheConfig(ctypes.Structure):
         ("verify_entry", ctypes.c_int32), ("eps", ctypes.c_float), ("arena", ctypes.c_void_p),
         ("arena_bytes", ctypes.c_size_t), ("device", ctypes.c_int32), ("path", ctypes.c_int32),
         ("layout", ctypes.c_int32),
+    ]
+
+
+class LayerConfig(ctypes.Structure):
+    _fields_ = [
+        ("n_seqs", ctypes.c_int32), ("host_q_start", ctypes.POINTER(ctypes.c_int64)),
+        ("host_kv_start", ctypes.POINTER(ctypes.c_int64)), ("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("causal", ctypes.c_int32), ("scale", ctypes.c_float),
+        ("norm_eps", ctypes.c_float), ("n_axes", ctypes.c_int32), ("axis_dims", ctypes.c_int32 * SPECA_MAX_AXES),
+        ("theta", ctypes.c_double), ("pairing", ctypes.c_int32), ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t), ("device", ctypes.c_int32),
     ]
 
 
@@ -111,6 +126,17 @@ def _lib() -> ctypes.CDLL:
     L.speca_cache_check.argtypes = [vp, vp]
     L.speca_cache_next_slot.argtypes = [vp, i32, i32, ctypes.POINTER(vp)]
     L.speca_forecast_weights.argtypes = [i32, i32, i32, i32, vp, dbl, ctypes.POINTER(i32), vp]
+    i64 = ctypes.c_int64
+    layerp = ctypes.POINTER(LayerConfig)
+    L.speca_layer_workspace_bytes.argtypes = [layerp, ctypes.POINTER(ctypes.c_size_t)]
+    L.speca_layer_create.argtypes = [layerp, ctypes.POINTER(vp)]
+    L.speca_layer_destroy.argtypes = [vp]
+    L.speca_layer_modulate.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp]
+    L.speca_layer_rope.argtypes = [vp] + [vp, i64, i64] * 4 + [vp] * 5
+    L.speca_layer_attention.argtypes = [vp] + [vp, i64, i64] * 4 + [vp] * 4
+    L.speca_layer_check.argtypes = [vp, vp]
+    L.speca_layer_last_error.argtypes = [vp]
+    L.speca_layer_last_error.restype = ctypes.c_char_p
     L.speca_status_string.argtypes = [i32]
     L.speca_status_string.restype = ctypes.c_char_p
     L.speca_last_error.argtypes = [vp]
@@ -391,6 +417,87 @@ def speca_cache_launch_count(cache) -> int:
     return n.value
 
 
+# ---- the verification layer ------------------------------------------------------------------------
+
+_TORCH_DTYPES = {SPECA_F32: torch.float32, SPECA_BF16: torch.bfloat16}
+
+
+def _layer_config(q_start, dtype, kv_start, n_heads, n_kv_heads, head_dim, causal, scale, norm_eps, axis_dims, theta, pairing):
+    def offsets(xs):
+        return (ctypes.c_int64 * len(xs))(*[int(x) for x in xs])
+
+    if kv_start is not None and len(kv_start) != len(q_start):
+        raise ValueError("kv_start and q_start describe different numbers of sequences")
+    if len(axis_dims) > SPECA_MAX_AXES:
+        raise ValueError("at most %d rotary axes" % SPECA_MAX_AXES)
+    cfg = LayerConfig(n_seqs=len(q_start) - 1, dtype=dtype, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
+                      causal=int(causal), scale=scale, norm_eps=norm_eps, n_axes=len(axis_dims), theta=theta, pairing=pairing)
+    cfg.host_q_start = offsets(q_start)
+    if kv_start is not None:
+        cfg.host_kv_start = offsets(kv_start)
+    cfg.axis_dims[:len(axis_dims)] = [int(d) for d in axis_dims]
+    return cfg
+
+
+def speca_layer_workspace_bytes(q_start, dtype, kv_start=None, n_heads=0, n_kv_heads=0, head_dim=0, causal=False, scale=0.0,
+                                norm_eps=0.0, axis_dims=(), theta=10000.0, pairing=SPECA_ROPE_INTERLEAVED) -> int:
+    cfg = _layer_config(q_start, dtype, kv_start, n_heads, n_kv_heads, head_dim, causal, scale, norm_eps, axis_dims, theta, pairing)
+    out = ctypes.c_size_t(0)
+    _check(_lib().speca_layer_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)))
+    return out.value
+
+
+def speca_layer_create(q_start, dtype, workspace, kv_start=None, n_heads=0, n_kv_heads=0, head_dim=0, causal=False, scale=0.0,
+                       norm_eps=0.0, axis_dims=(), theta=10000.0, pairing=SPECA_ROPE_INTERLEAVED, device=None,
+                       workspace_bytes=None) -> int:
+    """Returns the opaque handle (an integer address). ``workspace`` is a CUDA uint8 tensor the caller keeps alive, or
+    a raw device address together with ``workspace_bytes``."""
+    if isinstance(workspace, torch.Tensor):
+        device = workspace.device.index if device is None else device
+        workspace_bytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
+    cfg = _layer_config(q_start, dtype, kv_start, n_heads, n_kv_heads, head_dim, causal, scale, norm_eps, axis_dims, theta, pairing)
+    cfg.workspace, cfg.workspace_bytes, cfg.device = _dev_ptr(workspace), workspace_bytes or 0, device or 0
+    out = ctypes.c_void_p(None)
+    _check(_lib().speca_layer_create(ctypes.byref(cfg), ctypes.byref(out)))
+    return out.value
+
+
+def speca_layer_destroy(layer) -> None:
+    _check(_lib().speca_layer_destroy(layer))
+
+
+def _check_layer(status: int, layer):
+    if status != SPECA_OK:
+        raise SpecaError(status, _lib().speca_layer_last_error(layer).decode() if layer else "")
+
+
+def speca_layer_modulate(layer, dim, x, x_stride, branch, branch_stride, gate, scale, shift, mod_stride, dev_active_mask, x_out,
+                         x_out_stride, y, y_stride, stream=None) -> None:
+    """Device addresses and strides in elements, as in the header; ``SpecaLayer.modulate`` takes tensors."""
+    _check_layer(_lib().speca_layer_modulate(layer, dim, x, x_stride, branch, branch_stride, gate, scale, shift, mod_stride,
+                                             dev_active_mask, x_out, x_out_stride, y, y_stride, _stream_ptr(stream)), layer)
+
+
+def speca_layer_rope(layer, q, q_out, k, k_out, positions, q_weight, k_weight, dev_active_mask, stream=None) -> None:
+    """q, q_out, k, k_out: (address, row stride, head stride) each; ``SpecaLayer.rope`` takes tensors."""
+    _check_layer(_lib().speca_layer_rope(layer, *q, *q_out, *k, *k_out, positions, q_weight, k_weight, dev_active_mask,
+                                         _stream_ptr(stream)), layer)
+
+
+def speca_layer_attention(layer, q, k, v, o, dev_kv_len, dev_active_mask, dev_lse, stream=None) -> None:
+    """q, k, v, o: (address, row stride, head stride) each; ``SpecaLayer.attention`` takes tensors."""
+    _check_layer(_lib().speca_layer_attention(layer, *q, *k, *v, *o, dev_kv_len, dev_active_mask, dev_lse,
+                                              _stream_ptr(stream)), layer)
+
+
+def speca_layer_check(layer, stream=None) -> None:
+    _check_layer(_lib().speca_layer_check(layer, _stream_ptr(stream)), layer)
+
+
+def speca_layer_last_error(layer) -> str:
+    return _lib().speca_layer_last_error(layer).decode()
+
+
 def speca_status_string(status: int) -> str:
     return _lib().speca_status_string(status).decode()
 
@@ -523,3 +630,104 @@ class SpecaCache:
         tdt = torch.bfloat16 if self.dtype == SPECA_BF16 else torch.float32
         off = ptr - self.arena.data_ptr()
         return self.arena[off: off + n * d * (2 if self.dtype == SPECA_BF16 else 4)].view(tdt).view(n, d)
+
+
+class SpecaLayer:
+    """The parts of a verification layer that are not plain matrix products, over packed sequences: sequence s of a
+    ``[rows, ...]`` tensor is rows ``q_start[s]`` to ``q_start[s + 1] - 1``. Owns the workspace and the handle. Tensors
+    may be strided views whose last dimension is dense; outputs are the caller's."""
+
+    def __init__(self, q_start, dtype, kv_start=None, n_heads=0, n_kv_heads=0, head_dim=0, causal=False, scale=0.0, norm_eps=0.0,
+                 axis_dims=(), theta=10000.0, pairing=SPECA_ROPE_INTERLEAVED, device="cuda:0"):
+        self.handle = None
+        self.device = torch.device(device)
+        self.n_seqs, self.n_heads, self.n_kv_heads, self.head_dim = len(q_start) - 1, n_heads, n_kv_heads, head_dim
+        self.rows = int(q_start[-1])
+        self.kv_rows = int(kv_start[-1]) if kv_start is not None else self.rows
+        self.n_axes = len(axis_dims)
+        self.torch_dtype = _TORCH_DTYPES[dtype]
+        kw = dict(kv_start=kv_start, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, causal=causal, scale=scale,
+                  norm_eps=norm_eps, axis_dims=axis_dims, theta=theta, pairing=pairing)
+        nbytes = speca_layer_workspace_bytes(q_start, dtype, **kw)
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        self.handle = speca_layer_create(q_start, dtype, self.workspace, device=self.device.index or 0, **kw)
+
+    def close(self):
+        if self.handle:
+            handle, self.handle = self.handle, None
+            speca_layer_destroy(handle)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _tensor(self, t, name, shape, dtype=None):
+        """Address of a device tensor of this shape and type whose last dimension is dense; None stays None."""
+        if t is None:
+            return None
+        if not t.is_cuda or t.device != self.device:
+            raise TypeError("%s: a tensor on %s is expected" % (name, self.device))
+        if t.dtype != (dtype or self.torch_dtype):
+            raise TypeError("%s: %s is expected, not %s" % (name, dtype or self.torch_dtype, t.dtype))
+        if t.shape != shape:
+            raise ValueError("%s: shape %s is expected, not %s" % (name, tuple(shape), tuple(t.shape)))
+        if t.stride(-1) != 1 and shape[-1] > 1:
+            raise TypeError("%s: the last dimension must be dense" % name)
+        return t.data_ptr()
+
+    def _heads(self, t, name, rows, heads):
+        if t is None:
+            return None, 0, 0
+        p = self._tensor(t, name, (rows, heads, self.head_dim))
+        s = t.stride()
+        return p, s[0], s[1]
+
+    def _on(self, stream):
+        return torch.cuda.current_stream(self.device) if stream is None else stream
+
+    def _vector(self, t, name, n, dtype):
+        if t is None:
+            return None
+        return self._tensor(t, name, (n,), dtype)
+
+    def modulate(self, x, y, branch=None, gate=None, scale=None, shift=None, x_out=None, active=None, stream=None):
+        """x' = x + gate * branch; y = layer norm of x' * (1 + scale) + shift, the modulations by sequence."""
+        dim = x.shape[-1]
+        shape, mod_shape = (self.rows, dim), (self.n_seqs, dim)
+        mods = [m for m in (gate, scale, shift) if m is not None]
+        if len({m.stride(0) for m in mods}) > 1 and self.n_seqs > 1:
+            raise ValueError("gate, scale and shift must share one row stride")
+        speca_layer_modulate(
+            self.handle, dim, self._tensor(x, "x", shape), x.stride(0), self._tensor(branch, "branch", shape),
+            0 if branch is None else branch.stride(0), self._tensor(gate, "gate", mod_shape), self._tensor(scale, "scale", mod_shape),
+            self._tensor(shift, "shift", mod_shape), mods[0].stride(0) if mods else 0,
+            self._vector(active, "active", self.n_seqs, torch.uint8), self._tensor(x_out, "x_out", shape),
+            0 if x_out is None else x_out.stride(0), self._tensor(y, "y", shape), y.stride(0), self._on(stream))
+
+    def rope(self, q, q_out, k, k_out, positions, q_weight=None, k_weight=None, active=None, stream=None):
+        """Rotary positions (``positions``: fp32 [rows, axes]) of q and k, after an RMS norm where a weight is given."""
+        pos = self._tensor(positions, "positions", (self.rows, self.n_axes), torch.float32)
+        if pos is not None and not positions.is_contiguous():
+            raise TypeError("positions: must be contiguous")
+        speca_layer_rope(
+            self.handle, self._heads(q, "q", self.rows, self.n_heads), self._heads(q_out, "q_out", self.rows, self.n_heads),
+            self._heads(k, "k", self.rows, self.n_kv_heads), self._heads(k_out, "k_out", self.rows, self.n_kv_heads), pos,
+            self._vector(q_weight, "q_weight", self.head_dim, None), self._vector(k_weight, "k_weight", self.head_dim, None),
+            self._vector(active, "active", self.n_seqs, torch.uint8), self._on(stream))
+
+    def attention(self, q, k, v, out, lse=None, kv_len=None, active=None, stream=None):
+        """out = softmax(scale q k^T) v per sequence; ``kv_len``: int32 per sequence, keys that hold data."""
+        p_lse = self._tensor(lse, "lse", (self.n_heads, self.rows), torch.float32)
+        if p_lse is not None and not lse.is_contiguous():
+            raise TypeError("lse: must be contiguous")
+        speca_layer_attention(
+            self.handle, self._heads(q, "q", self.rows, self.n_heads), self._heads(k, "k", self.kv_rows, self.n_kv_heads),
+            self._heads(v, "v", self.kv_rows, self.n_kv_heads), self._heads(out, "out", self.rows, self.n_heads),
+            self._vector(kv_len, "kv_len", self.n_seqs, torch.int32), self._vector(active, "active", self.n_seqs, torch.uint8),
+            p_lse, self._on(stream))
+
+    def check(self, stream=None):
+        """Waits for `stream` and raises if a kernel of this layer gave up on a bounded wait."""
+        speca_layer_check(self.handle, self._on(stream))

@@ -14,8 +14,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libspeca.so")
-SOURCES = ["speca_kernels.cu", "speca_static.cu", "speca_api.cpp"]
-HEADERS = [os.path.join(CSRC, "speca_internal.h"), os.path.join(ROOT, "include", "speca.h")]
+SOURCES = ["speca_kernels.cu", "speca_static.cu", "speca_layer_rows.cu", "speca_attention.cu", "speca_api.cpp", "speca_layer.cpp"]
+HEADERS = [os.path.join(CSRC, "speca_internal.h"), os.path.join(CSRC, "speca_layer_internal.h"), os.path.join(ROOT, "include", "speca.h")]
 
 
 def _nvcc() -> str:
@@ -39,7 +39,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [
-        _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+        _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
         "-Xcompiler", "-fPIC,-O2,-Wall", "-shared", "-cudart", "static",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp,
     ] + [os.path.join(CSRC, s) for s in SOURCES]

@@ -1,0 +1,249 @@
+// Attention of the verification layer.
+#include <cuda_bf16.h>
+#include <math_constants.h>
+
+#include "speca_layer_internal.h"
+
+namespace speca {
+namespace {
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+__device__ __forceinline__ AttnUnit load_unit(const AttnUnit* units, int i) {
+    AttnUnit u;
+    const int4* src = reinterpret_cast<const int4*>(units + i);
+    int4* dst = reinterpret_cast<int4*>(&u);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) dst[k] = __ldg(src + k);
+    return u;
+}
+
+// Keys of the unit's sequence that hold data.
+__device__ __forceinline__ int kv_length(const AttnParams& p, const AttnUnit& u) {
+    return p.dev_kv_len == nullptr ? u.kv_cap : max(0, min(u.kv_cap, p.dev_kv_len[u.seq]));
+}
+// Keys that query `i` of the sequence sees: those in front of this index.
+__device__ __forceinline__ int visible_keys(const AttnParams& p, const AttnUnit& u, int kv_len, int i) {
+    return p.causal ? max(0, min(kv_len, i + 1 + kv_len - u.q_len)) : kv_len;
+}
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Joins the partial results of a row block whose last share has just been written: weights exp2(m_s - m)
+// in the order of the shares, whoever came last. One warp per row, lanes across the head.
+template <typename T>
+__device__ void join_rows(const AttnParams& p, const AttnUnit& u, int row0, int rows, int64_t part, int64_t split_stride, int warp,
+                          int n_warps) {
+    const int lane = threadIdx.x % 32;
+    const int64_t pitch = part_row_floats(p.head_dim);
+    for (int r = warp; r < rows; r += n_warps) {
+        const float* base = reinterpret_cast<const float*>(p.parts + part) + r * pitch;
+        float m = -CUDART_INF_F;
+        for (int s = 0; s < u.n_splits; ++s) m = fmaxf(m, __ldcg(base + s * split_stride + pitch - 4));
+        float l = 0.f, acc[SPECA_MAX_HEAD_DIM / 32] = {};
+        for (int s = 0; s < u.n_splits; ++s) {
+            const float* q = base + s * split_stride;
+            const float ls = __ldcg(q + pitch - 3);
+            if (ls == 0.f) continue;  // this share saw nothing and left its sums unwritten
+            const float w = exp2f(__ldcg(q + pitch - 4) - m);
+            l = fmaf(w, ls, l);
+#pragma unroll
+            for (int i = 0; i < SPECA_MAX_HEAD_DIM / 32; ++i)
+                if (lane + i * 32 < p.head_dim) acc[i] = fmaf(w, __ldcg(q + lane + i * 32), acc[i]);
+        }
+        const int pr = row0 + r, tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T* o = reinterpret_cast<T*>(p.o) + tok * p.o_row + head * p.o_head;
+#pragma unroll
+        for (int i = 0; i < SPECA_MAX_HEAD_DIM / 32; ++i)
+            if (lane + i * 32 < p.head_dim) put(o + lane + i * 32, acc[i] * inv);
+        if (p.lse != nullptr && lane == 0)
+            p.lse[static_cast<int64_t>(head) * p.total_q + tok] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// fp32 arithmetic on the CUDA cores
+// ------------------------------------------------------------------------------------------------
+// 32 packed rows against tiles of 64 keys: 128 threads, each with 4 rows x 4 keys of the scores and 4 rows x 8
+// columns of the output in registers; running maximum and sum per row, so scores never leave the chip.
+constexpr int kSimtThreads = 128;
+constexpr int kSimtPitch = SPECA_MAX_HEAD_DIM + 4;  // floats; rows 4 banks apart: 16-byte reads of 8 rows do not collide
+
+struct SimtSmem {
+    float q[kSimtRows][kSimtPitch];
+    float k[kSimtKeys][kSimtPitch];
+    float v[kSimtKeys][kSimtPitch];
+    float p[kSimtRows][kSimtKeys + 4];
+    int last;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const __grid_constant__ AttnParams p) {
+    extern __shared__ __align__(16) char smem_raw[];
+    SimtSmem& sm = *reinterpret_cast<SimtSmem*>(smem_raw);
+    const AttnUnit u = load_unit(p.units, blockIdx.x);
+    if (p.dev_mask != nullptr && p.dev_mask[u.seq] == 0) return;
+    const int kv_len = kv_length(p, u);
+    const int rows = min(kSimtRows, u.q_len * p.group - u.row0);
+    const int tiles = (kv_len + kSimtKeys - 1) / kSimtKeys, share = (tiles + u.n_splits - 1) / u.n_splits;
+    const int seen = visible_keys(p, u, kv_len, (u.row0 + rows - 1) / p.group);  // by the block's last row
+    const int t0 = u.split * share, t1 = min(min(tiles, t0 + share), (seen + kSimtKeys - 1) / kSimtKeys);
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int hd = p.head_dim, hd4 = (hd + 3) / 4;
+
+    for (int i = threadIdx.x; i < kSimtRows * hd4 * 4; i += kSimtThreads) {
+        const int r = i / (hd4 * 4), c = i % (hd4 * 4), pr = u.row0 + r;
+        float x = 0.f;
+        if (r < rows && c < hd)
+            x = to_float(reinterpret_cast<const T*>(p.q)[(u.q_start + pr / p.group) * p.q_row +
+                                                         (u.kv_head * p.group + pr % p.group) * p.q_head + c]);
+        sm.q[r][c] = x;
+    }
+    int limit[4];
+    float m[4], l[4], acc[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = ty * 4 + r;
+        limit[r] = row < rows ? visible_keys(p, u, kv_len, (u.row0 + row) / p.group) : 0;
+        m[r] = -CUDART_INF_F;
+        l[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[r][c] = 0.f;
+    }
+    for (int t = t0; t < t1; ++t) {
+        const int key0 = t * kSimtKeys;
+        __syncthreads();  // the previous tile has been read
+        for (int i = threadIdx.x; i < kSimtKeys * hd4 * 4; i += kSimtThreads) {
+            const int r = i / (hd4 * 4), c = i % (hd4 * 4);
+            float kx = 0.f, vx = 0.f;  // keys behind kv_len are not read: a weight of zero times whatever they hold may be NaN
+            if (key0 + r < kv_len && c < hd) {
+                const int64_t row = u.kv_start + key0 + r;
+                kx = to_float(reinterpret_cast<const T*>(p.k)[row * p.k_row + u.kv_head * p.k_head + c]);
+                vx = to_float(reinterpret_cast<const T*>(p.v)[row * p.v_row + u.kv_head * p.v_head + c]);
+            }
+            sm.k[r][c] = kx;
+            sm.v[r][c] = vx;
+        }
+        __syncthreads();
+        float s[4][4] = {};
+        for (int c = 0; c < hd4; ++c) {
+            float4 qa[4], kb[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) qa[r] = *reinterpret_cast<const float4*>(&sm.q[ty * 4 + r][c * 4]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kb[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][c * 4]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    s[r][j] = fmaf(qa[r].w, kb[j].w, fmaf(qa[r].z, kb[j].z, fmaf(qa[r].y, kb[j].y, fmaf(qa[r].x, kb[j].x, s[r][j]))));
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float top = -CUDART_INF_F;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[r][j] = key0 + tx + 16 * j < limit[r] ? s[r][j] * p.scale_log2 : -CUDART_INF_F;
+                top = fmaxf(top, s[r][j]);
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            top = fmaxf(top, m[r]);
+            const float ref = top == -CUDART_INF_F ? 0.f : top;  // a row that has seen nothing yet
+            const float f = exp2f(m[r] - ref);
+            m[r] = top;
+            float sum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float e = exp2f(s[r][j] - ref);
+                sum += e;
+                sm.p[ty * 4 + r][tx + 16 * j] = e;
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            l[r] = fmaf(l[r], f, sum);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) acc[r][c] *= f;
+        }
+        __syncwarp();  // rows of p belong to one half warp
+        for (int k = 0; k < kSimtKeys; k += 4) {
+            float4 pr[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) pr[r] = *reinterpret_cast<const float4*>(&sm.p[ty * 4 + r][k]);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (tx * 4 + h * 64 >= hd) continue;
+                    const float4 v = *reinterpret_cast<const float4*>(&sm.v[k + kk][tx * 4 + h * 64]);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float w = kk == 0 ? pr[r].x : kk == 1 ? pr[r].y : kk == 2 ? pr[r].z : pr[r].w;
+                        acc[r][h * 4 + 0] = fmaf(w, v.x, acc[r][h * 4 + 0]);
+                        acc[r][h * 4 + 1] = fmaf(w, v.y, acc[r][h * 4 + 1]);
+                        acc[r][h * 4 + 2] = fmaf(w, v.z, acc[r][h * 4 + 2]);
+                        acc[r][h * 4 + 3] = fmaf(w, v.w, acc[r][h * 4 + 3]);
+                    }
+                }
+            }
+        }
+        __syncwarp();
+    }
+    const int64_t pitch = part_row_floats(hd), split_stride = static_cast<int64_t>(rows) * pitch;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = ty * 4 + r, pr = u.row0 + row;
+        if (row >= rows) continue;
+        if (u.n_splits > 1) {
+            float* part = reinterpret_cast<float*>(p.parts + u.part) + u.split * split_stride + row * pitch;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const int col = tx * 4 + (c / 4) * 64 + c % 4;
+                if (col < hd) part[col] = acc[r][c];
+            }
+            if (tx == 0) {
+                part[pitch - 4] = m[r];
+                part[pitch - 3] = l[r];
+            }
+            continue;
+        }
+        const int tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
+        const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+        T* o = reinterpret_cast<T*>(p.o) + tok * p.o_row + head * p.o_head;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int col = tx * 4 + (c / 4) * 64 + c % 4;
+            if (col < hd) put(o + col, acc[r][c] * inv);
+        }
+        if (p.lse != nullptr && tx == 0)
+            p.lse[static_cast<int64_t>(head) * p.total_q + tok] = l[r] == 0.f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * kLn2;
+    }
+    if (u.n_splits == 1) return;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sm.last = atomicAdd(p.tickets + u.ticket, 1u) == static_cast<uint32_t>(u.n_splits) - 1;
+        if (sm.last) p.tickets[u.ticket] = 0;  // ready for the next launch
+    }
+    __syncthreads();
+    if (!sm.last) return;
+    __threadfence();
+    join_rows<T>(p, u, u.row0, rows, u.part, split_stride, threadIdx.x / 32, kSimtThreads / 32);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_simt(const AttnParams& p, int dtype, cudaStream_t stream) {
+    if (p.n_units == 0) return cudaSuccess;
+    auto* kernel = dtype == SPECA_BF16 ? attention_simt_kernel<__nv_bfloat16> : attention_simt_kernel<float>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SimtSmem));
+    if (e != cudaSuccess) return e;
+    kernel<<<p.n_units, kSimtThreads, sizeof(SimtSmem), stream>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace speca

@@ -1,0 +1,82 @@
+// Internal declarations shared by the verification layer's host dispatch (speca_layer.cpp) and its
+// kernels (speca_layer_rows.cu, speca_attention.cu). Not part of the public ABI.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "speca.h"
+
+namespace speca {
+
+// ---- row kernels --------------------------------------------------------------------------------
+struct ModulateParams {
+    const uint16_t* row_seq;  // sequence of every query row
+    const uint8_t* dev_mask;
+    const char *x, *branch, *gate, *scale, *shift;
+    char *x_out, *y;
+    int64_t x_stride, branch_stride, mod_stride, x_out_stride, y_stride;  // elements
+    int32_t rows, dim;
+    float eps;
+};
+// `vec`: elements per access (16 bytes of them, or 1 where a pointer, a stride or dim does not allow it)
+cudaError_t launch_modulate(const ModulateParams& p, int dtype, int vec, cudaStream_t stream);
+
+// Frequency of one pair of a head in turns (2 pi) per unit of position, and the axis it turns by (-1: kept).
+struct RopePair {
+    double turns;
+    int32_t axis;
+    int32_t pad;
+};
+struct RopeParams {
+    const uint16_t* row_seq;
+    const uint8_t* dev_mask;
+    const RopePair* pairs;  // [head_dim / 2]
+    const char *q, *k, *q_weight, *k_weight;
+    char *q_out, *k_out;
+    const float* positions;
+    int64_t q_row, q_head, qo_row, qo_head, k_row, k_head, ko_row, ko_head;  // strides, elements
+    int32_t rows, n_heads, n_kv_heads, head_dim, n_axes;
+    int32_t half;  // HALVES: distance of a pair's elements (R / 2); 0 = INTERLEAVED
+    float eps;
+};
+cudaError_t launch_rope(const RopeParams& p, int dtype, bool vectors, cudaStream_t stream);
+
+// ---- attention ----------------------------------------------------------------------------------
+// One unit: up to attn_rows() packed rows of one (sequence, key head), against one share of the
+// sequence's key tiles. Packed row r of a sequence is query r / group, query head kv_head * group + r % group:
+// the heads that share a key head share its tiles.
+struct AttnUnit {
+    int32_t seq, kv_head;
+    int32_t row0;     // first packed row
+    int32_t q_len, kv_cap;
+    int32_t q_start, kv_start;
+    int32_t split, n_splits;
+    int32_t ticket;   // n_splits > 1: first of the unit's counters
+    int64_t part;     // n_splits > 1: byte offset of the partial results of split 0 of this row block
+};
+static_assert(sizeof(AttnUnit) == 48, "three 16-byte loads");
+
+struct AttnParams {
+    const AttnUnit* units;
+    int32_t n_units;
+    int32_t n_heads, n_kv_heads, group, head_dim;
+    int32_t causal, total_q;
+    float scale_log2;  // scale * log2(e)
+    const char *q, *k, *v;
+    char* o;
+    int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;  // elements
+    const int32_t* dev_kv_len;
+    const uint8_t* dev_mask;
+    float* lse;
+    char* parts;        // partial results of split rows
+    uint32_t* tickets;  // arrival counters of split rows, zero between launches
+    uint32_t* gave_up;  // set by a wait that ran out
+};
+// Rows of a unit and keys of a tile of the kernel that serves a storage type.
+constexpr int kSimtRows = 32, kSimtKeys = 64;
+cudaError_t launch_attention_simt(const AttnParams& p, int dtype, cudaStream_t stream);
+
+// Partial result of one row: head_dim sums, then the running maximum (log2 domain) and the sum.
+__host__ __device__ constexpr int64_t part_row_floats(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }
+
+}  // namespace speca
