@@ -1,69 +1,9 @@
-// Attention of the verification layer.
-#include <cuda_bf16.h>
-#include <math_constants.h>
+// Attention of the verification layer in fp32, on the CUDA cores.
 
-#include "speca_layer_internal.h"
+#include "speca_attention_common.cuh"
 
 namespace speca {
 namespace {
-
-__device__ __forceinline__ float to_float(float x) { return x; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
-
-__device__ __forceinline__ AttnUnit load_unit(const AttnUnit* units, int i) {
-    AttnUnit u;
-    const int4* src = reinterpret_cast<const int4*>(units + i);
-    int4* dst = reinterpret_cast<int4*>(&u);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) dst[k] = __ldg(src + k);
-    return u;
-}
-
-// Keys of the unit's sequence that hold data.
-__device__ __forceinline__ int kv_length(const AttnParams& p, const AttnUnit& u) {
-    return p.dev_kv_len == nullptr ? u.kv_cap : max(0, min(u.kv_cap, p.dev_kv_len[u.seq]));
-}
-// Keys that query `i` of the sequence sees: those in front of this index.
-__device__ __forceinline__ int visible_keys(const AttnParams& p, const AttnUnit& u, int kv_len, int i) {
-    return p.causal ? max(0, min(kv_len, i + 1 + kv_len - u.q_len)) : kv_len;
-}
-
-constexpr float kLn2 = 0.6931471805599453f;
-
-// Joins the partial results of a row block whose last share has just been written: weights exp2(m_s - m)
-// in the order of the shares, whoever came last. One warp per row, lanes across the head.
-template <typename T>
-__device__ void join_rows(const AttnParams& p, const AttnUnit& u, int row0, int rows, int64_t part, int64_t split_stride, int warp,
-                          int n_warps) {
-    const int lane = threadIdx.x % 32;
-    const int64_t pitch = part_row_floats(p.head_dim);
-    for (int r = warp; r < rows; r += n_warps) {
-        const float* base = reinterpret_cast<const float*>(p.parts + part) + r * pitch;
-        float m = -CUDART_INF_F;
-        for (int s = 0; s < u.n_splits; ++s) m = fmaxf(m, __ldcg(base + s * split_stride + pitch - 4));
-        float l = 0.f, acc[SPECA_MAX_HEAD_DIM / 32] = {};
-        for (int s = 0; s < u.n_splits; ++s) {
-            const float* q = base + s * split_stride;
-            const float ls = __ldcg(q + pitch - 3);
-            if (ls == 0.f) continue;  // this share saw nothing and left its sums unwritten
-            const float w = exp2f(__ldcg(q + pitch - 4) - m);
-            l = fmaf(w, ls, l);
-#pragma unroll
-            for (int i = 0; i < SPECA_MAX_HEAD_DIM / 32; ++i)
-                if (lane + i * 32 < p.head_dim) acc[i] = fmaf(w, __ldcg(q + lane + i * 32), acc[i]);
-        }
-        const int pr = row0 + r, tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* o = reinterpret_cast<T*>(p.o) + tok * p.o_row + head * p.o_head;
-#pragma unroll
-        for (int i = 0; i < SPECA_MAX_HEAD_DIM / 32; ++i)
-            if (lane + i * 32 < p.head_dim) put(o + lane + i * 32, acc[i] * inv);
-        if (p.lse != nullptr && lane == 0)
-            p.lse[static_cast<int64_t>(head) * p.total_q + tok] = l == 0.f ? -CUDART_INF_F : (m + log2f(l)) * kLn2;
-    }
-}
 
 // ------------------------------------------------------------------------------------------------
 // fp32 arithmetic on the CUDA cores
@@ -81,8 +21,7 @@ struct SimtSmem {
     int last;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const __grid_constant__ AttnParams p) {
+__global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __grid_constant__ AttnParams p) {
     extern __shared__ __align__(16) char smem_raw[];
     SimtSmem& sm = *reinterpret_cast<SimtSmem*>(smem_raw);
     const AttnUnit u = load_unit(p.units, blockIdx.x);
@@ -99,8 +38,8 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const __gr
         const int r = i / (hd4 * 4), c = i % (hd4 * 4), pr = u.row0 + r;
         float x = 0.f;
         if (r < rows && c < hd)
-            x = to_float(reinterpret_cast<const T*>(p.q)[(u.q_start + pr / p.group) * p.q_row +
-                                                         (u.kv_head * p.group + pr % p.group) * p.q_head + c]);
+            x = reinterpret_cast<const float*>(p.q)[(u.q_start + pr / p.group) * p.q_row +
+                                                    (u.kv_head * p.group + pr % p.group) * p.q_head + c];
         sm.q[r][c] = x;
     }
     int limit[4];
@@ -122,8 +61,8 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const __gr
             float kx = 0.f, vx = 0.f;  // keys behind kv_len are not read: a weight of zero times whatever they hold may be NaN
             if (key0 + r < kv_len && c < hd) {
                 const int64_t row = u.kv_start + key0 + r;
-                kx = to_float(reinterpret_cast<const T*>(p.k)[row * p.k_row + u.kv_head * p.k_head + c]);
-                vx = to_float(reinterpret_cast<const T*>(p.v)[row * p.v_row + u.kv_head * p.v_head + c]);
+                kx = reinterpret_cast<const float*>(p.k)[row * p.k_row + u.kv_head * p.k_head + c];
+                vx = reinterpret_cast<const float*>(p.v)[row * p.v_row + u.kv_head * p.v_head + c];
             }
             sm.k[r][c] = kx;
             sm.v[r][c] = vx;
@@ -213,11 +152,11 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const __gr
         }
         const int tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
         const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
-        T* o = reinterpret_cast<T*>(p.o) + tok * p.o_row + head * p.o_head;
+        float* o = reinterpret_cast<float*>(p.o) + tok * p.o_row + head * p.o_head;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             const int col = tx * 4 + (c / 4) * 64 + c % 4;
-            if (col < hd) put(o + col, acc[r][c] * inv);
+            if (col < hd) o[col] = acc[r][c] * inv;
         }
         if (p.lse != nullptr && tx == 0)
             p.lse[static_cast<int64_t>(head) * p.total_q + tok] = l[r] == 0.f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * kLn2;
@@ -232,17 +171,16 @@ __global__ void __launch_bounds__(kSimtThreads) attention_simt_kernel(const __gr
     __syncthreads();
     if (!sm.last) return;
     __threadfence();
-    join_rows<T>(p, u, u.row0, rows, u.part, split_stride, threadIdx.x / 32, kSimtThreads / 32);
+    join_rows<float>(p, u, u.row0, rows, u.part, split_stride, threadIdx.x / 32, kSimtThreads / 32);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_simt(const AttnParams& p, int dtype, cudaStream_t stream) {
+cudaError_t launch_attention_f32(const AttnParams& p, cudaStream_t stream) {
     if (p.n_units == 0) return cudaSuccess;
-    auto* kernel = dtype == SPECA_BF16 ? attention_simt_kernel<__nv_bfloat16> : attention_simt_kernel<float>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SimtSmem));
+    cudaError_t e = cudaFuncSetAttribute(attention_f32_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SimtSmem));
     if (e != cudaSuccess) return e;
-    kernel<<<p.n_units, kSimtThreads, sizeof(SimtSmem), stream>>>(p);
+    attention_f32_kernel<<<p.n_units, kSimtThreads, sizeof(SimtSmem), stream>>>(p);
     return cudaGetLastError();
 }
 

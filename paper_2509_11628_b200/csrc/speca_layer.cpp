@@ -23,12 +23,16 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // How the attention of a storage type cuts its work.
 struct Tiling {
     int rows;          // most packed rows of a unit
+    int counters;      // arrival counters of a shared row block
     int keys;          // keys of a tile
     int target;        // units that fill the device: below it, long key ranges are shared out
     int min_share;     // fewest tiles worth a unit of its own
 };
-// 148 SMs x 2 resident blocks.
-constexpr Tiling kSimtTiling = {kSimtRows, kSimtKeys, 296, 4};
+// 148 SMs, with two resident blocks each in fp32 and one in bf16.
+Tiling tiling(int dtype, int group) {
+    if (dtype == SPECA_BF16) return Tiling{tc_unit_rows(group), 2, kTcKeys, 148, 4};
+    return Tiling{kSimtRows, 1, kSimtKeys, 296, 4};
+}
 
 struct Plan {
     std::vector<AttnUnit> units;
@@ -88,8 +92,8 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
     size_t part_bytes = 0;
     int n_tickets = 0;
     if (heads) {
-        const Tiling& tl = kSimtTiling;
         const int group = c->n_heads / c->n_kv_heads;
+        const Tiling tl = tiling(c->dtype, group);
         const int rows = tl.rows;
         auto blocks = [&](int s) { return ((qs[s + 1] - qs[s]) * group + rows - 1) / rows; };
         auto tiles = [&](int s) { return (ks[s + 1] - ks[s] + tl.keys - 1) / tl.keys; };
@@ -147,7 +151,7 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
                         cost.push_back(std::max<int64_t>(0, std::min(part_nt, (seen + tl.keys - 1) / tl.keys - i * part_nt)));
                     }
                     if (splits > 1) {
-                        n_tickets += 1;
+                        n_tickets += tl.counters;
                         part_bytes += static_cast<size_t>(splits * n * row_bytes);
                     }
                 }
@@ -206,10 +210,10 @@ struct DeviceGuard {
 struct speca_layer {
     int n_seqs, dtype, n_heads, n_kv_heads, head_dim, causal, n_axes, pairing, rotated, device;
     int64_t total_q, total_kv;
-    int n_units;
+    int n_units, sm_count;
     float scale, norm_eps;
     char* ws;
-    size_t units_off, row_seq_off, pairs_off, tickets_off, gave_up_off, parts_off;
+    size_t units_off, row_seq_off, pairs_off, tickets_off, gave_up_off, parts_off, counters_bytes;
     char last_error[256];
 };
 
@@ -300,6 +304,8 @@ speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t
     c->tickets_off = P.tickets_off;
     c->gave_up_off = P.gave_up_off;
     c->parts_off = P.parts_off;
+    c->counters_bytes = P.counters_bytes;
+    cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
     DeviceGuard guard(c->device);
     ce = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
     auto upload = [&](size_t off, const void* src, size_t n) {
@@ -481,7 +487,10 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
     if (!guard.ok) return fail(c, SPECA_ERR_CUDA, "cudaSetDevice failed");
     speca_status_t st = check_sticky(c);
     if (st != SPECA_OK) return st;
-    cudaError_t e = launch_attention_simt(p, c->dtype, static_cast<cudaStream_t>(stream));
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t e = c->dtype == SPECA_BF16 ? launch_attention_bf16(p, c->total_kv, c->sm_count, s) : launch_attention_f32(p, s);
+    if (e == cudaErrorNotSupported)
+        return fail(c, SPECA_ERR_UNSUPPORTED, "attention: the copy engine cannot address a tensor with these strides");
     return e == cudaSuccess ? SPECA_OK : cuda_fail(c, e, "attention");
 }
 
@@ -493,7 +502,8 @@ speca_status_t speca_layer_check(speca_layer_t* c, void* stream) {
     uint32_t gave_up = 0;
     cudaError_t e = cudaMemcpyAsync(&gave_up, c->ws + c->gave_up_off, sizeof gave_up, cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    if (e == cudaSuccess && gave_up != 0) e = cudaMemsetAsync(c->ws + c->gave_up_off, 0, sizeof gave_up, s);
+    // the flag and the arrival counters, which a kernel that gave up may have left in between
+    if (e == cudaSuccess && gave_up != 0) e = cudaMemsetAsync(c->ws + c->gave_up_off, 0, c->counters_bytes, s);
     if (e != cudaSuccess) return cuda_fail(c, e, "check");
     return gave_up == 0 ? SPECA_OK : fail(c, SPECA_ERR_CUDA, "a kernel gave up on a bounded wait: results since the last check are incomplete");
 }

@@ -1,5 +1,5 @@
 // Internal declarations shared by the verification layer's host dispatch (speca_layer.cpp) and its
-// kernels (speca_layer_rows.cu, speca_attention.cu). Not part of the public ABI.
+// kernels (speca_layer_rows.cu, speca_attention_*.cu). Not part of the public ABI.
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -42,7 +42,7 @@ struct RopeParams {
 cudaError_t launch_rope(const RopeParams& p, int dtype, bool vectors, cudaStream_t stream);
 
 // ---- attention ----------------------------------------------------------------------------------
-// One unit: up to attn_rows() packed rows of one (sequence, key head), against one share of the
+// One unit: a block of packed rows of one (sequence, key head), against one share of the
 // sequence's key tiles. Packed row r of a sequence is query r / group, query head kv_head * group + r % group:
 // the heads that share a key head share its tiles.
 struct AttnUnit {
@@ -51,7 +51,7 @@ struct AttnUnit {
     int32_t q_len, kv_cap;
     int32_t q_start, kv_start;
     int32_t split, n_splits;
-    int32_t ticket;   // n_splits > 1: first of the unit's counters
+    int32_t ticket;   // n_splits > 1: first of the row block's arrival counters
     int64_t part;     // n_splits > 1: byte offset of the partial results of split 0 of this row block
 };
 static_assert(sizeof(AttnUnit) == 48, "three 16-byte loads");
@@ -72,9 +72,12 @@ struct AttnParams {
     uint32_t* tickets;  // arrival counters of split rows, zero between launches
     uint32_t* gave_up;  // set by a wait that ran out
 };
-// Rows of a unit and keys of a tile of the kernel that serves a storage type.
-constexpr int kSimtRows = 32, kSimtKeys = 64;
-cudaError_t launch_attention_simt(const AttnParams& p, int dtype, cudaStream_t stream);
+constexpr int kSimtRows = 32, kSimtKeys = 64;  // rows of a unit, keys of a tile
+cudaError_t launch_attention_f32(const AttnParams& p, cudaStream_t stream);
+// Rows of a unit: two blocks of up to 128, whole queries. NotSupported: the copy engine cannot address a tensor.
+__host__ __device__ constexpr int tc_unit_rows(int group) { return 2 * (128 / group * group); }
+constexpr int kTcKeys = 128;
+cudaError_t launch_attention_bf16(const AttnParams& p, int64_t total_kv, int sm_count, cudaStream_t stream);
 
 // Partial result of one row: head_dim sums, then the running maximum (log2 domain) and the sum.
 __host__ __device__ constexpr int64_t part_row_floats(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }
