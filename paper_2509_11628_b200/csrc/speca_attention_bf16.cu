@@ -6,7 +6,7 @@
 // products run, the other's exponentials are formed. One unit at a time per SM, blocks persistent over units:
 //   warps 0-3, 4-7   softmax and output of block 0 and block 1: one thread per row, its 128 scores in registers
 //   warp 8           TMA loads: Q of the unit, then K_0, V_0, K_1, V_1, ... through a ring of tiles
-//   warp 9           issues the products (warps 10 and 11 complete the warpgroup)
+//   warps 9, 10      issue the products of block 0 and block 1 (warp 11 completes the warpgroup)
 // Products of one thread run in the order of issue, so S_b(j+1) may overwrite P_b(j) right behind the product
 // that reads it, and S_b(j+1) being ready says that O_b is at rest: the softmax threads themselves rescale O in the
 // rare tile that raises a row's maximum by more than 2^8 (sums and P are exact to a common factor; it keeps
@@ -21,11 +21,14 @@ namespace {
 
 // Three warpgroups of 168 registers a thread at launch; the two that form the softmax take 216 (a row of 128 scores
 // and its packed weights stay in registers), the one that loads and issues gives up what they take: 2 x 216 + 72 = 3 x 168.
+// (Two threads per row, 16 softmax warps of 104 registers, measured the same: what the shorter chains gain, telling each
+// other the maximum through shared memory costs.)
 constexpr int kTcThreads = 384;
+constexpr int kLoadWarp = 8, kIssueWarp = 9;
 constexpr int kBlockRows = 128;
 constexpr int kTileKeys = 128;
 constexpr uint32_t kPanelBytes = 128 * 128;  // 128 rows of 64 bf16: one 128-byte swizzle span per row
-constexpr uint32_t kSpinLimit = 1u << 20;    // polls of one wait; a healthy one ends within a few hundred
+constexpr uint32_t kSpinLimit = 1u << 18;    // polls of one wait (each sleeps up to 1.5 us); a healthy wait needs a few
 constexpr float kRescale = 8.f;              // log2 growth of a row's maximum that is left in P
 constexpr uint32_t kTmemCols = 512;          // S_0, S_1 (P over them), O_0, O_1: 128 columns each
 
@@ -36,13 +39,13 @@ struct Barriers {
     uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
     uint64_t kv_full[8], kv_empty[8];
     uint64_t part_done[2], last_set[2];
-    uint64_t drain;
+    uint64_t turn[2], drain[2];
     uint32_t tmem;
     uint32_t abort;
     uint32_t last[2];
 };
 constexpr uint32_t smem_bytes(int panels) {
-    return 1024 + (2 + ring_stages(panels)) * panels * kPanelBytes + static_cast<uint32_t>(sizeof(Barriers));
+    return (2 + ring_stages(panels)) * panels * kPanelBytes + static_cast<uint32_t>(sizeof(Barriers));
 }
 static_assert(smem_bytes(2) <= 232448 && smem_bytes(1) > 116224, "fits one SM, and no two blocks share one (tensor memory)");
 
@@ -66,24 +69,26 @@ __device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-// False when the phase did not complete within the limit, or another warp has given up. One thread waits.
-__device__ __forceinline__ bool bar_wait(Barriers& b, uint64_t* bar, uint32_t parity) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+// False when the phase did not complete within the limit. One thread waits.
+__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
+    for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
         if (bar_try(bar, parity)) return true;
-        if (spin % 256 == 255 && *reinterpret_cast<volatile uint32_t*>(&b.abort) != 0) return false;
-    }
-    *reinterpret_cast<volatile uint32_t*>(&b.abort) = 1;
     return false;
 }
-// The same for a whole warp, whose lanes all get one answer and leave together.
-__device__ __forceinline__ bool warp_wait(Barriers& b, uint64_t* bar, uint32_t parity) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+// The same for a whole warp, whose lanes all get one answer. The lanes may wait for different barriers: a wait that is
+// already satisfied takes 100 to 250 cycles to say so, several at once no more.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
+    for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
         if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
-        if (spin % 256 == 255 && __any_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&b.abort) != 0)) return false;
-    }
-    *reinterpret_cast<volatile uint32_t*>(&b.abort) = 1;
-    __syncwarp();
     return false;
+}
+// True in one lane of the converged warp. Unlike a comparison with a lane index it tells the compiler that one thread
+// is left, so the operands of the tensor instructions behind it go to uniform registers without a loop over lanes
+// (which cost 125 cycles an instruction).
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes != 0;
 }
 template <int N>
 __device__ __forceinline__ void more_registers() {
@@ -181,6 +186,79 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+// Two fp32 in one 64-bit register pair, for the packed instructions.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t r, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// 2^x of a pair without the special function unit, which forms 16 a cycle and SM where the products of a tile leave time
+// for just as many: x = n + f, |f| <= 1/2, n by adding 1.5 * 2^23 (its low bits are then n), 2^f by the polynomial of degree 3 of the
+// least relative error on [-1/2, 1/2] (Remez exchange; 7.5e-5, a fiftieth of bf16's rounding), n into the exponent. Below
+// 2^-125 the weight is zero, as the special function unit gives it below 2^-126; a NaN stays one.
+__device__ __forceinline__ void ex2_poly(uint64_t x2, float& e0, float& e1) {
+    float x0, x1;
+    unpair(x2, x0, x1);
+    const uint64_t magic = pair(12582912.f, 12582912.f), minus = pair(-1.f, -1.f);
+    const uint64_t t = add2(x2, magic);
+    const uint64_t f = add2(x2, fma2(t, minus, magic));
+    uint64_t y = fma2(f, pair(0.05517167f, 0.05517167f), pair(0.24261112f, 0.24261112f));
+    y = fma2(y, f, pair(0.69326099f, 0.69326099f));
+    y = fma2(y, f, pair(0.99992807f, 0.99992807f));
+    float t0, t1;
+    unpair(t, t0, t1);
+    unpair(y, e0, e1);
+    e0 = x0 >= -125.f ? __uint_as_float(__float_as_uint(e0) + (__float_as_uint(t0) << 23)) : max_nan(x0, 0.f);
+    e1 = x1 >= -125.f ? __uint_as_float(__float_as_uint(e1) + (__float_as_uint(t1) << 23)) : max_nan(x1, 0.f);
+}
+constexpr int kPolyEvery = 4;  // of the pairs, one in this many by polynomial (0: none)
+
+// Weights of 64 keys of a row, rounded to bf16, and their sum before the rounding.
+template <int EVERY>
+__device__ __forceinline__ void weights(const float* s, uint64_t scale2, uint64_t shift2, uint32_t* packed, uint64_t* l) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c) {
+        const uint64_t x2 = fma2(pair(s[2 * c], s[2 * c + 1]), scale2, shift2);
+        float e0, e1;
+        if (EVERY > 0 && c % (EVERY > 0 ? EVERY : 1) == EVERY - 1) {
+            ex2_poly(x2, e0, e1);
+        } else {
+            unpair(x2, e0, e1);
+            e0 = ex2(e0);
+            e1 = ex2(e1);
+        }
+        packed[c] = pack_bf16(e0, e1);
+        l[c % 2] = add2(l[c % 2], pair(e0, e1));
+    }
+}
+
 // What a unit asks of its two blocks.
 struct Work {
     int kv_len;
@@ -216,21 +294,183 @@ struct Ring {
     }
 };
 
-// PANELS: panels of 64 columns that a head spans (head_dim <= 64 or <= 128).
+// Shared memory of a block: Q of both row blocks, the ring of key and value tiles, the barriers.
 template <int PANELS>
+struct Smem {
+    static constexpr int kStages = ring_stages(PANELS);
+    static constexpr uint32_t kTileBytes = PANELS * kPanelBytes;
+    char* base;
+    __device__ __forceinline__ uint32_t q(int b) const { return smem_u32(base) + b * kTileBytes; }
+    __device__ __forceinline__ uint32_t kv(int stage) const { return smem_u32(base) + (2 + stage) * kTileBytes; }
+    __device__ __forceinline__ char* kv_ptr(int stage) const { return base + (2 + stage) * kTileBytes; }
+    __device__ __forceinline__ Barriers& bar() const { return *reinterpret_cast<Barriers*>(base + (2 + kStages) * kTileBytes); }
+};
+
+// ---- loads: one thread. False: a wait ran out ----
+template <int PANELS>
+__device__ __forceinline__ bool load_tiles(const AttnParams& p, const CUtensorMap& map_q, const CUtensorMap& map_k,
+                                           const CUtensorMap& map_v, const Smem<PANELS>& sm) {
+    constexpr uint32_t kTileBytes = Smem<PANELS>::kTileBytes;
+    constexpr int kStages = Smem<PANELS>::kStages;
+    Barriers& bar = sm.bar();
+    const int tokens = kBlockRows / p.group, block_rows = tokens * p.group;
+    Ring ring;
+    uint32_t q_phase = 0;  // bit b: block b
+    bool ok = true;
+    auto load_tile = [&](const CUtensorMap& map, int head, int row) {
+        if (!bar_wait(&bar.kv_empty[ring.stage], ring.phase ^ 1)) return false;
+        bar_expect(&bar.kv_full[ring.stage], kTileBytes);
+        for (int i = 0; i < PANELS; ++i)
+            tma_load(sm.kv(ring.stage) + i * kPanelBytes, &map, i * 64, head, row, &bar.kv_full[ring.stage]);
+        ring.next(kStages);
+        return true;
+    };
+    for (int i = blockIdx.x; i < p.n_units && ok; i += gridDim.x) {
+        const AttnUnit u = load_unit(p.units, i);
+        Work w;
+        if (!unit_work(p, u, block_rows, w)) continue;
+        const int n = max(w.n[0], w.n[1]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (w.n[b] > 0 && ok) {
+                ok = bar_wait(&bar.q_empty[b], (q_phase >> b & 1) ^ 1);
+                if (ok) {
+                    bar_expect(&bar.q_full[b], static_cast<uint32_t>(block_rows) * 128 * PANELS);
+                    for (int k = 0; k < PANELS; ++k)
+                        tma_load(sm.q(b) + k * kPanelBytes, &map_q, k * 64, u.kv_head * p.group,
+                                 u.q_start + u.row0 / p.group + b * tokens, &bar.q_full[b]);
+                    q_phase ^= 1u << b;
+                }
+            }
+            if (b == 0 && n > 0) ok = ok && load_tile(map_k, u.kv_head, u.kv_start + w.t0 * kTileKeys);
+        }
+        for (int j = 0; j < n && ok; ++j) {
+            const int row = u.kv_start + (w.t0 + j) * kTileKeys;
+            ok = load_tile(map_v, u.kv_head, row) && (j + 1 == n || load_tile(map_k, u.kv_head, row + kTileKeys));
+        }
+    }
+    if (ok) return true;
+    // copies in flight must land before the block gives its shared memory back
+    for (int i = 0; i < kStages; ++i) bar_wait(&bar.kv_full[i], i < ring.stage ? ring.phase : ring.phase ^ 1);
+    for (int b = 0; b < 2; ++b) bar_wait(&bar.q_full[b], (q_phase >> b & 1) ^ 1);
+    return false;
+}
+
+// ---- products of row block b: one warp, of which one thread issues. False: a wait ran out ----
+template <int STEPS>
+__device__ __forceinline__ bool issue_products(const AttnParams& p, const Smem<(STEPS + 3) / 4>& sm, uint32_t tmem, int b) {
+    constexpr int kPanels = (STEPS + 3) / 4, kStages = Smem<kPanels>::kStages;
+    constexpr uint32_t kDescS = mma_desc(kTileKeys, false), kDescO = mma_desc(16 * STEPS, true);
+    Barriers& bar = sm.bar();
+    const int block_rows = kBlockRows / p.group * p.group;
+    const int part = threadIdx.x % 4;  // the lanes wait for four things at once
+    const uint32_t tmem_s = tmem + b * 128, tmem_o = tmem + 256 + b * 128;
+    const uint64_t q_desc = smem_desc(sm.q(b), 16, 1024);
+    Ring ring;
+    uint32_t q_phase = 0, p_phase = 0, turn = 0;
+    constexpr int kHandOver = STEPS > 2 ? STEPS - 2 : 0;
+    auto score = [&](int stage, bool hand_over) {  // S = Q K^T
+        const uint64_t k_desc = smem_desc(sm.kv(stage), 16, 1024);
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            if (k == kHandOver && hand_over) bar_arrive(&bar.turn[1 - b]);
+            const uint64_t step = (k / 4) * (kPanelBytes / 16) + (k % 4) * 2;
+            mma_ss(tmem_s, q_desc + step, k_desc + step, kDescS, k > 0);
+        }
+        tc_commit(&bar.s_full[b]);
+    };
+    for (int i = blockIdx.x; i < p.n_units; i += gridDim.x) {
+        const AttnUnit u = load_unit(p.units, i);
+        Work w;
+        if (!unit_work(p, u, block_rows, w)) continue;
+        const int n = max(w.n[0], w.n[1]), own = b == 0 ? w.n[0] : w.n[1];
+        if (own > 0) {
+            if (!warp_wait(part == 0 ? &bar.q_full[b] : &bar.kv_full[ring.stage], part == 0 ? q_phase : ring.phase)) return false;
+            q_phase ^= 1;
+            tc_fence_after();
+            if (elect_one()) {
+                score(ring.stage, false);
+                if (own == 1) tc_commit(&bar.q_empty[b]);
+                tc_commit(&bar.kv_empty[ring.stage]);
+            }
+            __syncwarp();
+            ring.next(kStages);
+        }
+#pragma unroll 1
+        for (int j = 0; j < own; ++j) {
+            const Ring v_at = ring;
+            ring.next(kStages);
+            const Ring k_at = j + 1 < own ? ring : v_at;  // the last tile waits for no further keys
+            // The last tile may hold other rows behind kv_len. The product stops at the next multiple of 16 keys and the
+            // rows up to there are cleared (by both blocks): their weight is zero, but zero times NaN is not.
+            const int valid = min(kTileKeys, w.kv_len - (w.t0 + j) * kTileKeys), steps = (valid + 15) / 16;
+            if (valid < steps * 16) {
+                if (!warp_wait(&bar.kv_full[v_at.stage], v_at.phase)) return false;
+                char* v = sm.kv_ptr(v_at.stage) + valid * 128;
+                for (int e = threadIdx.x % 32; e < (steps * 16 - valid) * 8; e += 32)
+                    for (int k = 0; k < kPanels; ++k) *reinterpret_cast<uint4*>(v + k * kPanelBytes + e * 16) = make_uint4(0, 0, 0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            // O += P V and the next scores, in turn with the other block
+            const uint64_t v_desc = smem_desc(sm.kv(v_at.stage), kPanelBytes, 1024);
+            if (!warp_wait(part == 0 ? &bar.p_full[b] : part == 1 ? &bar.turn[b] : &bar.kv_full[part == 2 ? v_at.stage : k_at.stage],
+                           part == 0 ? p_phase : part == 1 ? turn : part == 2 ? v_at.phase : k_at.phase))
+                return false;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int k = 0; k < kTileKeys / 16; ++k)
+                    if (k < steps) mma_ts(tmem_o, tmem_s + k * 8, v_desc + k * 128, kDescO, j > 0 || k > 0);
+                if (j + 1 < own) {
+                    score(k_at.stage, true);
+                    tc_commit(&bar.kv_empty[v_at.stage]);
+                    tc_commit(&bar.kv_empty[k_at.stage]);
+                    if (j + 2 == own) tc_commit(&bar.q_empty[b]);
+                } else {
+                    bar_arrive(&bar.turn[1 - b]);
+                    tc_commit(&bar.o_full[b]);
+                    tc_commit(&bar.kv_empty[v_at.stage]);
+                }
+            }
+            __syncwarp();
+            p_phase ^= 1;
+            turn ^= 1;
+            if (j + 1 < own) ring.next(kStages);
+        }
+        // tiles that only the other block has a use for are given back as they arrive, and turns as they come
+        for (int j = own; j < n; ++j) {
+            for (int t = 0; t < 2; ++t) {
+                if (!warp_wait(&bar.kv_full[ring.stage], ring.phase)) return false;
+                if (elect_one()) bar_arrive(&bar.kv_empty[ring.stage]);
+                __syncwarp();
+                ring.next(kStages);
+            }
+            if (!warp_wait(&bar.turn[b], turn)) return false;
+            turn ^= 1;
+            if (elect_one()) bar_arrive(&bar.turn[1 - b]);
+            __syncwarp();
+        }
+    }
+    return true;
+}
+
+// STEPS: steps of 16 columns that a head spans.
+template <int STEPS>
 __global__ void __launch_bounds__(kTcThreads, 1)
     attention_bf16_kernel(const __grid_constant__ AttnParams p, const __grid_constant__ CUtensorMap map_q,
                           const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-    extern __shared__ char smem_raw[];
-    constexpr int kStages = ring_stages(PANELS);
-    constexpr uint32_t kTileBytes = PANELS * kPanelBytes;
-    char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    char* smem_q = smem;                       // two blocks
-    char* smem_kv = smem + 2 * kTileBytes;     // the ring
-    Barriers& bar = *reinterpret_cast<Barriers*>(smem_kv + kStages * kTileBytes);
+    extern __shared__ __align__(1024) char smem[];
+    constexpr int kPanels = (STEPS + 3) / 4;
+    const Smem<kPanels> sm{smem};
+    Barriers& bar = sm.bar();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int tokens = kBlockRows / p.group, block_rows = tokens * p.group;  // packed rows of a block
+    const int block_rows = kBlockRows / p.group * p.group;  // packed rows of a block
 
+    if (smem_u32(smem) % 1024 != 0) {  // the swizzled tiles rely on it
+        if (threadIdx.x == 0) atomicExch(p.gave_up, 1u);
+        return;
+    }
     if (threadIdx.x == 0) {
         for (int b = 0; b < 2; ++b) {
             bar_init(&bar.q_full[b], 1);
@@ -241,15 +481,19 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             bar_init(&bar.part_done[b], 4);
             bar_init(&bar.last_set[b], 1);
         }
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < sm.kStages; ++i) {
             bar_init(&bar.kv_full[i], 1);
-            bar_init(&bar.kv_empty[i], 1);
+            bar_init(&bar.kv_empty[i], 2);  // one arrival per block
         }
-        bar_init(&bar.drain, 1);
+        for (int b = 0; b < 2; ++b) {
+            bar_init(&bar.turn[b], 1);
+            bar_init(&bar.drain[b], 1);
+        }
         bar.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        bar_arrive(&bar.turn[0]);  // block 0 begins
     }
-    if (warp == 9) {
+    if (warp == kLoadWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&bar.tmem)), "r"(kTmemCols)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -259,145 +503,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&bar.tmem);
 
-    if (warp >= 8) fewer_registers<72>();
-    if (warp == 8) {
-        // ---- loads ----
-        if (lane == 0) {
-            Ring ring;
-            uint32_t q_phase[2] = {0, 0};
-            bool ok = true;
-            auto load_tile = [&](const CUtensorMap* map, int head, int row) {
-                ok = ok && bar_wait(bar, &bar.kv_empty[ring.stage], ring.phase ^ 1);
-                if (!ok) return;
-                bar_expect(&bar.kv_full[ring.stage], kTileBytes);
-                const uint32_t dst = smem_u32(smem_kv) + ring.stage * kTileBytes;
-                for (int i = 0; i < PANELS; ++i) tma_load(dst + i * kPanelBytes, map, i * 64, head, row, &bar.kv_full[ring.stage]);
-                ring.next(kStages);
-            };
-            for (int i = blockIdx.x; i < p.n_units && ok; i += gridDim.x) {
-                const AttnUnit u = load_unit(p.units, i);
-                Work w;
-                if (!unit_work(p, u, block_rows, w)) continue;
-                const int n = max(w.n[0], w.n[1]);
-                for (int b = 0; b < 2 && ok; ++b) {
-                    if (w.n[b] > 0) {
-                        ok = bar_wait(bar, &bar.q_empty[b], q_phase[b] ^ 1);
-                        if (!ok) break;
-                        bar_expect(&bar.q_full[b], static_cast<uint32_t>(block_rows) * 128 * PANELS);
-                        for (int k = 0; k < PANELS; ++k)
-                            tma_load(smem_u32(smem_q) + b * kTileBytes + k * kPanelBytes, &map_q, k * 64, u.kv_head * p.group,
-                                     u.q_start + u.row0 / p.group + b * tokens, &bar.q_full[b]);
-                        q_phase[b] ^= 1;
-                    }
-                    if (b == 0 && n > 0) load_tile(&map_k, u.kv_head, u.kv_start + w.t0 * kTileKeys);
-                }
-                for (int j = 0; j < n && ok; ++j) {
-                    const int row = u.kv_start + (w.t0 + j) * kTileKeys;
-                    load_tile(&map_v, u.kv_head, row);
-                    if (j + 1 < n) load_tile(&map_k, u.kv_head, row + kTileKeys);
-                }
-            }
-            if (!ok) {
-                // copies in flight must land before the block gives its shared memory back
-                for (int s = 0; s < kStages; ++s)
-                    for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
-                        if (bar_try(&bar.kv_full[s], s < ring.stage ? ring.phase : ring.phase ^ 1)) break;
-                for (int b = 0; b < 2; ++b)
-                    for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
-                        if (bar_try(&bar.q_full[b], q_phase[b] ^ 1)) break;
-            }
+    if (warp >= kLoadWarp) fewer_registers<72>();
+    if (warp == kLoadWarp) {
+        if (lane == 0 && !load_tiles<kPanels>(p, map_q, map_k, map_v, sm)) bar.abort = 1;
+    } else if (warp == kIssueWarp || warp == kIssueWarp + 1) {
+        const int b = warp - kIssueWarp;
+        if (!issue_products<STEPS>(p, sm, tmem, b)) {
+            bar.abort = 1;
+            if (elect_one()) tc_commit(&bar.drain[b]);  // products in flight must end before tensor memory is given back
+            warp_wait(&bar.drain[b], 0);
         }
-    } else if (warp == 9) {
-        // ---- products ----
-        const int k_steps = (p.head_dim + 15) / 16;
-        const uint32_t desc_s = mma_desc(kTileKeys, false), desc_o = mma_desc(16 * k_steps, true);
-        Ring ring;
-        uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
-        bool ok = true;
-        auto score = [&](int b, int stage) {  // S_b = Q_b K^T
-            if (lane == 0) {
-                const uint64_t qd = smem_desc(smem_u32(smem_q) + b * kTileBytes, 16, 1024);
-                const uint64_t kd = smem_desc(smem_u32(smem_kv) + stage * kTileBytes, 16, 1024);
-                for (int k = 0; k < k_steps; ++k) {
-                    const uint64_t step = (k / 4) * (kPanelBytes / 16) + (k % 4) * 2;
-                    mma_ss(tmem + b * 128, qd + step, kd + step, desc_s, k > 0);
-                }
-                tc_commit(&bar.s_full[b]);
-            }
-            __syncwarp();
-        };
-        for (int i = blockIdx.x; i < p.n_units && ok; i += gridDim.x) {
-            const AttnUnit u = load_unit(p.units, i);
-            Work w;
-            if (!unit_work(p, u, block_rows, w)) continue;
-            const int n = max(w.n[0], w.n[1]);
-            if (n == 0) continue;
-            ok = warp_wait(bar, &bar.kv_full[ring.stage], ring.phase);
-            for (int b = 0; b < 2 && ok; ++b) {
-                if (w.n[b] == 0) continue;
-                ok = warp_wait(bar, &bar.q_full[b], q_phase[b]);
-                if (!ok) break;
-                q_phase[b] ^= 1;
-                tc_fence_after();
-                score(b, ring.stage);
-                if (w.n[b] == 1 && lane == 0) tc_commit(&bar.q_empty[b]);
-            }
-            if (!ok) break;
-            if (lane == 0) tc_commit(&bar.kv_empty[ring.stage]);
-            ring.next(kStages);
-            for (int j = 0; j < n && ok; ++j) {
-                const int v_stage = ring.stage;
-                ok = warp_wait(bar, &bar.kv_full[ring.stage], ring.phase);
-                if (!ok) break;
-                ring.next(kStages);
-                // The last tile may hold other rows behind kv_len. The product stops at the next multiple of 16
-                // keys and the rows up to there are cleared: their weight is zero, but zero times NaN is not.
-                const int valid = min(kTileKeys, w.kv_len - (w.t0 + j) * kTileKeys), used = (valid + 15) / 16 * 16;
-                if (valid < used) {
-                    char* v = smem_kv + v_stage * kTileBytes;
-                    for (int e = lane; e < (used - valid) * 8 * PANELS; e += 32)
-                        *reinterpret_cast<uint4*>(v + (e / 8 % PANELS) * kPanelBytes + (valid + e / (8 * PANELS)) * 128 + e % 8 * 16) =
-                            make_uint4(0, 0, 0, 0);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
-                bool have_k = false;
-                for (int b = 0; b < 2 && ok; ++b) {
-                    if (j >= w.n[b]) continue;
-                    ok = warp_wait(bar, &bar.p_full[b], p_phase[b]);
-                    if (!ok) break;
-                    p_phase[b] ^= 1;
-                    tc_fence_after();
-                    if (lane == 0) {  // O_b += P_b V
-                        const uint64_t vd = smem_desc(smem_u32(smem_kv) + v_stage * kTileBytes, kPanelBytes, 1024);
-                        for (int k = 0; k < used / 16; ++k)
-                            mma_ts(tmem + 256 + b * 128, tmem + b * 128 + k * 8, vd + k * 128, desc_o, j > 0 || k > 0);
-                        if (j + 1 == w.n[b]) tc_commit(&bar.o_full[b]);
-                    }
-                    __syncwarp();
-                    if (j + 1 < w.n[b]) {
-                        if (!have_k) ok = warp_wait(bar, &bar.kv_full[ring.stage], ring.phase);
-                        if (!ok) break;
-                        have_k = true;
-                        tc_fence_after();
-                        score(b, ring.stage);
-                        if (j + 2 == w.n[b] && lane == 0) tc_commit(&bar.q_empty[b]);
-                    }
-                }
-                if (!ok) break;
-                if (lane == 0) {
-                    tc_commit(&bar.kv_empty[v_stage]);
-                    if (j + 1 < n) tc_commit(&bar.kv_empty[ring.stage]);
-                }
-                if (j + 1 < n) ring.next(kStages);
-            }
-        }
-        if (!ok) {  // products in flight must end before tensor memory is given back
-            if (lane == 0) tc_commit(&bar.drain);
-            for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
-                if (bar_try(&bar.drain, 0)) break;
-        }
-    } else if (warp < 8) {
+    } else if (warp < kLoadWarp) {
         // ---- softmax and output ----
         more_registers<216>();
         const int b = warp / 4;
@@ -409,17 +525,19 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         for (int i = blockIdx.x; i < p.n_units && ok; i += gridDim.x) {
             const AttnUnit u = load_unit(p.units, i);
             Work w;
-            if (!unit_work(p, u, block_rows, w) || w.rows[b] == 0) continue;
+            if (!unit_work(p, u, block_rows, w)) continue;
+            const int n = b == 0 ? w.n[0] : w.n[1], rows = b == 0 ? w.rows[0] : w.rows[1];
+            if (rows == 0) continue;
             const int pr = u.row0 + b * block_rows + row;  // packed row of the sequence
-            const bool live = row < w.rows[b];
+            const bool live = row < rows;
             const int limit = live ? visible_keys(p, u, w.kv_len, pr / p.group) : 0;
             // keys that every live row of the block sees: tiles in front of this index need no mask
             const int open = visible_keys(p, u, w.kv_len, (u.row0 + b * block_rows) / p.group);
             float ref = -CUDART_INF_F;  // the maximum that P and the sums refer to
-            float l = 0.f;
-            for (int j = 0; j < w.n[b]; ++j) {
+            uint64_t l[2] = {0, 0};   // four running sums in two pairs, joined at the end
+            for (int j = 0; j < n; ++j) {
                 const int key0 = (w.t0 + j) * kTileKeys;
-                ok = warp_wait(bar, &bar.s_full[b], s_phase);
+                ok = warp_wait(&bar.s_full[b], s_phase);
                 if (!ok) break;
                 s_phase ^= 1;
                 tc_fence_after();
@@ -435,10 +553,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 }
                 float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                for (int c = 4; c < 128; c += 4)
+                for (int c = 4; c < 124; c += 8)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], s[c + k]);
-                const float m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                    for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + 2 * k], s[c + 2 * k + 1]);
+                const float m = max3(max3(top[0], s[124], s[125]), max3(top[1], s[126], s[127]), fmaxf(top[2], top[3]));
                 const bool grow = (m - ref) * p.scale_log2 > kRescale;  // also from -inf, unless m is -inf too
                 if (j == 0) {
                     ref = m;
@@ -446,7 +564,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     const float next = fmaxf(ref, m);
                     const float f = next == -CUDART_INF_F ? 1.f : ex2((ref - next) * p.scale_log2);
                     ref = next;
-                    l *= f;
+                    l[0] = mul2(l[0], pair(f, f));
+                    l[1] = mul2(l[1], pair(f, f));
                     for (int c = 0; c < p.head_dim; c += 16) {
                         uint32_t o[16];
                         tmem_load16(tmem_o + c, o);
@@ -457,30 +576,25 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     }
                 }
                 const float shift = ref == -CUDART_INF_F ? 0.f : -ref * p.scale_log2;
-                float sum[2] = {0.f, 0.f};
+                const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
+                // The sum is over the weights before their rounding to bf16, but for the largest of each tile: where one
+                // key dominates, its rounding must divide out.
+                const float e_top = ex2(fmaf(m, p.scale_log2, shift));
+                l[0] = add2(l[0], pair(__uint_as_float(pack_bf16(0.f, e_top)) - e_top, 0.f));
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t packed[32];
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const float e0 = ex2(fmaf(s[h * 64 + 2 * c], p.scale_log2, shift));
-                        const float e1 = ex2(fmaf(s[h * 64 + 2 * c + 1], p.scale_log2, shift));
-                        packed[c] = pack_bf16(e0, e1);
-                        // the sum is over what the product will see: a weight's rounding then divides out where one key dominates
-                        sum[0] += __uint_as_float(packed[c] << 16);
-                        sum[1] += __uint_as_float(packed[c] & 0xffff0000u);
-                    }
+                    weights<kPolyEvery>(s + h * 64, scale2, shift2, packed, l);
                     tmem_store32(tmem_s + h * 32, packed);
                 }
-                l += sum[0] + sum[1];
                 tmem_wait_store();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(&bar.p_full[b]);
             }
             if (!ok) break;
-            if (w.n[b] > 0) {
-                ok = warp_wait(bar, &bar.o_full[b], o_phase);
+            if (n > 0) {
+                ok = warp_wait(&bar.o_full[b], o_phase);
                 if (!ok) break;
                 o_phase ^= 1;
                 tc_fence_after();
@@ -489,12 +603,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const int64_t pitch = part_row_floats(p.head_dim), split_stride = unit_rows * pitch;
             const int64_t part0 = u.part + b * block_rows * pitch * 4;  // of this block in share 0
             const int tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
-            const float inv = l == 0.f ? 0.f : 1.f / l;
+            float sums[4];
+            unpair(l[0], sums[0], sums[1]);
+            unpair(l[1], sums[2], sums[3]);
+            const float total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            const float inv = total == 0.f ? 0.f : 1.f / total;
             float* part = reinterpret_cast<float*>(p.parts + part0) + u.split * split_stride + row * pitch;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.o) + tok * p.o_row + head * p.o_head;
             for (int c = 0; c < p.head_dim; c += 16) {
                 uint32_t o[16] = {};
-                if (w.n[b] > 0) {
+                if (n > 0) {
                     tmem_load16(tmem_o + c, o);
                     tmem_wait_load<16>(o);
                 }
@@ -519,17 +637,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             if (u.n_splits == 1) {
                 if (live && p.lse != nullptr)
                     p.lse[static_cast<int64_t>(head) * p.total_q + tok] =
-                        l == 0.f ? -CUDART_INF_F : (ref * p.scale_log2 + log2f(l)) * kLn2;
+                        total == 0.f ? -CUDART_INF_F : (ref * p.scale_log2 + log2f(total)) * kLn2;
                 continue;
             }
             if (live) {
                 part[pitch - 4] = ref * p.scale_log2;
-                part[pitch - 3] = l;
+                part[pitch - 3] = total;
             }
             __threadfence();
             __syncwarp();
             if (lane == 0) bar_arrive(&bar.part_done[b]);
-            ok = warp_wait(bar, &bar.part_done[b], part_phase);
+            ok = warp_wait(&bar.part_done[b], part_phase);
             if (!ok) break;
             if (row == 0) {
                 const uint32_t before = atomicAdd(p.tickets + u.ticket + b, 1u);
@@ -538,21 +656,22 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 bar_arrive(&bar.last_set[b]);
             }
             __syncwarp();
-            ok = warp_wait(bar, &bar.last_set[b], part_phase);
+            ok = warp_wait(&bar.last_set[b], part_phase);
             if (!ok) break;
             part_phase ^= 1;
             // read by all four warps before they arrive at part_done again, so before it is set again
             if (*reinterpret_cast<volatile uint32_t*>(&bar.last[b])) {
                 __threadfence();
-                join_rows<__nv_bfloat16>(p, u, u.row0 + b * block_rows, w.rows[b], part0, split_stride, warp % 4, 4);
+                join_rows<__nv_bfloat16>(p, u, u.row0 + b * block_rows, rows, part0, split_stride, warp % 4, 4);
             }
         }
+        if (!ok) bar.abort = 1;
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t*>(&bar.abort) != 0) atomicExch(p.gave_up, 1u);
-    if (warp == 9) {
+    if (warp == kLoadWarp) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
     }
@@ -602,11 +721,15 @@ cudaError_t launch_attention_bf16(const AttnParams& p, int64_t total_kv, int sm_
         !encode(&k, kb, p.head_dim, p.n_kv_heads, kv_rows, p.k_row, p.k_head, 1, kTileKeys) ||
         !encode(&v, vb, p.head_dim, p.n_kv_heads, kv_rows, p.v_row, p.v_head, 1, kTileKeys))
         return cudaErrorNotSupported;
-    const int panels = p.head_dim > 64 ? 2 : 1;
-    auto* kernel = panels == 2 ? attention_bf16_kernel<2> : attention_bf16_kernel<1>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(panels));
+    using Kernel = void (*)(AttnParams, CUtensorMap, CUtensorMap, CUtensorMap);
+    static const Kernel kernels[] = {attention_bf16_kernel<1>, attention_bf16_kernel<2>, attention_bf16_kernel<3>, attention_bf16_kernel<4>,
+                                     attention_bf16_kernel<5>, attention_bf16_kernel<6>, attention_bf16_kernel<7>, attention_bf16_kernel<8>};
+    const int steps = (p.head_dim + 15) / 16;
+    const Kernel kernel = kernels[steps - 1];
+    const uint32_t smem = smem_bytes((steps + 3) / 4);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
-    kernel<<<p.n_units < sm_count ? p.n_units : sm_count, kTcThreads, smem_bytes(panels), stream>>>(p, q, k, v);
+    kernel<<<p.n_units < sm_count ? p.n_units : sm_count, kTcThreads, smem, stream>>>(p, q, k, v);
     return cudaGetLastError();
 }
 
