@@ -646,11 +646,15 @@ class SpecaLayer:
         self.kv_rows = int(kv_start[-1]) if kv_start is not None else self.rows
         self.n_axes = len(axis_dims)
         self.torch_dtype = _TORCH_DTYPES[dtype]
+        self.index = self.device.index or 0
+        self.q_shape = (self.rows, n_heads, head_dim)
+        self.k_shape = (self.kv_rows, n_kv_heads, head_dim)     # of keys and values
+        self.new_k_shape = (self.rows, n_kv_heads, head_dim)    # of the keys that belong to the query rows
         kw = dict(kv_start=kv_start, n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim, causal=causal, scale=scale,
                   norm_eps=norm_eps, axis_dims=axis_dims, theta=theta, pairing=pairing)
         nbytes = speca_layer_workspace_bytes(q_start, dtype, **kw)
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self.handle = speca_layer_create(q_start, dtype, self.workspace, device=self.device.index or 0, **kw)
+        self.handle = speca_layer_create(q_start, dtype, self.workspace, device=self.index, **kw)
 
     def close(self):
         if self.handle:
@@ -663,71 +667,78 @@ class SpecaLayer:
         except Exception:
             pass
 
-    def _tensor(self, t, name, shape, dtype=None):
-        """Address of a device tensor of this shape and type whose last dimension is dense; None stays None."""
-        if t is None:
-            return None
-        if not t.is_cuda or t.device != self.device:
-            raise TypeError("%s: a tensor on %s is expected" % (name, self.device))
-        if t.dtype != (dtype or self.torch_dtype):
-            raise TypeError("%s: %s is expected, not %s" % (name, dtype or self.torch_dtype, t.dtype))
-        if t.shape != shape:
-            raise ValueError("%s: shape %s is expected, not %s" % (name, tuple(shape), tuple(t.shape)))
-        if t.stride(-1) != 1 and shape[-1] > 1:
-            raise TypeError("%s: the last dimension must be dense" % name)
+    def _tensor(self, t, name, shape, dtype):
+        """Address of a device tensor of this shape and type whose last dimension is dense."""
+        if t.dtype is not dtype or t.shape != shape or not t.is_cuda or t.get_device() != self.index or (
+                t.stride(-1) != 1 and shape[-1] > 1):
+            self._refuse(t, name, shape, dtype)
         return t.data_ptr()
 
-    def _heads(self, t, name, rows, heads):
+    def _refuse(self, t, name, shape, dtype):
+        if not t.is_cuda or t.get_device() != self.index:
+            raise TypeError("%s: a tensor on %s is expected" % (name, self.device))
+        if t.dtype is not dtype:
+            raise TypeError("%s: %s is expected, not %s" % (name, dtype, t.dtype))
+        if t.shape != shape:
+            raise ValueError("%s: shape %s is expected, not %s" % (name, tuple(shape), tuple(t.shape)))
+        raise TypeError("%s: the last dimension must be dense" % name)
+
+    def _heads(self, t, name, shape):
+        """(address, row stride, head stride) of a [rows, heads, head_dim] tensor."""
         if t is None:
             return None, 0, 0
-        p = self._tensor(t, name, (rows, heads, self.head_dim))
+        p = self._tensor(t, name, shape, self.torch_dtype)
         s = t.stride()
         return p, s[0], s[1]
 
-    def _on(self, stream):
-        return torch.cuda.current_stream(self.device) if stream is None else stream
-
     def _vector(self, t, name, n, dtype):
-        if t is None:
-            return None
-        return self._tensor(t, name, (n,), dtype)
+        return None if t is None else self._tensor(t, name, (n,), dtype)
+
+    def _stream(self, stream):
+        return torch.cuda.current_stream(self.device) if stream is None else stream
 
     def modulate(self, x, y, branch=None, gate=None, scale=None, shift=None, x_out=None, active=None, stream=None):
         """x' = x + gate * branch; y = layer norm of x' * (1 + scale) + shift, the modulations by sequence."""
-        dim = x.shape[-1]
+        dim, dt = x.shape[-1], self.torch_dtype
         shape, mod_shape = (self.rows, dim), (self.n_seqs, dim)
-        mods = [m for m in (gate, scale, shift) if m is not None]
-        if len({m.stride(0) for m in mods}) > 1 and self.n_seqs > 1:
-            raise ValueError("gate, scale and shift must share one row stride")
-        speca_layer_modulate(
-            self.handle, dim, self._tensor(x, "x", shape), x.stride(0), self._tensor(branch, "branch", shape),
-            0 if branch is None else branch.stride(0), self._tensor(gate, "gate", mod_shape), self._tensor(scale, "scale", mod_shape),
-            self._tensor(shift, "shift", mod_shape), mods[0].stride(0) if mods else 0,
-            self._vector(active, "active", self.n_seqs, torch.uint8), self._tensor(x_out, "x_out", shape),
-            0 if x_out is None else x_out.stride(0), self._tensor(y, "y", shape), y.stride(0), self._on(stream))
+        mods, mod_stride = [None, None, None], None
+        for i, m in enumerate((gate, scale, shift)):
+            if m is not None:
+                mods[i] = self._tensor(m, ("gate", "scale", "shift")[i], mod_shape, dt)
+                if mod_stride is None:
+                    mod_stride = m.stride(0)
+                elif m.stride(0) != mod_stride and self.n_seqs > 1:
+                    raise ValueError("gate, scale and shift must share one row stride")
+        b, b_stride = (None, 0) if branch is None else (self._tensor(branch, "branch", shape, dt), branch.stride(0))
+        o, o_stride = (None, 0) if x_out is None else (self._tensor(x_out, "x_out", shape, dt), x_out.stride(0))
+        speca_layer_modulate(self.handle, dim, self._tensor(x, "x", shape, dt), x.stride(0), b, b_stride, mods[0], mods[1], mods[2],
+                             mod_stride or 0, self._vector(active, "active", self.n_seqs, torch.uint8), o, o_stride,
+                             self._tensor(y, "y", shape, dt), y.stride(0), self._stream(stream))
 
     def rope(self, q, q_out, k, k_out, positions, q_weight=None, k_weight=None, active=None, stream=None):
         """Rotary positions (``positions``: fp32 [rows, axes]) of q and k, after an RMS norm where a weight is given."""
         pos = self._tensor(positions, "positions", (self.rows, self.n_axes), torch.float32)
-        if pos is not None and not positions.is_contiguous():
+        if not positions.is_contiguous():
             raise TypeError("positions: must be contiguous")
         speca_layer_rope(
-            self.handle, self._heads(q, "q", self.rows, self.n_heads), self._heads(q_out, "q_out", self.rows, self.n_heads),
-            self._heads(k, "k", self.rows, self.n_kv_heads), self._heads(k_out, "k_out", self.rows, self.n_kv_heads), pos,
-            self._vector(q_weight, "q_weight", self.head_dim, None), self._vector(k_weight, "k_weight", self.head_dim, None),
-            self._vector(active, "active", self.n_seqs, torch.uint8), self._on(stream))
+            self.handle, self._heads(q, "q", self.q_shape), self._heads(q_out, "q_out", self.q_shape),
+            self._heads(k, "k", self.new_k_shape), self._heads(k_out, "k_out", self.new_k_shape), pos,
+            self._vector(q_weight, "q_weight", self.head_dim, self.torch_dtype),
+            self._vector(k_weight, "k_weight", self.head_dim, self.torch_dtype),
+            self._vector(active, "active", self.n_seqs, torch.uint8), self._stream(stream))
 
     def attention(self, q, k, v, out, lse=None, kv_len=None, active=None, stream=None):
         """out = softmax(scale q k^T) v per sequence; ``kv_len``: int32 per sequence, keys that hold data."""
-        p_lse = self._tensor(lse, "lse", (self.n_heads, self.rows), torch.float32)
-        if p_lse is not None and not lse.is_contiguous():
-            raise TypeError("lse: must be contiguous")
+        p_lse = None
+        if lse is not None:
+            p_lse = self._tensor(lse, "lse", (self.n_heads, self.rows), torch.float32)
+            if not lse.is_contiguous():
+                raise TypeError("lse: must be contiguous")
         speca_layer_attention(
-            self.handle, self._heads(q, "q", self.rows, self.n_heads), self._heads(k, "k", self.kv_rows, self.n_kv_heads),
-            self._heads(v, "v", self.kv_rows, self.n_kv_heads), self._heads(out, "out", self.rows, self.n_heads),
-            self._vector(kv_len, "kv_len", self.n_seqs, torch.int32), self._vector(active, "active", self.n_seqs, torch.uint8),
-            p_lse, self._on(stream))
+            self.handle, self._heads(q, "q", self.q_shape), self._heads(k, "k", self.k_shape), self._heads(v, "v", self.k_shape),
+            self._heads(out, "out", self.q_shape), self._vector(kv_len, "kv_len", self.n_seqs, torch.int32),
+            self._vector(active, "active", self.n_seqs, torch.uint8), p_lse, self._stream(stream))
 
     def check(self, stream=None):
         """Waits for `stream` and raises if a kernel of this layer gave up on a bounded wait."""
-        speca_layer_check(self.handle, self._on(stream))
+        speca_layer_check(self.handle, self._stream(stream))

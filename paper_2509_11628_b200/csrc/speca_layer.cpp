@@ -421,12 +421,13 @@ speca_status_t speca_layer_rope(speca_layer_t* c, const void* q, int64_t q_row_s
     p.n_kv_heads = c->n_kv_heads;
     p.head_dim = c->head_dim;
     p.n_axes = c->n_axes;
+    p.rotated = c->rotated;
     p.half = c->pairing == SPECA_ROPE_HALVES ? c->rotated / 2 : 0;
     p.eps = c->norm_eps;
     // four pairs as one or two accesses: heads of a multiple of 8 elements and, for HALVES, a multiple of 4 pairs
     const bool vectors = c->head_dim % 8 == 0 && p.half % 4 == 0 && on_16(c, q, q_row_stride, q_head_stride) &&
                          on_16(c, q_out, q_out_row_stride, q_out_head_stride) && on_16(c, k, k_row_stride, k_head_stride) &&
-                         on_16(c, k_out, k_out_row_stride, k_out_head_stride);
+                         on_16(c, k_out, k_out_row_stride, k_out_head_stride) && on_16(c, q_weight, 0, 0) && on_16(c, k_weight, 0, 0);
     DeviceGuard guard(c->device);
     if (!guard.ok) return fail(c, SPECA_ERR_CUDA, "cudaSetDevice failed");
     speca_status_t st = check_sticky(c);

@@ -36,6 +36,7 @@ struct RopeParams {
     const float* positions;
     int64_t q_row, q_head, qo_row, qo_head, k_row, k_head, ko_row, ko_head;  // strides, elements
     int32_t rows, n_heads, n_kv_heads, head_dim, n_axes;
+    int32_t rotated;  // elements of a head that turn
     int32_t half;  // HALVES: distance of a pair's elements (R / 2); 0 = INTERLEAVED
     float eps;
 };

@@ -60,9 +60,9 @@ __device__ __forceinline__ float sum_lanes(float x) {
 // x' = x + gate * branch, y = (x' - mean) * rstd * (1 + scale) + shift. One pass over memory: the G
 // threads of a row keep it in registers (NV accesses of E elements each), so the variance is the
 // mean of squared deviations from the finished mean and nothing is read twice.
-constexpr int kModThreads = 128;
 
-// Sum over the row's threads: inside the warp, then through shared memory if the row has several warps.
+// Sum over the row's threads: inside the warp, then through shared memory if the row has several warps (`red`: one
+// float per warp, of this sum alone, so that one barrier is enough).
 template <int G>
 __device__ __forceinline__ float sum_row(float x, float* red) {
     if constexpr (G <= 32) return sum_lanes<G>(x);
@@ -73,14 +73,13 @@ __device__ __forceinline__ float sum_row(float x, float* red) {
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < G / 32; ++i) s += red[first + i];
-    __syncthreads();
     return s;
 }
 
 template <int DT, int E, int NV, int G, int NT>
 __global__ void __launch_bounds__(NT) modulate_kernel(const __grid_constant__ ModulateParams p) {
     using T = typename Type<DT>::T;
-    __shared__ float red[NT / 32];
+    __shared__ float red[2][NT / 32];
     const int row = blockIdx.x * (NT / G) + threadIdx.x / G;
     const int t = threadIdx.x % G;
     bool live = row < p.rows;
@@ -146,7 +145,7 @@ __global__ void __launch_bounds__(NT) modulate_kernel(const __grid_constant__ Mo
         }
     }
     // every thread takes part in the sums: a row's threads may share a warp or a barrier with a dead row's
-    const float mean = sum_row<G>(sum, red) / p.dim;
+    const float mean = sum_row<G>(sum, red[0]) / p.dim;
     float sq = 0.f;
     if (live) {
 #pragma unroll
@@ -159,7 +158,7 @@ __global__ void __launch_bounds__(NT) modulate_kernel(const __grid_constant__ Mo
             }
         }
     }
-    const float rstd = 1.f / sqrtf(sum_row<G>(sq, red) / p.dim + p.eps);
+    const float rstd = 1.f / sqrtf(sum_row<G>(sq, red[1]) / p.dim + p.eps);
     if (!live) return;
     const char* ps = p.scale == nullptr ? nullptr : p.scale + seq * p.mod_stride * static_cast<int64_t>(sizeof(T));
     const char* pt = p.shift == nullptr ? nullptr : p.shift + seq * p.mod_stride * static_cast<int64_t>(sizeof(T));
@@ -184,7 +183,7 @@ __global__ void __launch_bounds__(NT) modulate_kernel(const __grid_constant__ Mo
 template <int DT>
 __global__ void __launch_bounds__(1024) modulate_long_kernel(const __grid_constant__ ModulateParams p) {
     using T = typename Type<DT>::T;
-    __shared__ float red[32];
+    __shared__ float red[2][32];
     const int row = blockIdx.x;
     const int seq = p.row_seq[row];
     if (p.dev_mask != nullptr && p.dev_mask[seq] == 0) return;
@@ -199,13 +198,13 @@ __global__ void __launch_bounds__(1024) modulate_long_kernel(const __grid_consta
     };
     float sum = 0.f;
     for (int c = threadIdx.x; c < p.dim; c += 1024) sum += value(c);
-    const float mean = sum_row<1024>(sum, red) / p.dim;
+    const float mean = sum_row<1024>(sum, red[0]) / p.dim;
     float sq = 0.f;
     for (int c = threadIdx.x; c < p.dim; c += 1024) {
         const float d = value(c) - mean;
         sq = fmaf(d, d, sq);
     }
-    const float rstd = 1.f / sqrtf(sum_row<1024>(sq, red) / p.dim + p.eps);
+    const float rstd = 1.f / sqrtf(sum_row<1024>(sq, red[1]) / p.dim + p.eps);
     for (int c = threadIdx.x; c < p.dim; c += 1024) {
         const float v = value(c);
         if (p.x_out != nullptr) (reinterpret_cast<T*>(p.x_out) + row * p.x_out_stride)[c] = from_float<T>(v);
@@ -220,15 +219,19 @@ void run_modulate(const ModulateParams& p, cudaStream_t stream) {
     modulate_kernel<DT, E, NV, G, NT><<<(p.rows + per - 1) / per, NT, 0, stream>>>(p);
 }
 
-// Elements a row's threads can hold: NV accesses of E elements by G threads.
+// A row's threads hold NV accesses of E elements each. Few threads with two or three accesses beat one access per thread
+// (loads in flight) and many accesses per thread (registers): on rows of 3072 bf16 elements 128 threads x 3 ran at
+// 5.8 TB/s over 20926 rows, 128 x 4 at 5.0, 384 x 1 at 4.0, 32 x 12 at 3.6.
 template <int DT, int E>
 void dispatch_modulate(const ModulateParams& p, cudaStream_t stream) {
     const int n = (p.dim + E - 1) / E;  // accesses per row
-    if (n <= 32 * 2) return run_modulate<DT, E, 2, 32, kModThreads>(p, stream);
-    if (n <= 32 * 6) return run_modulate<DT, E, 6, 32, kModThreads>(p, stream);
-    if (n <= 128 * 4) return run_modulate<DT, E, 4, 128, 128>(p, stream);
+    if (n <= 32 * 2) return run_modulate<DT, E, 2, 32, 128>(p, stream);
+    if (n <= 64 * 2) return run_modulate<DT, E, 2, 64, 128>(p, stream);
+    if (n <= 128 * 2) return run_modulate<DT, E, 2, 128, 128>(p, stream);
+    if (n <= 128 * 3) return run_modulate<DT, E, 3, 128, 128>(p, stream);
+    if (n <= 128 * 5) return run_modulate<DT, E, 5, 128, 128>(p, stream);
+    if (n <= 256 * 4) return run_modulate<DT, E, 4, 256, 256>(p, stream);
     if (n <= 512 * 4) return run_modulate<DT, E, 4, 512, 512>(p, stream);
-    if (n <= 512 * 8) return run_modulate<DT, E, 8, 512, 512>(p, stream);
     modulate_long_kernel<DT><<<p.rows, 1024, 0, stream>>>(p);
 }
 
@@ -236,174 +239,201 @@ void dispatch_modulate(const ModulateParams& p, cudaStream_t stream) {
 // rotary positions
 // ------------------------------------------------------------------------------------------------
 // L lanes share one head of one row; each holds 4 pairs (with vectors: consecutive pairs, one or two
-// accesses; else pairs lane, lane + L, ...). The angle of a pair is the same for every head of a row, so
-// a lane keeps its row, computes 4 angles once and turns its share of all heads of q and k with them.
+// accesses; else pairs lane, lane + L, ...). Several lane groups share a row: each takes its part of the heads of q
+// and k. The block first forms the rotations of its rows in shared memory: an angle serves every head of a row.
 constexpr int kRopeThreads = 256;
 constexpr int kRopePairs = 4;   // pairs per lane
-constexpr int kRopeAhead = 4;   // heads whose loads are in flight per lane
+constexpr int kRopeAhead = 3;   // heads whose loads are in flight per lane
+constexpr int kRopeBlocks = 4;  // per SM
+constexpr float kKept = 2.f;    // no cosine: the pair is copied, so that an infinity in it stays where it is
 
+// The 8 elements that a lane holds of a head, as pairs (a, b).
 template <int DT, bool VEC, bool HALVES, int L>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constant__ RopeParams p, int groups_per_row) {
+struct HeadPart {
     using T = typename Type<DT>::T;
-    constexpr int kGroups = kRopeThreads / L;
-    const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    const int rows_per_block = kGroups / groups_per_row;
-    const int row = blockIdx.x * rows_per_block + group / groups_per_row;
-    const int head0 = group % groups_per_row;
-    const int n_pairs = p.head_dim / 2, n_all = p.n_heads + (p.k == nullptr ? 0 : p.n_kv_heads);
-    const bool live = row < p.rows && (p.dev_mask == nullptr || p.dev_mask[p.row_seq[row]] != 0);
+    int first, n_pairs, half;  // first pair, pairs of the head, distance of a pair's elements (HALVES)
+    bool split;                // VEC, HALVES: the lane's pairs lie in the rotated part
+    __device__ __forceinline__ HeadPart(int lane, int n, int h)
+        : first(VEC ? lane * kRopePairs : lane), n_pairs(n), half(h), split(HALVES && lane * kRopePairs < h) {}
+    __device__ __forceinline__ int pair(int i) const { return VEC ? first + i : first + i * L; }
+    __device__ __forceinline__ bool holds(int i) const { return VEC ? first < n_pairs : pair(i) < n_pairs; }
+    // HALVES, behind the rotated part: the remaining elements two by two
+    __device__ __forceinline__ int e0(int i) const { return HALVES && pair(i) < half ? pair(i) : 2 * pair(i); }
+    __device__ __forceinline__ int e1(int i) const { return HALVES && pair(i) < half ? pair(i) + half : 2 * pair(i) + 1; }
+    // VEC, HALVES: a = 4 elements, b = their partners, or the 4 elements behind them where nothing turns
+    __device__ __forceinline__ int second() const { return split ? first + half : 2 * first + kRopePairs; }
+    __device__ __forceinline__ int start() const { return split ? first : 2 * first; }
 
-    // pair i of this lane and the elements it consists of
-    int pair[kRopePairs], e0[kRopePairs], e1[kRopePairs];
+    __device__ __forceinline__ void read(const char* src, int64_t at, T (&a)[kRopePairs], T (&b)[kRopePairs]) const {
+        if constexpr (VEC && !HALVES) {
+            if (first >= n_pairs) return;
+            const Pack<T, 2 * kRopePairs> v = load<T, 2 * kRopePairs>(src, at + 2 * first);
 #pragma unroll
-    for (int i = 0; i < kRopePairs; ++i) {
-        pair[i] = VEC ? lane * kRopePairs + i : lane + i * L;
-        // HALVES: pairs behind the rotated part hold its remaining elements two by two
-        const bool split = HALVES && pair[i] < p.half;
-        e0[i] = split ? pair[i] : 2 * pair[i];
-        e1[i] = split ? pair[i] + p.half : 2 * pair[i] + 1;
+            for (int i = 0; i < kRopePairs; ++i) a[i] = v.e[2 * i], b[i] = v.e[2 * i + 1];
+        } else if constexpr (VEC) {
+            if (first >= n_pairs) return;
+            const Pack<T, kRopePairs> u = load<T, kRopePairs>(src, at + start()), v = load<T, kRopePairs>(src, at + second());
+#pragma unroll
+            for (int i = 0; i < kRopePairs; ++i) a[i] = u.e[i], b[i] = v.e[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRopePairs; ++i) {
+                if (!holds(i)) continue;
+                a[i] = reinterpret_cast<const T*>(src)[at + e0(i)];
+                b[i] = reinterpret_cast<const T*>(src)[at + e1(i)];
+            }
+        }
     }
-    float c[kRopePairs], s[kRopePairs];
-    bool kept[kRopePairs];  // copied, so that an infinity in it stays where it is
+    __device__ __forceinline__ void write(char* dst, int64_t at, const float (&a)[kRopePairs], const float (&b)[kRopePairs]) const {
+        if constexpr (VEC && !HALVES) {
+            if (first >= n_pairs) return;
+            Pack<T, 2 * kRopePairs> v;
 #pragma unroll
-    for (int i = 0; i < kRopePairs; ++i) kept[i] = true;
-    if (live) {
+            for (int i = 0; i < kRopePairs; ++i) v.e[2 * i] = from_float<T>(a[i]), v.e[2 * i + 1] = from_float<T>(b[i]);
+            store<T, 2 * kRopePairs>(dst, at + 2 * first, v);
+        } else if constexpr (VEC) {
+            if (first >= n_pairs) return;
+            Pack<T, kRopePairs> u, v;
+#pragma unroll
+            for (int i = 0; i < kRopePairs; ++i) u.e[i] = from_float<T>(a[i]), v.e[i] = from_float<T>(b[i]);
+            store<T, kRopePairs>(dst, at + start(), u);
+            store<T, kRopePairs>(dst, at + second(), v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kRopePairs; ++i) {
+                if (!holds(i)) continue;
+                reinterpret_cast<T*>(dst)[at + e0(i)] = from_float<T>(a[i]);
+                reinterpret_cast<T*>(dst)[at + e1(i)] = from_float<T>(b[i]);
+            }
+        }
+    }
+};
+
+// All heads of q or of k of one row, by the row's lane groups. A head x turns into r R(w x), r the reciprocal root mean
+// square, w the weight: the rotation is linear, so w goes into its coefficients once and r is applied behind it.
+template <int DT, bool VEC, bool HALVES, bool KEPT, bool NORM, int L>
+__device__ __forceinline__ void turn_heads(const HeadPart<DT, VEC, HALVES, L>& part, const char* src, int64_t head_in, char* dst,
+                                           int64_t head_out, int n_heads, int head0, int step, const char* w,
+                                           const float2 (&cs)[kRopePairs], bool live, float inv_dim, float eps) {
+    using T = typename Type<DT>::T;
+    float ca[kRopePairs], sb[kRopePairs], sa[kRopePairs], cb[kRopePairs];  // (a, b) -> (ca a - sb b, sa a + cb b)
+    {
+        T wa[kRopePairs], wb[kRopePairs];
+        if (NORM && w != nullptr) part.read(w, 0, wa, wb);
 #pragma unroll
         for (int i = 0; i < kRopePairs; ++i) {
-            c[i] = 1.f;
-            s[i] = 0.f;
-            if (pair[i] >= n_pairs) continue;
-            const RopePair f = p.pairs[pair[i]];
-            if (f.axis < 0) continue;
-            kept[i] = false;
-            const double turns = f.turns * static_cast<double>(p.positions[static_cast<int64_t>(row) * p.n_axes + f.axis]);
-            sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &s[i], &c[i]);
+            const bool weighted = NORM && w != nullptr && part.holds(i);
+            const float fa = weighted ? to_float(wa[i]) : 1.f, fb = weighted ? to_float(wb[i]) : 1.f;
+            const bool kept = KEPT && cs[i].x == kKept;
+            ca[i] = (kept ? 1.f : cs[i].x) * fa;
+            cb[i] = (kept ? 1.f : cs[i].x) * fb;
+            sa[i] = cs[i].y * fa;
+            sb[i] = cs[i].y * fb;
         }
     }
     // the groups of a warp run the same number of rounds: sums over the head are shuffles of the whole warp
-    const int rounds = (n_all + groups_per_row * kRopeAhead - 1) / (groups_per_row * kRopeAhead);
-    for (int round = 0; round < rounds; ++round) {
-        float a[kRopeAhead][kRopePairs], b[kRopeAhead][kRopePairs];
+    for (int first = 0; first < n_heads; first += step * kRopeAhead) {
+        T in[kRopeAhead][2][kRopePairs];
 #pragma unroll
         for (int j = 0; j < kRopeAhead; ++j) {
-            const int h = head0 + (round * kRopeAhead + j) * groups_per_row;
-#pragma unroll
-            for (int i = 0; i < kRopePairs; ++i) a[j][i] = b[j][i] = 0.f;
-            if (!live || h >= n_all) continue;
-            const char* src = h < p.n_heads ? p.q : p.k;
-            const int64_t at = h < p.n_heads ? row * p.q_row + h * p.q_head : row * p.k_row + (h - p.n_heads) * p.k_head;
-            if constexpr (VEC && !HALVES) {
-                if (pair[0] < n_pairs) {
-                    const Pack<T, 2 * kRopePairs> v = load<T, 2 * kRopePairs>(src, at + 2 * pair[0]);
-#pragma unroll
-                    for (int i = 0; i < kRopePairs; ++i) {
-                        a[j][i] = to_float(v.e[2 * i]);
-                        b[j][i] = to_float(v.e[2 * i + 1]);
-                    }
-                }
-            } else if constexpr (VEC) {
-                if (pair[0] < n_pairs) {
-                    // rotated: 4 elements and their 4 partners; kept: 8 consecutive ones
-                    const bool split = pair[0] < p.half;
-                    const Pack<T, kRopePairs> u = load<T, kRopePairs>(src, at + e0[0]);
-                    const Pack<T, kRopePairs> v = load<T, kRopePairs>(src, at + (split ? e1[0] : e0[0] + kRopePairs));
-#pragma unroll
-                    for (int i = 0; i < kRopePairs; ++i) {
-                        a[j][i] = to_float(u.e[i]);
-                        b[j][i] = to_float(v.e[i]);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kRopePairs; ++i) {
-                    if (pair[i] >= n_pairs) continue;
-                    a[j][i] = to_float(reinterpret_cast<const T*>(src)[at + e0[i]]);
-                    b[j][i] = to_float(reinterpret_cast<const T*>(src)[at + e1[i]]);
-                }
-            }
+            const int h = first + j * step + head0;
+            if (live && h < n_heads) part.read(src, h * head_in, in[j][0], in[j][1]);
         }
 #pragma unroll
         for (int j = 0; j < kRopeAhead; ++j) {
-            const int h = head0 + (round * kRopeAhead + j) * groups_per_row;
-            const bool is_q = h < p.n_heads;
-            const char* w = is_q ? p.q_weight : p.k_weight;
-            if (p.q_weight != nullptr || p.k_weight != nullptr) {
+            if (first + j * step >= n_heads) break;  // the same for every group
+            const int h = first + j * step + head0;
+            const bool use = live && h < n_heads;
+            float a[kRopePairs], b[kRopePairs], r = 1.f;
+#pragma unroll
+            for (int i = 0; i < kRopePairs; ++i) {
+                const bool has = use && part.holds(i);
+                a[i] = has ? to_float(in[j][0][i]) : 0.f;
+                b[i] = has ? to_float(in[j][1][i]) : 0.f;
+            }
+            if (NORM && w != nullptr) {
                 float sq = 0.f;
 #pragma unroll
-                for (int i = 0; i < kRopePairs; ++i) sq = fmaf(a[j][i], a[j][i], fmaf(b[j][i], b[j][i], sq));
-                sq = sum_lanes<L>(sq);
-                if (w != nullptr) {
-                    const float r = 1.f / sqrtf(sq / p.head_dim + p.eps);
-                    // in registers a kept pair of HALVES holds elements 4 apart (see the load)
-#pragma unroll
-                    for (int i = 0; i < kRopePairs; ++i) {
-                        if (pair[i] >= n_pairs) continue;
-                        const bool apart = VEC && HALVES && pair[i] >= p.half;
-                        a[j][i] *= r * to_float(reinterpret_cast<const T*>(w)[apart ? e0[0] + i : e0[i]]);
-                        b[j][i] *= r * to_float(reinterpret_cast<const T*>(w)[apart ? e0[0] + kRopePairs + i : e1[i]]);
-                    }
-                }
+                for (int i = 0; i < kRopePairs; ++i) sq = fmaf(a[i], a[i], fmaf(b[i], b[i], sq));
+                r = rsqrtf(fmaf(sum_lanes<L>(sq), inv_dim, eps));
             }
-            if (!live || h >= n_all) continue;
-            char* dst = is_q ? p.q_out : p.k_out;
-            const int64_t at = is_q ? row * p.qo_row + h * p.qo_head : row * p.ko_row + (h - p.n_heads) * p.ko_head;
+            if (!use) continue;
             float ra[kRopePairs], rb[kRopePairs];
 #pragma unroll
             for (int i = 0; i < kRopePairs; ++i) {
-                ra[i] = kept[i] ? a[j][i] : fmaf(a[j][i], c[i], -b[j][i] * s[i]);
-                rb[i] = kept[i] ? b[j][i] : fmaf(a[j][i], s[i], b[j][i] * c[i]);
+                const bool kept = KEPT && cs[i].x == kKept;
+                ra[i] = kept ? ca[i] * a[i] : fmaf(ca[i], a[i], -sb[i] * b[i]);
+                rb[i] = kept ? cb[i] * b[i] : fmaf(sa[i], a[i], cb[i] * b[i]);
+                if (NORM) ra[i] *= r, rb[i] *= r;
             }
-            if constexpr (VEC && !HALVES) {
-                if (pair[0] < n_pairs) {
-                    Pack<T, 2 * kRopePairs> v;
-#pragma unroll
-                    for (int i = 0; i < kRopePairs; ++i) {
-                        v.e[2 * i] = from_float<T>(ra[i]);
-                        v.e[2 * i + 1] = from_float<T>(rb[i]);
-                    }
-                    store<T, 2 * kRopePairs>(dst, at + 2 * pair[0], v);
-                }
-            } else if constexpr (VEC) {
-                if (pair[0] < n_pairs) {
-                    const bool split = pair[0] < p.half;
-                    Pack<T, kRopePairs> u, v;
-#pragma unroll
-                    for (int i = 0; i < kRopePairs; ++i) {
-                        u.e[i] = from_float<T>(ra[i]);
-                        v.e[i] = from_float<T>(rb[i]);
-                    }
-                    store<T, kRopePairs>(dst, at + e0[0], u);
-                    store<T, kRopePairs>(dst, at + (split ? e1[0] : e0[0] + kRopePairs), v);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kRopePairs; ++i) {
-                    if (pair[i] >= n_pairs) continue;
-                    reinterpret_cast<T*>(dst)[at + e0[i]] = from_float<T>(ra[i]);
-                    reinterpret_cast<T*>(dst)[at + e1[i]] = from_float<T>(rb[i]);
-                }
-            }
+            part.write(dst, h * head_out, ra, rb);
         }
     }
 }
 
-template <int DT, bool VEC, bool HALVES, int L>
-void run_rope(const RopeParams& p, cudaStream_t stream) {
-    const int groups = kRopeThreads / L;
-    const int heads = p.n_heads + (p.k == nullptr ? 0 : p.n_kv_heads);
-    // lane groups per row: enough that each keeps about kRopeAhead heads in flight
-    int gpr = 1;
-    while (gpr < groups && gpr * kRopeAhead < heads) gpr *= 2;
-    const int per = groups / gpr;
-    rope_kernel<DT, VEC, HALVES, L><<<(p.rows + per - 1) / per, kRopeThreads, 0, stream>>>(p, gpr);
+template <int DT, bool VEC, bool HALVES, bool KEPT, bool NORM, int L>
+__global__ void __launch_bounds__(kRopeThreads, kRopeBlocks) rope_kernel(const __grid_constant__ RopeParams p, int groups_per_row) {
+    constexpr int kGroups = kRopeThreads / L;
+    constexpr int64_t kBytes = Type<DT>::kBytes;
+    __shared__ float2 turn[kGroups * kRopePairs * L];  // [row of the block][pair]: cosine, sine
+    const int group = threadIdx.x / L;
+    const int rows_per_block = kGroups / groups_per_row, row0 = blockIdx.x * rows_per_block;
+    const int own = group / groups_per_row, row = row0 + own, head0 = group % groups_per_row;
+    const int n_pairs = p.head_dim / 2;
+    const bool live = row < p.rows && (p.dev_mask == nullptr || p.dev_mask[p.row_seq[row]] != 0);
+    const HeadPart<DT, VEC, HALVES, L> part(threadIdx.x % L, n_pairs, p.half);
+    for (int i = threadIdx.x; i < rows_per_block * n_pairs; i += kRopeThreads) {
+        const int r = i / n_pairs, pair = i % n_pairs;
+        const RopePair f = p.pairs[pair];
+        float2 t = make_float2(kKept, 0.f);
+        if (f.axis >= 0 && row0 + r < p.rows) {
+            // the angle in turns, reduced in fp64 to half a turn either way
+            const double turns = f.turns * static_cast<double>(p.positions[static_cast<int64_t>(row0 + r) * p.n_axes + f.axis]);
+            sincospif(static_cast<float>(2.0 * (turns - rint(turns))), &t.y, &t.x);
+        }
+        turn[i] = t;
+    }
+    __syncthreads();
+    float2 cs[kRopePairs];
+#pragma unroll
+    for (int i = 0; i < kRopePairs; ++i) cs[i] = part.holds(i) ? turn[own * n_pairs + part.pair(i)] : make_float2(kKept, 0.f);
+    const float inv_dim = 1.f / p.head_dim;
+    turn_heads<DT, VEC, HALVES, KEPT, NORM, L>(part, p.q + row * p.q_row * kBytes, p.q_head, p.q_out + row * p.qo_row * kBytes, p.qo_head,
+                                               p.n_heads, head0, groups_per_row, p.q_weight, cs, live, inv_dim, p.eps);
+    if (p.k != nullptr)
+        turn_heads<DT, VEC, HALVES, KEPT, NORM, L>(part, p.k + row * p.k_row * kBytes, p.k_head, p.k_out + row * p.ko_row * kBytes,
+                                                   p.ko_head, p.n_kv_heads, head0, groups_per_row, p.k_weight, cs, live, inv_dim, p.eps);
 }
 
-template <int DT, bool VEC, bool HALVES>
+template <int DT, bool VEC, bool HALVES, bool KEPT, int L>
+void run_rope(const RopeParams& p, cudaStream_t stream) {
+    const int groups = kRopeThreads / L;
+    // Lane groups per row: as many rows per block as give every thread an angle to form, or (few rows: SMs idle)
+    // enough groups that each keeps no more than kRopeAhead heads in flight.
+    int gpr = groups;
+    while (gpr > 1 && groups / gpr * (p.head_dim / 2) < kRopeThreads) gpr /= 2;
+    while (gpr < groups && gpr * kRopeAhead < p.n_heads && static_cast<int64_t>(p.rows) * gpr < groups * 592ll) gpr *= 2;
+    const int per = groups / gpr, grid = (p.rows + per - 1) / per;
+    if (p.q_weight != nullptr || p.k_weight != nullptr)
+        rope_kernel<DT, VEC, HALVES, KEPT, true, L><<<grid, kRopeThreads, 0, stream>>>(p, gpr);
+    else
+        rope_kernel<DT, VEC, HALVES, KEPT, false, L><<<grid, kRopeThreads, 0, stream>>>(p, gpr);
+}
+
+template <int DT, bool VEC, bool HALVES, bool KEPT>
 void dispatch_rope(const RopeParams& p, cudaStream_t stream) {
     const int lanes = (p.head_dim / 2 + kRopePairs - 1) / kRopePairs;
-    if (lanes <= 4) return run_rope<DT, VEC, HALVES, 4>(p, stream);
-    if (lanes <= 8) return run_rope<DT, VEC, HALVES, 8>(p, stream);
-    return run_rope<DT, VEC, HALVES, 16>(p, stream);
+    if (lanes <= 4) return run_rope<DT, VEC, HALVES, KEPT, 4>(p, stream);
+    if (lanes <= 8) return run_rope<DT, VEC, HALVES, KEPT, 8>(p, stream);
+    return run_rope<DT, VEC, HALVES, KEPT, 16>(p, stream);
+}
+template <int DT, bool VEC>
+void dispatch_rope(const RopeParams& p, cudaStream_t stream) {
+    const bool kept = p.rotated < p.head_dim;
+    if (p.half > 0)
+        kept ? dispatch_rope<DT, VEC, true, true>(p, stream) : dispatch_rope<DT, VEC, true, false>(p, stream);
+    else
+        kept ? dispatch_rope<DT, VEC, false, true>(p, stream) : dispatch_rope<DT, VEC, false, false>(p, stream);
 }
 
 }  // namespace
@@ -420,18 +450,10 @@ cudaError_t launch_modulate(const ModulateParams& p, int dtype, int vec, cudaStr
 
 cudaError_t launch_rope(const RopeParams& p, int dtype, bool vectors, cudaStream_t stream) {
     if (p.rows == 0) return cudaSuccess;
-    const bool halves = p.half > 0;
-    if (dtype == SPECA_BF16) {
-        if (vectors)
-            halves ? dispatch_rope<SPECA_BF16, true, true>(p, stream) : dispatch_rope<SPECA_BF16, true, false>(p, stream);
-        else
-            halves ? dispatch_rope<SPECA_BF16, false, true>(p, stream) : dispatch_rope<SPECA_BF16, false, false>(p, stream);
-    } else {
-        if (vectors)
-            halves ? dispatch_rope<SPECA_F32, true, true>(p, stream) : dispatch_rope<SPECA_F32, true, false>(p, stream);
-        else
-            halves ? dispatch_rope<SPECA_F32, false, true>(p, stream) : dispatch_rope<SPECA_F32, false, false>(p, stream);
-    }
+    if (dtype == SPECA_BF16)
+        vectors ? dispatch_rope<SPECA_BF16, true>(p, stream) : dispatch_rope<SPECA_BF16, false>(p, stream);
+    else
+        vectors ? dispatch_rope<SPECA_F32, true>(p, stream) : dispatch_rope<SPECA_F32, false>(p, stream);
     return cudaGetLastError();
 }
 
