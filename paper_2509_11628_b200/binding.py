@@ -668,11 +668,11 @@ class SpecaLayer:
             pass
 
     def _tensor(self, t, name, shape, dtype):
-        """Address of a device tensor of this shape and type whose last dimension is dense."""
-        if t.dtype is not dtype or t.shape != shape or not t.is_cuda or t.get_device() != self.index or (
-                t.stride(-1) != 1 and shape[-1] > 1):
+        """(address, strides) of a device tensor of this shape and type whose last dimension is dense."""
+        s = t.stride()
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self.index or (s[-1] != 1 and shape[-1] > 1):
             self._refuse(t, name, shape, dtype)
-        return t.data_ptr()
+        return t.data_ptr(), s
 
     def _refuse(self, t, name, shape, dtype):
         if not t.is_cuda or t.get_device() != self.index:
@@ -687,37 +687,38 @@ class SpecaLayer:
         """(address, row stride, head stride) of a [rows, heads, head_dim] tensor."""
         if t is None:
             return None, 0, 0
-        p = self._tensor(t, name, shape, self.torch_dtype)
-        s = t.stride()
+        p, s = self._tensor(t, name, shape, self.torch_dtype)
         return p, s[0], s[1]
 
     def _vector(self, t, name, n, dtype):
-        return None if t is None else self._tensor(t, name, (n,), dtype)
+        return None if t is None else self._tensor(t, name, (n,), dtype)[0]
 
     def _stream(self, stream):
-        return torch.cuda.current_stream(self.device) if stream is None else stream
+        """The stream's address; of the device's current stream without the Stream object around it (2 us a call)."""
+        return torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream
 
     def modulate(self, x, y, branch=None, gate=None, scale=None, shift=None, x_out=None, active=None, stream=None):
         """x' = x + gate * branch; y = layer norm of x' * (1 + scale) + shift, the modulations by sequence."""
         dim, dt = x.shape[-1], self.torch_dtype
         shape, mod_shape = (self.rows, dim), (self.n_seqs, dim)
+        px, sx = self._tensor(x, "x", shape, dt)
+        py, sy = self._tensor(y, "y", shape, dt)
+        pb, sb = (None, (0,)) if branch is None else self._tensor(branch, "branch", shape, dt)
+        po, so = (None, (0,)) if x_out is None else self._tensor(x_out, "x_out", shape, dt)
         mods, mod_stride = [None, None, None], None
         for i, m in enumerate((gate, scale, shift)):
             if m is not None:
-                mods[i] = self._tensor(m, ("gate", "scale", "shift")[i], mod_shape, dt)
+                mods[i], s = self._tensor(m, ("gate", "scale", "shift")[i], mod_shape, dt)
                 if mod_stride is None:
-                    mod_stride = m.stride(0)
-                elif m.stride(0) != mod_stride and self.n_seqs > 1:
+                    mod_stride = s[0]
+                elif s[0] != mod_stride and self.n_seqs > 1:
                     raise ValueError("gate, scale and shift must share one row stride")
-        b, b_stride = (None, 0) if branch is None else (self._tensor(branch, "branch", shape, dt), branch.stride(0))
-        o, o_stride = (None, 0) if x_out is None else (self._tensor(x_out, "x_out", shape, dt), x_out.stride(0))
-        speca_layer_modulate(self.handle, dim, self._tensor(x, "x", shape, dt), x.stride(0), b, b_stride, mods[0], mods[1], mods[2],
-                             mod_stride or 0, self._vector(active, "active", self.n_seqs, torch.uint8), o, o_stride,
-                             self._tensor(y, "y", shape, dt), y.stride(0), self._stream(stream))
+        speca_layer_modulate(self.handle, dim, px, sx[0], pb, sb[0], mods[0], mods[1], mods[2], mod_stride or 0,
+                             self._vector(active, "active", self.n_seqs, torch.uint8), po, so[0], py, sy[0], self._stream(stream))
 
     def rope(self, q, q_out, k, k_out, positions, q_weight=None, k_weight=None, active=None, stream=None):
         """Rotary positions (``positions``: fp32 [rows, axes]) of q and k, after an RMS norm where a weight is given."""
-        pos = self._tensor(positions, "positions", (self.rows, self.n_axes), torch.float32)
+        pos, _ = self._tensor(positions, "positions", (self.rows, self.n_axes), torch.float32)
         if not positions.is_contiguous():
             raise TypeError("positions: must be contiguous")
         speca_layer_rope(
@@ -731,7 +732,7 @@ class SpecaLayer:
         """out = softmax(scale q k^T) v per sequence; ``kv_len``: int32 per sequence, keys that hold data."""
         p_lse = None
         if lse is not None:
-            p_lse = self._tensor(lse, "lse", (self.n_heads, self.rows), torch.float32)
+            p_lse, _ = self._tensor(lse, "lse", (self.n_heads, self.rows), torch.float32)
             if not lse.is_contiguous():
                 raise TypeError("lse: must be contiguous")
         speca_layer_attention(

@@ -14,7 +14,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libspeca.so")
-SOURCES = ["speca_kernels.cu", "speca_static.cu", "speca_layer_rows.cu", "speca_attention_bf16.cu", "speca_attention_f32.cu", "speca_api.cpp", "speca_layer.cpp"]
+SOURCES = ["speca_kernels.cu", "speca_static.cu", "speca_layer_rows.cu", "speca_attention_bf16.cu", "speca_attention_f32.cu", "speca_attention_join.cu",
+           "speca_api.cpp", "speca_layer.cpp"]
 HEADERS = [os.path.join(CSRC, "speca_internal.h"), os.path.join(CSRC, "speca_layer_internal.h"),
            os.path.join(CSRC, "speca_attention_common.cuh"), os.path.join(ROOT, "include", "speca.h")]
 

@@ -38,11 +38,9 @@ __host__ __device__ constexpr int ring_stages(int panels) { return panels == 2 ?
 struct Barriers {
     uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2];
     uint64_t kv_full[8], kv_empty[8];
-    uint64_t part_done[2], last_set[2];
     uint64_t turn[2], drain[2];
     uint32_t tmem;
     uint32_t abort;
-    uint32_t last[2];
 };
 constexpr uint32_t smem_bytes(int panels) {
     return (2 + ring_stages(panels)) * panels * kPanelBytes + static_cast<uint32_t>(sizeof(Barriers));
@@ -478,8 +476,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             bar_init(&bar.s_full[b], 1);
             bar_init(&bar.p_full[b], 4);  // one arrival per warp
             bar_init(&bar.o_full[b], 1);
-            bar_init(&bar.part_done[b], 4);
-            bar_init(&bar.last_set[b], 1);
         }
         for (int i = 0; i < sm.kStages; ++i) {
             bar_init(&bar.kv_full[i], 1);
@@ -520,7 +516,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         const int row = threadIdx.x % 128;
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
         const uint32_t tmem_s = tmem + lanes + b * 128, tmem_o = tmem + lanes + 256 + b * 128;
-        uint32_t s_phase = 0, o_phase = 0, part_phase = 0;
+        uint32_t s_phase = 0, o_phase = 0;
         bool ok = true;
         for (int i = blockIdx.x; i < p.n_units && ok; i += gridDim.x) {
             const AttnUnit u = load_unit(p.units, i);
@@ -643,26 +639,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             if (live) {
                 part[pitch - 4] = ref * p.scale_log2;
                 part[pitch - 3] = total;
-            }
-            __threadfence();
-            __syncwarp();
-            if (lane == 0) bar_arrive(&bar.part_done[b]);
-            ok = warp_wait(&bar.part_done[b], part_phase);
-            if (!ok) break;
-            if (row == 0) {
-                const uint32_t before = atomicAdd(p.tickets + u.ticket + b, 1u);
-                bar.last[b] = before == static_cast<uint32_t>(u.n_splits) - 1;
-                if (bar.last[b]) p.tickets[u.ticket + b] = 0;  // ready for the next launch
-                bar_arrive(&bar.last_set[b]);
-            }
-            __syncwarp();
-            ok = warp_wait(&bar.last_set[b], part_phase);
-            if (!ok) break;
-            part_phase ^= 1;
-            // read by all four warps before they arrive at part_done again, so before it is set again
-            if (*reinterpret_cast<volatile uint32_t*>(&bar.last[b])) {
-                __threadfence();
-                join_rows<__nv_bfloat16>(p, u, u.row0 + b * block_rows, rows, part0, split_stride, warp % 4, 4);
             }
         }
         if (!ok) bar.abort = 1;

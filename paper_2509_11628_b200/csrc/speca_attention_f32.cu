@@ -18,8 +18,21 @@ struct SimtSmem {
     float k[kSimtKeys][kSimtPitch];
     float v[kSimtKeys][kSimtPitch];
     float p[kSimtRows][kSimtKeys + 4];
-    int last;
 };
+
+// One row of up to 128 elements by one warp, zeros behind its end (up to a multiple of 4) or where there is none.
+__device__ __forceinline__ void fill_row(float* dst, const float* src, bool there, int hd, int lane, bool vectors) {
+    if (vectors) {
+        if (lane * 4 < hd)
+            *reinterpret_cast<float4*>(dst + lane * 4) = there ? *reinterpret_cast<const float4*>(src + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < SPECA_MAX_HEAD_DIM / 32; ++i) {
+        const int c = lane + i * 32;
+        if (c < (hd + 3) / 4 * 4) dst[c] = there && c < hd ? src[c] : 0.f;
+    }
+}
 
 __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __grid_constant__ AttnParams p) {
     extern __shared__ __align__(16) char smem_raw[];
@@ -34,13 +47,15 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
     const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     const int hd = p.head_dim, hd4 = (hd + 3) / 4;
 
-    for (int i = threadIdx.x; i < kSimtRows * hd4 * 4; i += kSimtThreads) {
-        const int r = i / (hd4 * 4), c = i % (hd4 * 4), pr = u.row0 + r;
-        float x = 0.f;
-        if (r < rows && c < hd)
-            x = reinterpret_cast<const float*>(p.q)[(u.q_start + pr / p.group) * p.q_row +
-                                                    (u.kv_head * p.group + pr % p.group) * p.q_head + c];
-        sm.q[r][c] = x;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const float* pq = reinterpret_cast<const float*>(p.q);
+    const float* pk = reinterpret_cast<const float*>(p.k) + u.kv_start * p.k_row + u.kv_head * p.k_head;
+    const float* pv = reinterpret_cast<const float*>(p.v) + u.kv_start * p.v_row + u.kv_head * p.v_head;
+#pragma unroll
+    for (int i = 0; i < kSimtRows / 4; ++i) {  // a warp per row
+        const int r = warp + i * 4, pr = u.row0 + r;
+        fill_row(sm.q[r], pq + (u.q_start + pr / p.group) * p.q_row + (u.kv_head * p.group + pr % p.group) * p.q_head, r < rows, hd,
+                 lane, p.vectors);
     }
     int limit[4];
     float m[4], l[4], acc[4][8];
@@ -56,16 +71,12 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
     for (int t = t0; t < t1; ++t) {
         const int key0 = t * kSimtKeys;
         __syncthreads();  // the previous tile has been read
-        for (int i = threadIdx.x; i < kSimtKeys * hd4 * 4; i += kSimtThreads) {
-            const int r = i / (hd4 * 4), c = i % (hd4 * 4);
-            float kx = 0.f, vx = 0.f;  // keys behind kv_len are not read: a weight of zero times whatever they hold may be NaN
-            if (key0 + r < kv_len && c < hd) {
-                const int64_t row = u.kv_start + key0 + r;
-                kx = reinterpret_cast<const float*>(p.k)[row * p.k_row + u.kv_head * p.k_head + c];
-                vx = reinterpret_cast<const float*>(p.v)[row * p.v_row + u.kv_head * p.v_head + c];
-            }
-            sm.k[r][c] = kx;
-            sm.v[r][c] = vx;
+        // keys behind kv_len are not read: a weight of zero times whatever they hold may be NaN
+#pragma unroll
+        for (int i = 0; i < kSimtKeys / 4; ++i) {
+            const int r = warp + i * 4, key = key0 + r;
+            fill_row(sm.k[r], pk + key * p.k_row, key < kv_len, hd, lane, p.vectors);
+            fill_row(sm.v[r], pv + key * p.v_row, key < kv_len, hd, lane, p.vectors);
         }
         __syncthreads();
         float s[4][4] = {};
@@ -161,17 +172,6 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
         if (p.lse != nullptr && tx == 0)
             p.lse[static_cast<int64_t>(head) * p.total_q + tok] = l[r] == 0.f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * kLn2;
     }
-    if (u.n_splits == 1) return;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sm.last = atomicAdd(p.tickets + u.ticket, 1u) == static_cast<uint32_t>(u.n_splits) - 1;
-        if (sm.last) p.tickets[u.ticket] = 0;  // ready for the next launch
-    }
-    __syncthreads();
-    if (!sm.last) return;
-    __threadfence();
-    join_rows<float>(p, u, u.row0, rows, u.part, split_stride, threadIdx.x / 32, kSimtThreads / 32);
 }
 
 }  // namespace

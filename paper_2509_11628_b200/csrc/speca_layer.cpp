@@ -23,24 +23,24 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // How the attention of a storage type cuts its work.
 struct Tiling {
     int rows;          // most packed rows of a unit
-    int counters;      // arrival counters of a shared row block
     int keys;          // keys of a tile
     int target;        // units that fill the device: below it, long key ranges are shared out
     int min_share;     // fewest tiles worth a unit of its own
 };
 // 148 SMs, with two resident blocks each in fp32 and one in bf16.
 Tiling tiling(int dtype, int group) {
-    if (dtype == SPECA_BF16) return Tiling{tc_unit_rows(group), 2, kTcKeys, 148, 4};
-    return Tiling{kSimtRows, 1, kSimtKeys, 296, 4};
+    if (dtype == SPECA_BF16) return Tiling{tc_unit_rows(group), kTcKeys, 148, 4};
+    return Tiling{kSimtRows, kSimtKeys, 296, 4};
 }
 
 struct Plan {
     std::vector<AttnUnit> units;
+    std::vector<JoinBlock> joins;
+    int join_rows = 0;
     std::vector<uint16_t> row_seq;
     std::vector<RopePair> pairs;
-    size_t units_off, row_seq_off, pairs_off, tickets_off, gave_up_off, parts_off, total;
+    size_t units_off, joins_off, row_seq_off, pairs_off, gave_up_off, parts_off, total;
     int64_t total_q, total_kv;
-    size_t counters_bytes;
 };
 
 speca_status_t check_offsets(const int64_t* start, int n, int64_t* total) {
@@ -90,7 +90,6 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
         std::fill(P->row_seq.begin() + qs[s], P->row_seq.begin() + qs[s + 1], static_cast<uint16_t>(s));
 
     size_t part_bytes = 0;
-    int n_tickets = 0;
     if (heads) {
         const int group = c->n_heads / c->n_kv_heads;
         const Tiling tl = tiling(c->dtype, group);
@@ -145,13 +144,15 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
                         u.kv_start = static_cast<int32_t>(ks[s]);
                         u.split = i;
                         u.n_splits = splits;
-                        u.ticket = n_tickets;
+                        u.pad = 0;
                         u.part = static_cast<int64_t>(part_bytes);
                         P->units.push_back(u);
                         cost.push_back(std::max<int64_t>(0, std::min(part_nt, (seen + tl.keys - 1) / tl.keys - i * part_nt)));
                     }
                     if (splits > 1) {
-                        n_tickets += tl.counters;
+                        P->joins.push_back(JoinBlock{s, h, static_cast<int32_t>(r), static_cast<int32_t>(n), static_cast<int32_t>(qs[s]),
+                                                     splits, static_cast<int64_t>(part_bytes)});
+                        P->join_rows = std::max(P->join_rows, static_cast<int>(n));
                         part_bytes += static_cast<size_t>(splits * n * row_bytes);
                     }
                 }
@@ -168,14 +169,14 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
     size_t off = 0;
     P->units_off = off;
     off = align_up(off + P->units.size() * sizeof(AttnUnit), kAlign);
+    P->joins_off = off;
+    off = align_up(off + P->joins.size() * sizeof(JoinBlock), kAlign);
     P->row_seq_off = off;
     off = align_up(off + P->row_seq.size() * sizeof(uint16_t), kAlign);
     P->pairs_off = off;
     off = align_up(off + P->pairs.size() * sizeof(RopePair), kAlign);
-    P->gave_up_off = off;  // the gave-up flag, then the arrival counters: cleared together
-    P->tickets_off = off + kAlign;
-    P->counters_bytes = kAlign + n_tickets * sizeof(uint32_t);
-    off = align_up(off + P->counters_bytes, kAlign);
+    P->gave_up_off = off;
+    off += kAlign;
     P->parts_off = off;
     P->total = off + part_bytes;
     return SPECA_OK;
@@ -210,10 +211,10 @@ struct DeviceGuard {
 struct speca_layer {
     int n_seqs, dtype, n_heads, n_kv_heads, head_dim, causal, n_axes, pairing, rotated, device;
     int64_t total_q, total_kv;
-    int n_units, sm_count;
+    int n_units, n_joins, join_rows, sm_count;
     float scale, norm_eps;
     char* ws;
-    size_t units_off, row_seq_off, pairs_off, tickets_off, gave_up_off, parts_off, counters_bytes;
+    size_t units_off, joins_off, row_seq_off, pairs_off, gave_up_off, parts_off;
     char last_error[256];
 };
 
@@ -295,16 +296,17 @@ speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t
     c->total_q = P.total_q;
     c->total_kv = P.total_kv;
     c->n_units = static_cast<int>(P.units.size());
+    c->n_joins = static_cast<int>(P.joins.size());
+    c->join_rows = P.join_rows;
     c->scale = cfg->scale > 0.f ? cfg->scale : (cfg->head_dim > 0 ? 1.f / std::sqrt(static_cast<float>(cfg->head_dim)) : 1.f);
     c->norm_eps = cfg->norm_eps > 0.f ? cfg->norm_eps : 1e-6f;
     c->ws = static_cast<char*>(cfg->workspace);
     c->units_off = P.units_off;
+    c->joins_off = P.joins_off;
     c->row_seq_off = P.row_seq_off;
     c->pairs_off = P.pairs_off;
-    c->tickets_off = P.tickets_off;
     c->gave_up_off = P.gave_up_off;
     c->parts_off = P.parts_off;
-    c->counters_bytes = P.counters_bytes;
     cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
     DeviceGuard guard(c->device);
     ce = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
@@ -312,9 +314,10 @@ speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t
         if (ce == cudaSuccess && n > 0) ce = cudaMemcpy(c->ws + off, src, n, cudaMemcpyHostToDevice);
     };
     upload(P.units_off, P.units.data(), P.units.size() * sizeof(AttnUnit));
+    upload(P.joins_off, P.joins.data(), P.joins.size() * sizeof(JoinBlock));
     upload(P.row_seq_off, P.row_seq.data(), P.row_seq.size() * sizeof(uint16_t));
     upload(P.pairs_off, P.pairs.data(), P.pairs.size() * sizeof(RopePair));
-    if (ce == cudaSuccess) ce = cudaMemset(c->ws + P.gave_up_off, 0, P.counters_bytes);
+    if (ce == cudaSuccess) ce = cudaMemset(c->ws + P.gave_up_off, 0, sizeof(uint32_t));
     // the copies come from pageable memory: wait, so that work on any stream finds them done
     if (ce == cudaSuccess) ce = cudaDeviceSynchronize();
     if (ce != cudaSuccess) {
@@ -458,19 +461,23 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
     if (!on_elements(c, q) || !on_elements(c, k) || !on_elements(c, v) || !on_elements(c, o) ||
         reinterpret_cast<uintptr_t>(dev_lse) % 4 != 0 || reinterpret_cast<uintptr_t>(dev_kv_len) % 4 != 0)
         return fail(c, SPECA_ERR_ALIGNMENT, "attention: a tensor is not aligned to the element size");
-    if (c->dtype == SPECA_BF16 &&
-        (!on_16(c, q, q_row_stride, q_head_stride) || !on_16(c, k, k_row_stride, k_head_stride) ||
-         !on_16(c, v, v_row_stride, v_head_stride) || !on_16(c, o, o_row_stride, o_head_stride)))
+    const bool wide = on_16(c, q, q_row_stride, q_head_stride) && on_16(c, k, k_row_stride, k_head_stride) &&
+                      on_16(c, v, v_row_stride, v_head_stride) && on_16(c, o, o_row_stride, o_head_stride);
+    if (c->dtype == SPECA_BF16 && !wide)
         return fail(c, SPECA_ERR_ALIGNMENT, "attention: bf16 tensors start on 16 bytes, with strides of multiples of 8 elements");
     AttnParams p;
     p.units = reinterpret_cast<const AttnUnit*>(c->ws + c->units_off);
+    p.joins = reinterpret_cast<const JoinBlock*>(c->ws + c->joins_off);
     p.n_units = c->n_units;
+    p.n_joins = c->n_joins;
+    p.join_rows = c->join_rows;
     p.n_heads = c->n_heads;
     p.n_kv_heads = c->n_kv_heads;
     p.group = c->n_heads / c->n_kv_heads;
     p.head_dim = c->head_dim;
     p.causal = c->causal;
     p.total_q = static_cast<int32_t>(c->total_q);
+    p.vectors = wide && c->head_dim % 4 == 0;
     p.scale_log2 = static_cast<float>(c->scale * 1.4426950408889634);
     p.q = static_cast<const char*>(q);
     p.k = static_cast<const char*>(k);
@@ -482,7 +489,6 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
     p.dev_mask = dev_active_mask;
     p.lse = dev_lse;
     p.parts = c->ws + c->parts_off;
-    p.tickets = reinterpret_cast<uint32_t*>(c->ws + c->tickets_off);
     p.gave_up = reinterpret_cast<uint32_t*>(c->ws + c->gave_up_off);
     DeviceGuard guard(c->device);
     if (!guard.ok) return fail(c, SPECA_ERR_CUDA, "cudaSetDevice failed");
@@ -490,6 +496,7 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
     if (st != SPECA_OK) return st;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t e = c->dtype == SPECA_BF16 ? launch_attention_bf16(p, c->total_kv, c->sm_count, s) : launch_attention_f32(p, s);
+    if (e == cudaSuccess) e = launch_attention_join(p, c->dtype, s);
     if (e == cudaErrorNotSupported)
         return fail(c, SPECA_ERR_UNSUPPORTED, "attention: the copy engine cannot address a tensor with these strides");
     return e == cudaSuccess ? SPECA_OK : cuda_fail(c, e, "attention");
@@ -503,8 +510,7 @@ speca_status_t speca_layer_check(speca_layer_t* c, void* stream) {
     uint32_t gave_up = 0;
     cudaError_t e = cudaMemcpyAsync(&gave_up, c->ws + c->gave_up_off, sizeof gave_up, cudaMemcpyDeviceToHost, s);
     if (e == cudaSuccess) e = cudaStreamSynchronize(s);
-    // the flag and the arrival counters, which a kernel that gave up may have left in between
-    if (e == cudaSuccess && gave_up != 0) e = cudaMemsetAsync(c->ws + c->gave_up_off, 0, c->counters_bytes, s);
+    if (e == cudaSuccess && gave_up != 0) e = cudaMemsetAsync(c->ws + c->gave_up_off, 0, sizeof gave_up, s);
     if (e != cudaSuccess) return cuda_fail(c, e, "check");
     return gave_up == 0 ? SPECA_OK : fail(c, SPECA_ERR_CUDA, "a kernel gave up on a bounded wait: results since the last check are incomplete");
 }

@@ -52,16 +52,25 @@ struct AttnUnit {
     int32_t q_len, kv_cap;
     int32_t q_start, kv_start;
     int32_t split, n_splits;
-    int32_t ticket;   // n_splits > 1: first of the row block's arrival counters
-    int64_t part;     // n_splits > 1: byte offset of the partial results of split 0 of this row block
+    int32_t pad;
+    int64_t part;     // n_splits > 1: byte offset of the partial results of split 0 of this unit's rows
 };
 static_assert(sizeof(AttnUnit) == 48, "three 16-byte loads");
 
+// Rows whose keys were shared out: their partial results are joined by a launch of its own.
+struct JoinBlock {
+    int32_t seq, kv_head, row0, rows, q_start, n_splits;
+    int64_t part;
+};
+static_assert(sizeof(JoinBlock) == 32, "two 16-byte loads");
+
 struct AttnParams {
     const AttnUnit* units;
-    int32_t n_units;
+    const JoinBlock* joins;
+    int32_t n_units, n_joins, join_rows;  // join_rows: the most rows of a block
     int32_t n_heads, n_kv_heads, group, head_dim;
     int32_t causal, total_q;
+    int32_t vectors;   // every row starts on 16 bytes and holds a multiple of 4 elements
     float scale_log2;  // scale * log2(e)
     const char *q, *k, *v;
     char* o;
@@ -69,8 +78,7 @@ struct AttnParams {
     const int32_t* dev_kv_len;
     const uint8_t* dev_mask;
     float* lse;
-    char* parts;        // partial results of split rows
-    uint32_t* tickets;  // arrival counters of split rows, zero between launches
+    char* parts;        // partial results of shared rows
     uint32_t* gave_up;  // set by a wait that ran out
 };
 constexpr int kSimtRows = 32, kSimtKeys = 64;  // rows of a unit, keys of a tile
@@ -79,6 +87,9 @@ cudaError_t launch_attention_f32(const AttnParams& p, cudaStream_t stream);
 __host__ __device__ constexpr int tc_unit_rows(int group) { return 2 * (128 / group * group); }
 constexpr int kTcKeys = 128;
 cudaError_t launch_attention_bf16(const AttnParams& p, int64_t total_kv, int sm_count, cudaStream_t stream);
+
+// Joins the partial results of shared rows, behind either attention kernel on the same stream.
+cudaError_t launch_attention_join(const AttnParams& p, int dtype, cudaStream_t stream);
 
 // Partial result of one row: head_dim sums, then the running maximum (log2 domain) and the sum.
 __host__ __device__ constexpr int64_t part_row_floats(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }
