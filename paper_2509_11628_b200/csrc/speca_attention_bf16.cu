@@ -257,38 +257,46 @@ __device__ __forceinline__ void weights(const float* s, uint64_t scale2, uint64_
     }
 }
 
-// What a unit asks of its two blocks.
+// What a unit asks of its two blocks. Wide units: two blocks of rows against the same key tiles. Narrow ones (few
+// rows against many keys): the same rows twice, each against a share of the keys of its own, so that two chains of
+// products and exponentials hide each other's waits there too.
 struct Work {
     int kv_len;
-    int t0;       // first key tile
+    int t0[2];    // first key tile of each block
     int n[2];     // key tiles of each block
+    int r0[2];    // first packed row of each block
     int rows[2];  // rows of each block
 };
 __device__ __forceinline__ bool unit_work(const AttnParams& p, const AttnUnit& u, int block_rows, Work& w) {
     if (p.dev_mask != nullptr && p.dev_mask[u.seq] == 0) return false;
     w.kv_len = kv_length(p, u);
     const int tiles = (w.kv_len + kTileKeys - 1) / kTileKeys, share = (tiles + u.n_splits - 1) / u.n_splits;
-    w.t0 = u.split * share;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-        const int r0 = u.row0 + b * block_rows;
-        w.rows[b] = max(0, min(block_rows, u.q_len * p.group - r0));
+        const int split = u.split + (u.narrow ? b : 0);
+        w.r0[b] = u.row0 + (u.narrow ? 0 : b * block_rows);
+        w.rows[b] = split < u.n_splits ? max(0, min(block_rows, u.q_len * p.group - w.r0[b])) : 0;
+        w.t0[b] = split * share;
         w.n[b] = 0;
         if (w.rows[b] == 0) continue;
-        const int seen = visible_keys(p, u, w.kv_len, (r0 + w.rows[b] - 1) / p.group);  // by the block's last row
-        w.n[b] = max(0, min(w.t0 + share, (seen + kTileKeys - 1) / kTileKeys) - w.t0);
+        const int seen = visible_keys(p, u, w.kv_len, (w.r0[b] + w.rows[b] - 1) / p.group);  // by the block's last row
+        w.n[b] = max(0, min(w.t0[b] + share, (seen + kTileKeys - 1) / kTileKeys) - w.t0[b]);
     }
     return true;
 }
 
+// A place in the ring of tiles.
 struct Ring {
     int stage = 0;
     uint32_t phase = 0;
-    __device__ __forceinline__ void next(int stages) {
-        if (++stage == stages) {
-            stage = 0;
-            phase ^= 1;
+    __device__ __forceinline__ Ring ahead(int k, int stages) const {
+        Ring r = *this;
+        r.stage += k;
+        if (r.stage >= stages) {
+            r.stage -= stages;
+            r.phase ^= 1;
         }
+        return r;
     }
 };
 
@@ -311,7 +319,7 @@ __device__ __forceinline__ bool load_tiles(const AttnParams& p, const CUtensorMa
     constexpr uint32_t kTileBytes = Smem<PANELS>::kTileBytes;
     constexpr int kStages = Smem<PANELS>::kStages;
     Barriers& bar = sm.bar();
-    const int tokens = kBlockRows / p.group, block_rows = tokens * p.group;
+    const int block_rows = kBlockRows / p.group * p.group;
     Ring ring;
     uint32_t q_phase = 0;  // bit b: block b
     bool ok = true;
@@ -320,14 +328,15 @@ __device__ __forceinline__ bool load_tiles(const AttnParams& p, const CUtensorMa
         bar_expect(&bar.kv_full[ring.stage], kTileBytes);
         for (int i = 0; i < PANELS; ++i)
             tma_load(sm.kv(ring.stage) + i * kPanelBytes, &map, i * 64, head, row, &bar.kv_full[ring.stage]);
-        ring.next(kStages);
+        ring = ring.ahead(1, kStages);
         return true;
     };
     for (int i = blockIdx.x; i < p.n_units && ok; i += gridDim.x) {
         const AttnUnit u = load_unit(p.units, i);
         Work w;
         if (!unit_work(p, u, block_rows, w)) continue;
-        const int n = max(w.n[0], w.n[1]);
+        // tiles of block 0's keys and, in a narrow unit, of block 1's
+        const int n0 = u.narrow ? w.n[0] : max(w.n[0], w.n[1]), n1 = u.narrow ? w.n[1] : 0;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
             if (w.n[b] > 0 && ok) {
@@ -336,15 +345,18 @@ __device__ __forceinline__ bool load_tiles(const AttnParams& p, const CUtensorMa
                     bar_expect(&bar.q_full[b], static_cast<uint32_t>(block_rows) * 128 * PANELS);
                     for (int k = 0; k < PANELS; ++k)
                         tma_load(sm.q(b) + k * kPanelBytes, &map_q, k * 64, u.kv_head * p.group,
-                                 u.q_start + u.row0 / p.group + b * tokens, &bar.q_full[b]);
+                                 u.q_start + w.r0[b] / p.group, &bar.q_full[b]);
                     q_phase ^= 1u << b;
                 }
             }
-            if (b == 0 && n > 0) ok = ok && load_tile(map_k, u.kv_head, u.kv_start + w.t0 * kTileKeys);
+            if ((b == 0 ? n0 : n1) > 0) ok = ok && load_tile(map_k, u.kv_head, u.kv_start + w.t0[b] * kTileKeys);
         }
-        for (int j = 0; j < n && ok; ++j) {
-            const int row = u.kv_start + (w.t0 + j) * kTileKeys;
-            ok = load_tile(map_v, u.kv_head, row) && (j + 1 == n || load_tile(map_k, u.kv_head, row + kTileKeys));
+        for (int j = 0; j < max(n0, n1) && ok; ++j) {
+            const int row0 = u.kv_start + (w.t0[0] + j) * kTileKeys, row1 = u.kv_start + (w.t0[1] + j) * kTileKeys;
+            if (j < n0) ok = load_tile(map_v, u.kv_head, row0);
+            if (j < n1) ok = ok && load_tile(map_v, u.kv_head, row1);
+            if (j + 1 < n0) ok = ok && load_tile(map_k, u.kv_head, row0 + kTileKeys);
+            if (j + 1 < n1) ok = ok && load_tile(map_k, u.kv_head, row1 + kTileKeys);
         }
     }
     if (ok) return true;
@@ -381,73 +393,87 @@ __device__ __forceinline__ bool issue_products(const AttnParams& p, const Smem<(
         const AttnUnit u = load_unit(p.units, i);
         Work w;
         if (!unit_work(p, u, block_rows, w)) continue;
-        const int n = max(w.n[0], w.n[1]), own = b == 0 ? w.n[0] : w.n[1];
-        if (own > 0) {
-            if (!warp_wait(part == 0 ? &bar.q_full[b] : &bar.kv_full[ring.stage], part == 0 ? q_phase : ring.phase)) return false;
-            q_phase ^= 1;
-            tc_fence_after();
-            if (elect_one()) {
-                score(ring.stage, false);
-                if (own == 1) tc_commit(&bar.q_empty[b]);
-                tc_commit(&bar.kv_empty[ring.stage]);
-            }
+        const bool narrow = u.narrow != 0;
+        const int own = b == 0 ? w.n[0] : w.n[1], t0 = b == 0 ? w.t0[0] : w.t0[1];
+        const int n0 = narrow ? w.n[0] : max(w.n[0], w.n[1]), n1 = narrow ? w.n[1] : 0;  // as loaded
+        // a tile that this block has no use for is given back as it arrives
+        auto give_back = [&](Ring at) {
+            if (!warp_wait(&bar.kv_full[at.stage], at.phase)) return false;
+            if (elect_one()) bar_arrive(&bar.kv_empty[at.stage]);
             __syncwarp();
-            ring.next(kStages);
+            return true;
+        };
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if ((c == 0 ? n0 : n1) == 0) continue;
+            if (narrow ? c == b : own > 0) {
+                if (!warp_wait(part == 0 ? &bar.q_full[b] : &bar.kv_full[ring.stage], part == 0 ? q_phase : ring.phase)) return false;
+                q_phase ^= 1;
+                tc_fence_after();
+                if (elect_one()) {
+                    score(ring.stage, false);
+                    if (own == 1) tc_commit(&bar.q_empty[b]);
+                    tc_commit(&bar.kv_empty[ring.stage]);
+                }
+                __syncwarp();
+            } else if (!give_back(ring)) {
+                return false;
+            }
+            ring = ring.ahead(1, kStages);
         }
 #pragma unroll 1
-        for (int j = 0; j < own; ++j) {
-            const Ring v_at = ring;
-            ring.next(kStages);
-            const Ring k_at = j + 1 < own ? ring : v_at;  // the last tile waits for no further keys
-            // The last tile may hold other rows behind kv_len. The product stops at the next multiple of 16 keys and the
-            // rows up to there are cleared (by both blocks): their weight is zero, but zero times NaN is not.
-            const int valid = min(kTileKeys, w.kv_len - (w.t0 + j) * kTileKeys), steps = (valid + 15) / 16;
-            if (valid < steps * 16) {
-                if (!warp_wait(&bar.kv_full[v_at.stage], v_at.phase)) return false;
-                char* v = sm.kv_ptr(v_at.stage) + valid * 128;
-                for (int e = threadIdx.x % 32; e < (steps * 16 - valid) * 8; e += 32)
-                    for (int k = 0; k < kPanels; ++k) *reinterpret_cast<uint4*>(v + k * kPanelBytes + e * 16) = make_uint4(0, 0, 0, 0);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            }
-            // O += P V and the next scores, in turn with the other block
-            const uint64_t v_desc = smem_desc(sm.kv(v_at.stage), kPanelBytes, 1024);
-            if (!warp_wait(part == 0 ? &bar.p_full[b] : part == 1 ? &bar.turn[b] : &bar.kv_full[part == 2 ? v_at.stage : k_at.stage],
-                           part == 0 ? p_phase : part == 1 ? turn : part == 2 ? v_at.phase : k_at.phase))
-                return false;
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int k = 0; k < kTileKeys / 16; ++k)
-                    if (k < steps) mma_ts(tmem_o, tmem_s + k * 8, v_desc + k * 128, kDescO, j > 0 || k > 0);
-                if (j + 1 < own) {
-                    score(k_at.stage, true);
-                    tc_commit(&bar.kv_empty[v_at.stage]);
-                    tc_commit(&bar.kv_empty[k_at.stage]);
-                    if (j + 2 == own) tc_commit(&bar.q_empty[b]);
-                } else {
-                    bar_arrive(&bar.turn[1 - b]);
-                    tc_commit(&bar.o_full[b]);
-                    tc_commit(&bar.kv_empty[v_at.stage]);
+        for (int j = 0; j < max(n0, n1); ++j) {
+            // V_j of block 0's keys, of block 1's, K_j+1 of block 0's, of block 1's, as far as there are such
+            const int v0 = j < n0, v1 = j < n1, k0 = j + 1 < n0, k1 = j + 1 < n1;
+            const Ring at_v1 = ring.ahead(v0, kStages), at_k0 = ring.ahead(v0 + v1, kStages), at_k1 = ring.ahead(v0 + v1 + k0, kStages);
+            const bool second = narrow && b == 1;
+            if (j < own) {
+                const bool more = j + 1 < own;
+                const Ring v_at = second ? at_v1 : ring, k_at = !more ? v_at : second ? at_k1 : at_k0;
+                // The last tile may hold other rows behind kv_len. The product stops at the next multiple of 16 keys and the
+                // rows up to there are cleared (by both blocks): their weight is zero, but zero times NaN is not.
+                const int valid = min(kTileKeys, w.kv_len - (t0 + j) * kTileKeys), steps = (valid + 15) / 16;
+                if (valid < steps * 16) {
+                    if (!warp_wait(&bar.kv_full[v_at.stage], v_at.phase)) return false;
+                    char* v = sm.kv_ptr(v_at.stage) + valid * 128;
+                    for (int e = threadIdx.x % 32; e < (steps * 16 - valid) * 8; e += 32)
+                        for (int k = 0; k < kPanels; ++k) *reinterpret_cast<uint4*>(v + k * kPanelBytes + e * 16) = make_uint4(0, 0, 0, 0);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
                 }
-            }
-            __syncwarp();
-            p_phase ^= 1;
-            turn ^= 1;
-            if (j + 1 < own) ring.next(kStages);
-        }
-        // tiles that only the other block has a use for are given back as they arrive, and turns as they come
-        for (int j = own; j < n; ++j) {
-            for (int t = 0; t < 2; ++t) {
-                if (!warp_wait(&bar.kv_full[ring.stage], ring.phase)) return false;
-                if (elect_one()) bar_arrive(&bar.kv_empty[ring.stage]);
+                // O += P V and the next scores, in turn with the other block
+                const uint64_t v_desc = smem_desc(sm.kv(v_at.stage), kPanelBytes, 1024);
+                if (!warp_wait(part == 0 ? &bar.p_full[b] : part == 1 ? &bar.turn[b] : &bar.kv_full[part == 2 ? v_at.stage : k_at.stage],
+                               part == 0 ? p_phase : part == 1 ? turn : part == 2 ? v_at.phase : k_at.phase))
+                    return false;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
+                    for (int k = 0; k < kTileKeys / 16; ++k)
+                        if (k < steps) mma_ts(tmem_o, tmem_s + k * 8, v_desc + k * 128, kDescO, j > 0 || k > 0);
+                    if (more) {
+                        score(k_at.stage, true);
+                        tc_commit(&bar.kv_empty[v_at.stage]);
+                        tc_commit(&bar.kv_empty[k_at.stage]);
+                        if (j + 2 == own) tc_commit(&bar.q_empty[b]);
+                    } else {
+                        bar_arrive(&bar.turn[1 - b]);
+                        tc_commit(&bar.o_full[b]);
+                        tc_commit(&bar.kv_empty[v_at.stage]);
+                    }
+                }
                 __syncwarp();
-                ring.next(kStages);
+                p_phase ^= 1;
+            } else {
+                if (!warp_wait(&bar.turn[b], turn)) return false;
+                if (elect_one()) bar_arrive(&bar.turn[1 - b]);
+                __syncwarp();
             }
-            if (!warp_wait(&bar.turn[b], turn)) return false;
             turn ^= 1;
-            if (elect_one()) bar_arrive(&bar.turn[1 - b]);
-            __syncwarp();
+            const bool back_v = narrow ? (second ? v0 : v1) != 0 : j >= own && v0, back_k = narrow ? (second ? k0 : k1) != 0 : j + 1 >= own && k0;
+            if (back_v && !give_back(narrow && !second ? at_v1 : ring)) return false;
+            if (back_k && !give_back(narrow && !second ? at_k1 : at_k0)) return false;
+            ring = ring.ahead(v0 + v1 + k0 + k1, kStages);
         }
     }
     return true;
@@ -523,16 +549,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             Work w;
             if (!unit_work(p, u, block_rows, w)) continue;
             const int n = b == 0 ? w.n[0] : w.n[1], rows = b == 0 ? w.rows[0] : w.rows[1];
+            const int t0 = b == 0 ? w.t0[0] : w.t0[1], r0 = b == 0 ? w.r0[0] : w.r0[1];
             if (rows == 0) continue;
-            const int pr = u.row0 + b * block_rows + row;  // packed row of the sequence
+            const int pr = r0 + row;  // packed row of the sequence
             const bool live = row < rows;
             const int limit = live ? visible_keys(p, u, w.kv_len, pr / p.group) : 0;
             // keys that every live row of the block sees: tiles in front of this index need no mask
-            const int open = visible_keys(p, u, w.kv_len, (u.row0 + b * block_rows) / p.group);
+            const int open = visible_keys(p, u, w.kv_len, r0 / p.group);
             float ref = -CUDART_INF_F;  // the maximum that P and the sums refer to
             uint64_t l[2] = {0, 0};   // four running sums in two pairs, joined at the end
             for (int j = 0; j < n; ++j) {
-                const int key0 = (w.t0 + j) * kTileKeys;
+                const int key0 = (t0 + j) * kTileKeys;
                 ok = warp_wait(&bar.s_full[b], s_phase);
                 if (!ok) break;
                 s_phase ^= 1;
@@ -595,16 +622,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 o_phase ^= 1;
                 tc_fence_after();
             }
-            const int unit_rows = w.rows[0] + w.rows[1];
-            const int64_t pitch = part_row_floats(p.head_dim), split_stride = unit_rows * pitch;
-            const int64_t part0 = u.part + b * block_rows * pitch * 4;  // of this block in share 0
+            const int64_t pitch = part_row_floats(p.head_dim);
+            const int unit_rows = u.narrow ? rows : w.rows[0] + w.rows[1], split = u.split + (u.narrow ? b : 0);
             const int tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
             float sums[4];
             unpair(l[0], sums[0], sums[1]);
             unpair(l[1], sums[2], sums[3]);
             const float total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
             const float inv = total == 0.f ? 0.f : 1.f / total;
-            float* part = reinterpret_cast<float*>(p.parts + part0) + u.split * split_stride + row * pitch;
+            float* part = reinterpret_cast<float*>(p.parts + u.part) + (static_cast<int64_t>(split) * unit_rows + pr - u.row0) * pitch;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.o) + tok * p.o_row + head * p.o_head;
             for (int c = 0; c < p.head_dim; c += 16) {
                 uint32_t o[16] = {};

@@ -23,14 +23,15 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // How the attention of a storage type cuts its work.
 struct Tiling {
     int rows;          // most packed rows of a unit
+    int narrow;        // a unit of so few rows takes two shares at once
     int keys;          // keys of a tile
     int target;        // units that fill the device: below it, long key ranges are shared out
     int min_share;     // fewest tiles worth a unit of its own
 };
 // 148 SMs, with two resident blocks each in fp32 and one in bf16.
 Tiling tiling(int dtype, int group) {
-    if (dtype == SPECA_BF16) return Tiling{tc_unit_rows(group), kTcKeys, 148, 4};
-    return Tiling{kSimtRows, kSimtKeys, 296, 4};
+    if (dtype == SPECA_BF16) return Tiling{2 * tc_block_rows(group), tc_block_rows(group), kTcKeys, 148, 4};
+    return Tiling{kSimtRows, 0, kSimtKeys, 296, 4};
 }
 
 struct Plan {
@@ -95,6 +96,7 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
         const Tiling tl = tiling(c->dtype, group);
         const int rows = tl.rows;
         auto blocks = [&](int s) { return ((qs[s + 1] - qs[s]) * group + rows - 1) / rows; };
+        auto narrow = [&](int s) { return (qs[s + 1] - qs[s]) * group <= tl.narrow; };
         auto tiles = [&](int s) { return (ks[s + 1] - ks[s] + tl.keys - 1) / tl.keys; };
         // The share of key tiles a unit takes: all of them, unless that leaves SMs idle. Then the smallest
         // share whose units still fit the device at once (more would only add rows to join).
@@ -104,9 +106,16 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
             if (blocks(s) > 0) longest = std::max(longest, tiles(s));
         }
         if (whole > (int64_t(1) << 26)) return SPECA_ERR_SHAPE;
+        // shares of a sequence's keys; both halves of a narrow unit are put to use where there are tiles for it
+        auto shares = [&](int s, int64_t share) {
+            const int64_t n = std::max<int64_t>(1, (tiles(s) + share - 1) / share);
+            return n == 1 && narrow(s) && tiles(s) >= 2 * tl.min_share ? 2 : n;
+        };
         auto count = [&](int64_t share) {
             int64_t n = 0;
-            for (int s = 0; s < c->n_seqs; ++s) n += blocks(s) * c->n_kv_heads * std::max<int64_t>(1, (tiles(s) + share - 1) / share);
+            for (int s = 0; s < c->n_seqs; ++s) {
+                n += blocks(s) * c->n_kv_heads * (narrow(s) ? (shares(s, share) + 1) / 2 : shares(s, share));
+            }
             return n;
         };
         int64_t share = longest;
@@ -125,7 +134,7 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
         const int64_t row_bytes = part_row_floats(c->head_dim) * 4;
         for (int s = 0; s < c->n_seqs; ++s) {
             const int64_t q_len = qs[s + 1] - qs[s], kv = ks[s + 1] - ks[s], nt = tiles(s);
-            const int splits = static_cast<int>(std::max<int64_t>(1, (nt + share - 1) / share));
+            const int splits = static_cast<int>(shares(s, share));
             if (q_len * group > kMaxRows) return SPECA_ERR_SHAPE;
             for (int h = 0; h < c->n_kv_heads; ++h)
                 for (int64_t r = 0; r < q_len * group; r += rows) {
@@ -133,7 +142,8 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
                     const int64_t last = (r + n - 1) / group;
                     const int64_t seen = c->causal ? std::max<int64_t>(0, std::min(kv, last + 1 + kv - q_len)) : kv;
                     const int64_t part_nt = (nt + splits - 1) / splits;
-                    for (int i = 0; i < splits; ++i) {
+                    const int step = narrow(s) && splits > 1 ? 2 : 1;
+                    for (int i = 0; i < splits; i += step) {
                         AttnUnit u;
                         u.seq = s;
                         u.kv_head = h;
@@ -144,7 +154,7 @@ speca_status_t make_plan_impl(const speca_layer_config_t* c, Plan* P) {
                         u.kv_start = static_cast<int32_t>(ks[s]);
                         u.split = i;
                         u.n_splits = splits;
-                        u.pad = 0;
+                        u.narrow = step == 2;
                         u.part = static_cast<int64_t>(part_bytes);
                         P->units.push_back(u);
                         cost.push_back(std::max<int64_t>(0, std::min(part_nt, (seen + tl.keys - 1) / tl.keys - i * part_nt)));

@@ -52,7 +52,7 @@ struct AttnUnit {
     int32_t q_len, kv_cap;
     int32_t q_start, kv_start;
     int32_t split, n_splits;
-    int32_t pad;
+    int32_t narrow;   // the unit takes shares split and split + 1 of the keys, for rows of one block
     int64_t part;     // n_splits > 1: byte offset of the partial results of split 0 of this unit's rows
 };
 static_assert(sizeof(AttnUnit) == 48, "three 16-byte loads");
@@ -84,7 +84,7 @@ struct AttnParams {
 constexpr int kSimtRows = 32, kSimtKeys = 64;  // rows of a unit, keys of a tile
 cudaError_t launch_attention_f32(const AttnParams& p, cudaStream_t stream);
 // Rows of a unit: two blocks of up to 128, whole queries. NotSupported: the copy engine cannot address a tensor.
-__host__ __device__ constexpr int tc_unit_rows(int group) { return 2 * (128 / group * group); }
+__host__ __device__ constexpr int tc_block_rows(int group) { return 128 / group * group; }
 constexpr int kTcKeys = 128;
 cudaError_t launch_attention_bf16(const AttnParams& p, int64_t total_kv, int sm_count, cudaStream_t stream);
 
