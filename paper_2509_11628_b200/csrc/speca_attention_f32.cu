@@ -20,17 +20,35 @@ struct SimtSmem {
     float p[kSimtRows][kSimtKeys + 4];
 };
 
-// One row of up to 128 elements by one warp, zeros behind its end (up to a multiple of 4) or where there is none.
-__device__ __forceinline__ void fill_row(float* dst, const float* src, bool there, int hd, int lane, bool vectors) {
+// Eight rows of up to 128 elements (row 4 i of `row`, i < 8) by one warp, zeros behind their end (up to a multiple of 4) or
+// where there is none. All loads are issued before the first store waits for one: row by row, a tile's 32 rows
+// per warp took 12 us of latency.
+template <typename Row>
+__device__ __forceinline__ void fill_rows(float (*dst)[kSimtPitch], const Row& row, int hd, int lane, bool vectors) {
     if (vectors) {
-        if (lane * 4 < hd)
-            *reinterpret_cast<float4*>(dst + lane * 4) = there ? *reinterpret_cast<const float4*>(src + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float* src = row(i * 4);
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (src != nullptr && lane * 4 < hd) v[i] = __ldg(reinterpret_cast<const float4*>(src + lane * 4));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (lane * 4 < hd) *reinterpret_cast<float4*>(&dst[i * 4][lane * 4]) = v[i];
         return;
     }
+#pragma unroll 1
+    for (int c = lane; c < (hd + 3) / 4 * 4; c += 32) {
+        float v[8];
 #pragma unroll
-    for (int i = 0; i < SPECA_MAX_HEAD_DIM / 32; ++i) {
-        const int c = lane + i * 32;
-        if (c < (hd + 3) / 4 * 4) dst[c] = there && c < hd ? src[c] : 0.f;
+        for (int i = 0; i < 8; ++i) {
+            const float* src = row(i * 4);
+            v[i] = 0.f;
+            if (src != nullptr && c < hd) v[i] = __ldg(src + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dst[i * 4][c] = v[i];
     }
 }
 
@@ -51,12 +69,13 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
     const float* pq = reinterpret_cast<const float*>(p.q);
     const float* pk = reinterpret_cast<const float*>(p.k) + u.kv_start * p.k_row + u.kv_head * p.k_head;
     const float* pv = reinterpret_cast<const float*>(p.v) + u.kv_start * p.v_row + u.kv_head * p.v_head;
-#pragma unroll
-    for (int i = 0; i < kSimtRows / 4; ++i) {  // a warp per row
-        const int r = warp + i * 4, pr = u.row0 + r;
-        fill_row(sm.q[r], pq + (u.q_start + pr / p.group) * p.q_row + (u.kv_head * p.group + pr % p.group) * p.q_head, r < rows, hd,
-                 lane, p.vectors);
-    }
+    static_assert(kSimtRows == 32 && kSimtKeys == 64, "8 rows of Q and 16 of K and V per warp");
+    auto query = [&](int r) -> const float* {
+        const int pr = u.row0 + warp + r;
+        if (warp + r >= rows) return nullptr;
+        return pq + (u.q_start + pr / p.group) * p.q_row + (u.kv_head * p.group + pr % p.group) * p.q_head;
+    };
+    fill_rows(sm.q + warp, query, hd, lane, p.vectors);
     int limit[4];
     float m[4], l[4], acc[4][8];
 #pragma unroll
@@ -72,14 +91,17 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
         const int key0 = t * kSimtKeys;
         __syncthreads();  // the previous tile has been read
         // keys behind kv_len are not read: a weight of zero times whatever they hold may be NaN
-#pragma unroll
-        for (int i = 0; i < kSimtKeys / 4; ++i) {
-            const int r = warp + i * 4, key = key0 + r;
-            fill_row(sm.k[r], pk + key * p.k_row, key < kv_len, hd, lane, p.vectors);
-            fill_row(sm.v[r], pv + key * p.v_row, key < kv_len, hd, lane, p.vectors);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            const int r0 = half * 32 + warp;
+            auto key = [&](int r) { return key0 + r0 + r < kv_len ? pk + (key0 + r0 + r) * p.k_row : nullptr; };
+            auto value = [&](int r) { return key0 + r0 + r < kv_len ? pv + (key0 + r0 + r) * p.v_row : nullptr; };
+            fill_rows(sm.k + r0, key, hd, lane, p.vectors);
+            fill_rows(sm.v + r0, value, hd, lane, p.vectors);
         }
         __syncthreads();
         float s[4][4] = {};
+#pragma unroll 2  // a tile's code runs once or a few times: written out in full, fetching it took longer than running it
         for (int c = 0; c < hd4; ++c) {
             float4 qa[4], kb[4];
 #pragma unroll
@@ -120,6 +142,7 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
             for (int c = 0; c < 8; ++c) acc[r][c] *= f;
         }
         __syncwarp();  // rows of p belong to one half warp
+#pragma unroll 1
         for (int k = 0; k < kSimtKeys; k += 4) {
             float4 pr[4];
 #pragma unroll
