@@ -241,6 +241,10 @@ void dispatch_modulate(const ModulateParams& p, cudaStream_t stream) {
 // L lanes share one head of one row; each holds 4 pairs (with vectors: consecutive pairs, one or two
 // accesses; else pairs lane, lane + L, ...). Several lane groups share a row: each takes its part of the heads of q
 // and k. The block first forms the rotations of its rows in shared memory: an angle serves every head of a row.
+// Bound by memory in the end (read once, written once), by instructions on the way there: 20926 rows x 48 heads of 128 bf16 with the
+// norm take 106 us = 4.8 TB/s; with angles formed by every lane group, weights read per head and applied apart
+// from the rotation it was 295 us. 3 heads in flight per lane and 4 blocks per SM beat 2, 4 and 6 heads (110, 120, 128 us)
+// and 3 or 5 blocks.
 constexpr int kRopeThreads = 256;
 constexpr int kRopePairs = 4;   // pairs per lane
 constexpr int kRopeAhead = 3;   // heads whose loads are in flight per lane
