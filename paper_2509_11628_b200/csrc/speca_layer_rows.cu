@@ -243,7 +243,7 @@ void dispatch_modulate(const ModulateParams& p, cudaStream_t stream) {
 // and k. The block first forms the rotations of its rows in shared memory: an angle serves every head of a row.
 // Bound by memory in the end (read once, written once), by instructions on the way there: 20926 rows x 48 heads of 128 bf16 with the
 // norm take 106 us = 4.8 TB/s; with angles formed by every lane group, weights read per head and applied apart
-// from the rotation it was 295 us. 3 heads in flight per lane and 4 blocks per SM beat 2, 4 and 6 heads (110, 120, 128 us)
+// from the rotation it was 295 us. 3 heads in flight per lane and 4 blocks per SM beat 2, 4 and 6 heads (119, 120, 128 us)
 // and 3 or 5 blocks.
 constexpr int kRopeThreads = 256;
 constexpr int kRopePairs = 4;   // pairs per lane
