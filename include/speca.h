@@ -595,7 +595,8 @@ typedef struct {
  * Host only. Errors: INVALID_ARG, SHAPE, NOMEM. */
 speca_status_t speca_layer_workspace_bytes(const speca_layer_config_t* cfg, size_t* out_bytes);
 
-/* Builds the handle and fills the workspace (this call copies to the device and waits for it). A layer
+/* Builds the handle and fills the workspace: waits for the device, so that work still pending on the memory is done, copies to
+ * it and waits again, so that work on any stream finds it filled. Not to be called while a stream is captured. A layer
  * serves one stream at a time: the calls of one handle share its workspace.
  * Errors: as above, ALIGNMENT (workspace), NOMEM (workspace too small), UNSUPPORTED (not sm_100), CUDA. */
 speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t** out);

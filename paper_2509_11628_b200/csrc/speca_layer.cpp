@@ -319,7 +319,8 @@ speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t
     c->parts_off = P.parts_off;
     cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, c->device);
     DeviceGuard guard(c->device);
-    ce = guard.ok ? cudaSuccess : cudaErrorInvalidDevice;
+    // what is still pending on the memory (its last user's kernels, on any stream) must not land on the lists written here
+    ce = guard.ok ? cudaDeviceSynchronize() : cudaErrorInvalidDevice;
     auto upload = [&](size_t off, const void* src, size_t n) {
         if (ce == cudaSuccess && n > 0) ce = cudaMemcpy(c->ws + off, src, n, cudaMemcpyHostToDevice);
     };
