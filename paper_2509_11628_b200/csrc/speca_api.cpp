@@ -338,11 +338,15 @@ speca_status_t speca_cache_create(const speca_cache_config_t* cfg, speca_cache_t
         return SPECA_ERR_CUDA;
     }
     const Layout& L = c->L;
-    ce = cudaMemcpy(c->arena + L.segs_off, L.segs.data(), L.segs.size() * sizeof(SegDesc), cudaMemcpyHostToDevice);
+    // what is still pending on the memory (its last user's kernels, on any stream) must not land on the tables written
+    // here, and work on any stream must find them written
+    ce = cudaDeviceSynchronize();
+    if (ce == cudaSuccess) ce = cudaMemcpy(c->arena + L.segs_off, L.segs.data(), L.segs.size() * sizeof(SegDesc), cudaMemcpyHostToDevice);
     for (int k = 0; k < kNumTileSizes && ce == cudaSuccess; ++k)
         ce = cudaMemcpy(c->arena + L.tiles_off[k], L.tiles[k].data(), L.tiles[k].size() * sizeof(uint32_t),
                         cudaMemcpyHostToDevice);
     if (ce == cudaSuccess) ce = cudaMemset(c->arena + L.ticket_off, 0, kCounterBytes);
+    if (ce == cudaSuccess) ce = cudaDeviceSynchronize();
     if (ce != cudaSuccess) {
         delete c;
         return SPECA_ERR_CUDA;
