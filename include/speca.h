@@ -561,6 +561,7 @@ speca_status_t speca_cache_launch_count(const speca_cache_t* cache, uint64_t* ou
  * bf16, the operand type of the tensor cores, and divides by the sum of the rounded weights).
  */
 #define SPECA_MAX_SEQS     512 /* most packed sequences of one layer */
+#define SPECA_MAX_ROWS     2147418112 /* 2^31 - 2^16: most query rows (times the heads that share a key head), key rows, elements of a row */
 #define SPECA_MAX_HEAD_DIM 128
 #define SPECA_MAX_GROUP    128 /* most query heads that share one key / value head */
 #define SPECA_MAX_AXES     4   /* most position axes of the rotary embedding */
@@ -573,7 +574,7 @@ typedef struct speca_layer speca_layer_t; /* opaque, owned by the library */
 
 typedef struct {
     int32_t n_seqs;              /* 1 .. SPECA_MAX_SEQS */
-    const int64_t* host_q_start; /* n_seqs + 1 row offsets, ascending from 0; rows in total below 2^31 */
+    const int64_t* host_q_start; /* n_seqs + 1 row offsets, ascending from 0; at most SPECA_MAX_ROWS in total */
     const int64_t* host_kv_start; /* the same for keys and values; NULL = as the queries */
     int32_t dtype;               /* speca_dtype_t of every tensor */
     int32_t n_heads, n_kv_heads; /* n_kv_heads divides n_heads; query head h reads key head h * n_kv_heads / n_heads.
@@ -606,7 +607,7 @@ speca_status_t speca_layer_create(const speca_layer_config_t* cfg, speca_layer_t
 speca_status_t speca_layer_destroy(speca_layer_t* layer);
 
 /*
- * Adaptive layer norm over rows of `dim` elements (any dim >= 1):
+ * Adaptive layer norm over rows of `dim` elements (1 .. SPECA_MAX_ROWS):
  *   x' = x + gate_s * branch      (x' = x when branch is NULL)
  *   y  = (x' - mean(x')) / sqrt(var(x') + norm_eps) * (1 + scale_s) + shift_s
  * with s the row's sequence. y is computed from the unrounded x'.

@@ -27,7 +27,7 @@ SPECA_LAYOUT_TABLES, SPECA_LAYOUT_HISTORY = 0, 1
 SPECA_FEATURE_IN_PLACE = 1   # as feats[entry]: the features already sit in the planes speca_cache_next_slot names
 SPECA_MAX_ORDER, SPECA_MAX_BATCH, SPECA_MAX_ENTRIES, SPECA_MAX_HORIZON = 4, 64, 512, 8
 SPECA_ROPE_INTERLEAVED, SPECA_ROPE_HALVES = 0, 1
-SPECA_MAX_SEQS, SPECA_MAX_HEAD_DIM, SPECA_MAX_GROUP, SPECA_MAX_AXES = 512, 128, 128, 4
+SPECA_MAX_SEQS, SPECA_MAX_ROWS, SPECA_MAX_HEAD_DIM, SPECA_MAX_GROUP, SPECA_MAX_AXES = 512, (1 << 31) - (1 << 16), 128, 128, 4
 
 EXPORTS = [
     "speca_cache_arena_bytes", "speca_cache_create", "speca_cache_destroy", "speca_cache_reset",

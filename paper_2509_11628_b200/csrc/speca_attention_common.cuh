@@ -23,7 +23,7 @@ __device__ __forceinline__ int kv_length(const AttnParams& p, const AttnUnit& u)
 }
 // Keys that query `i` of the sequence sees: those in front of this index.
 __device__ __forceinline__ int visible_keys(const AttnParams& p, const AttnUnit& u, int kv_len, int i) {
-    return p.causal ? max(0, min(kv_len, i + 1 + kv_len - u.q_len)) : kv_len;
+    return p.causal ? max(0, kv_len - max(0, u.q_len - 1 - i)) : kv_len;
 }
 
 constexpr float kLn2 = 0.6931471805599453f;

@@ -17,7 +17,10 @@ using namespace speca;
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
+// Rows, keys and elements of a row are counted in 32 bits on the device, where they are rounded up to blocks and tiles and
+// key ranges end up to a tile per share behind the last key: the limit leaves room for that.
+constexpr int64_t kMaxRows = SPECA_MAX_ROWS;
+static_assert(kMaxRows + 65536 <= int64_t(1) << 31 && 2 * 296 * kSimtKeys <= 65536 && 296 * kTcKeys <= 65536, "sums of a count and a tile fit");
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // How the attention of a storage type cuts its work.
@@ -355,7 +358,7 @@ speca_status_t speca_layer_modulate(speca_layer_t* c, int32_t dim, const void* x
                                     int64_t mod_stride, const uint8_t* dev_active_mask, void* x_out, int64_t x_out_stride,
                                     void* y, int64_t y_stride, void* stream) {
     if (c == nullptr) return SPECA_ERR_INVALID_ARG;
-    if (dim < 1) return fail(c, SPECA_ERR_SHAPE, "modulate: dim below 1");
+    if (dim < 1 || dim > kMaxRows) return fail(c, SPECA_ERR_SHAPE, "modulate: dim outside 1 .. %lld", static_cast<long long>(kMaxRows));
     for (int64_t* s : {&x_stride, &branch_stride, &x_out_stride, &y_stride}) drop_stride(c->total_q, *s);
     drop_stride(c->n_seqs, mod_stride);
     if (c->total_q > 0 && (x == nullptr || y == nullptr)) return fail(c, SPECA_ERR_INVALID_ARG, "modulate: null tensor");

@@ -41,3 +41,38 @@ def test_work_pending_on_the_arena_ends_before_it_is_written(S, lib):
     assert lib.speca_cache_create(ctypes.byref(cfg), ctypes.byref(out)) == S.SPECA_OK
     events = lib.host_events().decode()
     assert "C" in events and events[0] == "S" and events[-1] == "S", events
+
+
+# ---- limits: kernels round rows and keys up to their tiles in 32 bits ------------------------------------------------
+
+MOST = (1 << 31) - (1 << 16)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("causal", [False, True])
+def test_key_rows_leave_room_to_round_up(S, lib, dtype, causal):
+    kw = dict(causal=causal, n_heads=1, n_kv_heads=1, head_dim=8)
+    args = lambda n: S._layer_config([0, 1], dtype, [0, n], scale=0.0, norm_eps=0.0, axis_dims=(), theta=1.0, pairing=0, **kw)
+    out = ctypes.c_size_t(0)
+    for n, status in ((MOST, S.SPECA_OK), (MOST + 1, S.SPECA_ERR_SHAPE), ((1 << 31) - 1, S.SPECA_ERR_SHAPE)):
+        assert lib.speca_layer_workspace_bytes(ctypes.byref(args(n)), ctypes.byref(out)) == status, n
+
+
+def test_packed_rows_leave_room_to_round_up(S, lib):
+    # rows x heads per key head are indexed in 32 bits too: 128 heads over 2^24 rows reach 2^31
+    out = ctypes.c_size_t(0)
+    for n, status in ((1 << 10, S.SPECA_OK), ((1 << 24) - 511, S.SPECA_ERR_SHAPE), (1 << 24, S.SPECA_ERR_SHAPE)):
+        cfg = S._layer_config([0, n], S.SPECA_BF16, [0, 1], 128, 1, 8, False, 0.0, 0.0, (), 1.0, 0)
+        assert lib.speca_layer_workspace_bytes(ctypes.byref(cfg), ctypes.byref(out)) == status, n
+
+
+def test_modulate_dim_leaves_room_to_round_up(S, lib):
+    layer, mem = H.layer(S, lib, [0, 1], S.SPECA_F32)
+    p, i64 = ctypes.c_void_p(mem.ptr), ctypes.c_int64
+
+    def call(dim):
+        return lib.speca_layer_modulate(layer, dim, p, i64(dim), None, i64(0), None, None, None, i64(0), None, None, i64(0), p, i64(dim), None)
+
+    assert call(MOST) == S.SPECA_OK            # counted by the runtime, not run
+    assert call(MOST + 1) == S.SPECA_ERR_SHAPE
+    assert call((1 << 31) - 1) == S.SPECA_ERR_SHAPE
