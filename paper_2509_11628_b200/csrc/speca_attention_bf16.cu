@@ -591,12 +591,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + 2 * k], s[c + 2 * k + 1]);
                 const float m = max3(max3(top[0], s[124], s[125]), max3(top[1], s[126], s[127]), fmaxf(top[2], top[3]));
-                const bool grow = (m - ref) * p.scale_log2 > kRescale;  // also from -inf, unless m is -inf too
+                // Each row goes by its own scores, so that its weights round the same whatever shares the warp. Rows that are not
+                // live (other sequences' queries, or what shared memory held) have no say. Also from -inf, unless m is -inf too.
+                const float mine = live ? m : -CUDART_INF_F;
+                const bool grow = (mine - ref) * p.scale_log2 > kRescale;
                 if (j == 0) {
                     ref = m;
                 } else if (__any_sync(0xffffffffu, grow)) {
-                    const float next = fmaxf(ref, m);
-                    const float f = next == -CUDART_INF_F ? 1.f : ex2((ref - next) * p.scale_log2);
+                    const float next = grow ? mine : ref, f = grow ? ex2((ref - next) * p.scale_log2) : 1.f;
                     ref = next;
                     l[0] = mul2(l[0], pair(f, f));
                     l[1] = mul2(l[1], pair(f, f));
