@@ -558,7 +558,8 @@ speca_status_t speca_cache_launch_count(const speca_cache_t* cache, uint64_t* ou
  * speca_layer_t holds the packing and, if the workspace is given, everything the calls need on the
  * device. Strides are counted in elements; the last dimension is always dense. All arithmetic is fp32,
  * rounded once to the storage type on the way out (the bf16 attention also rounds the softmax weights to
- * bf16, the operand type of the tensor cores, and divides by the sum of the rounded weights).
+ * bf16, the operand type of the tensor cores, and divides by the sum of the weights before that rounding, but for
+ * the largest of each tile of keys, which counts as rounded: the rounding of a key that dominates a row divides out).
  */
 #define SPECA_MAX_SEQS     512 /* most packed sequences of one layer */
 #define SPECA_MAX_ROWS     2147418112 /* 2^31 - 2^16: most query rows (times the heads that share a key head), key rows, elements of a row */
@@ -656,7 +657,9 @@ speca_status_t speca_layer_rope(speca_layer_t* layer, const void* q, int64_t q_r
  *                 rows and heads in elements. o may not overlap an input.
  *   dev_kv_len    device, n_seqs int32, or NULL: keys that hold data, per sequence (clamped to
  *                 0 .. the sequence's rows in host_kv_start). Read on the device, so a captured call follows a growing cache.
- *   dev_lse       device fp32 [n_heads, query rows] or NULL: natural log of the sum of exp(scale * <q, k>).
+ *   dev_lse       device fp32 [n_heads, query rows] or NULL: natural log of the sum of exp(scale * <q, k>), of the weights
+ *                 before any rounding to bf16 (in bf16 to 8e-5 beside the scores' own error: one exponential in four
+ *                 is formed by a polynomial).
  * bf16 runs on the tensor cores and needs q, k, v and o on 16-byte boundaries with strides of multiples
  * of 8 elements. Results do not depend on the launch: no atomics on values, a fixed order of sums.
  * Errors: INVALID_ARG, STATE (a layer without heads), SHAPE, ALIGNMENT, UNSUPPORTED (a stride the copy

@@ -569,6 +569,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             const int open = visible_keys(p, u, w.kv_len, r0 / p.group);
             float ref = -CUDART_INF_F;  // the maximum that P and the sums refer to
             uint64_t l[2] = {0, 0};   // four running sums in two pairs, joined at the end
+            float off = 0.f;          // what the largest weights' rounding added, for the divisor alone
             for (int j = 0; j < n; ++j) {
                 const int key0 = (t0 + j) * kTileKeys;
                 ok = warp_wait(&bar.s_full[b], s_phase);
@@ -602,6 +603,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     ref = next;
                     l[0] = mul2(l[0], pair(f, f));
                     l[1] = mul2(l[1], pair(f, f));
+                    off *= f;
                     for (int c = 0; c < p.head_dim; c += 16) {
                         uint32_t o[16];
                         tmem_load16(tmem_o + c, o);
@@ -613,10 +615,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 }
                 const float shift = ref == -CUDART_INF_F ? 0.f : -ref * p.scale_log2;
                 const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
-                // The sum is over the weights before their rounding to bf16, but for the largest of each tile: where one
-                // key dominates, its rounding must divide out.
+                // The sum is over the weights before their rounding to bf16. In the divisor the largest of each tile counts
+                // as rounded: where one key dominates, its rounding must divide out.
                 const float e_top = ex2(fmaf(m, p.scale_log2, shift));
-                l[0] = add2(l[0], pair(__uint_as_float(pack_bf16(0.f, e_top)) - e_top, 0.f));
+                off += __uint_as_float(pack_bf16(0.f, e_top)) - e_top;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t packed[32];
@@ -642,7 +644,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             unpair(l[0], sums[0], sums[1]);
             unpair(l[1], sums[2], sums[3]);
             const float total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-            const float inv = total == 0.f ? 0.f : 1.f / total;
+            const float inv = total == 0.f ? 0.f : 1.f / (total + off);
             float* part = reinterpret_cast<float*>(p.parts + u.part) + (static_cast<int64_t>(split) * unit_rows + pr - u.row0) * pitch;
             __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.o) + tok * p.o_row + head * p.o_head;
             for (int c = 0; c < p.head_dim; c += 16) {
@@ -678,6 +680,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             if (live) {
                 part[pitch - 4] = ref * p.scale_log2;
                 part[pitch - 3] = total;
+                part[pitch - 2] = total + off;
             }
         }
         if (!ok) bar.abort = 1;

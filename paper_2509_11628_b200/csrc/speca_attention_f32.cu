@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
             }
             if (tx == 0) {
                 part[pitch - 4] = m[r];
-                part[pitch - 3] = l[r];
+                part[pitch - 3] = part[pitch - 2] = l[r];
             }
             continue;
         }

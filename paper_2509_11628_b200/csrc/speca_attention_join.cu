@@ -1,8 +1,8 @@
 // Joins the partial results of rows whose keys were shared out over several units.
 //
-// Share s of a row left sums O_s, their weights' sum l_s and the maximum m_s they refer to; the row is
-// sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s with m the largest m_s, added up in the order of the shares. One warp per
-// row: the statistics of 32 shares at once by the lanes, then the sums with the lanes across the head.
+// Share s of a row left sums O_s, their divisor d_s, their weights' sum l_s and the maximum m_s they refer to; the row is
+// sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) d_s with m the largest m_s, its log-sum that of the l_s, added up in the order of the
+// shares. One warp per row: the statistics of 32 shares at once by the lanes, then the sums with the lanes across the head.
 #include "speca_attention_common.cuh"
 
 namespace speca {
@@ -30,16 +30,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_cons
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.f;
+    float l = 0.f, d = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const bool holds = lane * 4 < p.head_dim;
     for (int s0 = 0; s0 < jb.n_splits; s0 += 32) {
-        float w = 0.f, wl = 0.f;  // a share that saw nothing left its sums unwritten: weight zero, not read
+        float w = 0.f, wl = 0.f, wd = 0.f;  // a share that saw nothing left its sums unwritten: weight zero, not read
         if (s0 + lane < jb.n_splits) {
-            const float2 stat = *reinterpret_cast<const float2*>(base + (s0 + lane) * stride + pitch - 4);
+            const float4 stat = *reinterpret_cast<const float4*>(base + (s0 + lane) * stride + pitch - 4);
             if (stat.y != 0.f) {
                 w = exp2f(stat.x - m);
                 wl = w * stat.y;
+                wd = w * stat.z;
             }
         }
         const int n = min(32, jb.n_splits - s0);
@@ -56,6 +57,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_cons
                 if (s + k >= n) break;
                 const float ws = __shfl_sync(0xffffffffu, w, s + k);
                 l += __shfl_sync(0xffffffffu, wl, s + k);
+                d += __shfl_sync(0xffffffffu, wd, s + k);
                 acc.x = fmaf(ws, v[k].x, acc.x);
                 acc.y = fmaf(ws, v[k].y, acc.y);
                 acc.z = fmaf(ws, v[k].z, acc.z);
@@ -64,7 +66,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const __grid_cons
         }
     }
     const int pr = jb.row0 + row, tok = jb.q_start + pr / p.group, head = jb.kv_head * p.group + pr % p.group;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const float inv = l == 0.f ? 0.f : 1.f / d;
     T* o = reinterpret_cast<T*>(p.o) + tok * p.o_row + head * p.o_head + lane * 4;
     const float out[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
 #pragma unroll

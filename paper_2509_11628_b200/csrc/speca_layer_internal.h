@@ -91,7 +91,8 @@ cudaError_t launch_attention_bf16(const AttnParams& p, int64_t total_kv, int sm_
 // Joins the partial results of shared rows, behind either attention kernel on the same stream.
 cudaError_t launch_attention_join(const AttnParams& p, int dtype, cudaStream_t stream);
 
-// Partial result of one row: head_dim sums, then the running maximum (log2 domain) and the sum.
+// Partial result of one row: head_dim sums, then the running maximum (log2 domain), the sum of the weights and what the
+// sums divide by (the same, but for the rounding of the largest weights to bf16).
 __host__ __device__ constexpr int64_t part_row_floats(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }
 
 }  // namespace speca
