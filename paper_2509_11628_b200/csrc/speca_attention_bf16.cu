@@ -245,18 +245,18 @@ __device__ __forceinline__ void ex2_poly(uint64_t x2, float& e0, float& e1) {
     e0 = x0 >= -125.f ? __uint_as_float(__float_as_uint(e0) + (__float_as_uint(t0) << 23)) : max_nan(x0, 0.f);
     e1 = x1 >= -125.f ? __uint_as_float(__float_as_uint(e1) + (__float_as_uint(t1) << 23)) : max_nan(x1, 0.f);
 }
-// Of the pairs, one in this many by polynomial (0: none): 4608 rows x 24 heads of 128 / 16 heads of 64 took 231 / 140 us
+// Of the pairs, the last of so many by polynomial: 4608 rows x 24 heads of 128 / 16 heads of 64 took 231 / 140 us
 // with none, 222 / 127 with one in 8 or 4, 227 / 132 with one in 2.
 constexpr int kPolyEvery = 4;
+static_assert(kPolyEvery == 4, "the softmax keeps the maximum of the polynomial's keys apart");
 
 // Weights of 64 keys of a row, rounded to bf16, and their sum before the rounding.
-template <int EVERY>
 __device__ __forceinline__ void weights(const float* s, uint64_t scale2, uint64_t shift2, uint32_t* packed, uint64_t* l) {
 #pragma unroll
     for (int c = 0; c < 32; ++c) {
         const uint64_t x2 = fma2(pair(s[2 * c], s[2 * c + 1]), scale2, shift2);
         float e0, e1;
-        if (EVERY > 0 && c % (EVERY > 0 ? EVERY : 1) == EVERY - 1) {
+        if (c % kPolyEvery == kPolyEvery - 1) {
             ex2_poly(x2, e0, e1);
         } else {
             unpair(x2, e0, e1);
@@ -586,12 +586,14 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
                     for (int c = 0; c < 128; ++c) s[c] = c < seen ? s[c] : -CUDART_INF_F;
                 }
-                float top[4] = {s[0], s[1], s[2], s[3]};
+                float top[4];  // of the pairs by their place in eight keys: the last are the polynomial's
 #pragma unroll
-                for (int c = 4; c < 124; c += 8)
+                for (int k = 0; k < 4; ++k) top[k] = fmaxf(s[2 * k], s[2 * k + 1]);
+#pragma unroll
+                for (int c = 8; c < 128; c += 8)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[c + 2 * k], s[c + 2 * k + 1]);
-                const float m = max3(max3(top[0], s[124], s[125]), max3(top[1], s[126], s[127]), fmaxf(top[2], top[3]));
+                const float m_ex2 = max3(top[0], top[1], top[2]), m = max3(top[3], m_ex2, m_ex2);
                 // Each row goes by its own scores, so that its weights round the same whatever shares the warp. Rows that are not
                 // live (other sequences' queries, or what shared memory held) have no say. Also from -inf, unless m is -inf too.
                 const float mine = live ? m : -CUDART_INF_F;
@@ -616,13 +618,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 const float shift = ref == -CUDART_INF_F ? 0.f : -ref * p.scale_log2;
                 const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), shift2 = pair(shift, shift);
                 // The sum is over the weights before their rounding to bf16. In the divisor the largest of each tile counts
-                // as rounded: where one key dominates, its rounding must divide out.
-                const float e_top = ex2(fmaf(m, p.scale_log2, shift));
+                // as rounded: where one key dominates, its rounding must divide out. Formed as the stored weight was, since
+                // next to a rounding boundary of bf16 the polynomial and the special function unit round apart.
+                const float x_top = fmaf(m, p.scale_log2, shift);
+                float e_top, e_poly;
+                ex2_poly(pair(x_top, x_top), e_poly, e_top);
+                e_top = m > m_ex2 ? e_poly : ex2(x_top);
                 off += __uint_as_float(pack_bf16(0.f, e_top)) - e_top;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t packed[32];
-                    weights<kPolyEvery>(s + h * 64, scale2, shift2, packed, l);
+                    weights(s + h * 64, scale2, shift2, packed, l);
                     tmem_store32(tmem_s + h * 32, packed);
                 }
                 tmem_wait_store();

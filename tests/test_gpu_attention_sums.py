@@ -69,6 +69,19 @@ def test_lse_is_that_of_the_exact_weights(S, at, n, rows):
     assert float(((lse - want).abs() - bound).max()) <= 0, float((lse - want).abs().max())
 
 
+@pytest.mark.parametrize("at,n,rows", CASES)
+def test_the_rounding_of_a_dominating_weight_divides_out(S, at, n, rows):
+    # one value behind all keys: o is it, times the weights' sum as multiplied over the sum as divided by. They may differ by
+    # the polynomial's error and the first key's, both far below half a unit of bf16 (2^-9), so the bits are v's.
+    for seed in range(8 if rows < 100 else 1):
+        g = torch.rand(rows, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV) * 7.6 + 0.3
+        q, k, v, _ = scores(g, [at], n, rows, 2, one_v=True, seed=seed)
+        o, _ = attend(S, q, k, v)
+        want = v[:1].expand_as(o)
+        off = (o != want).any(-1)
+        assert not bool(off.any()), "%d of %d rows" % (int(off.sum()), off.numel())
+
+
 def test_exponentials_of_every_key_of_eight(S):
     # the weights of the tile's keys of one residue mod 8 against key 0: an exponential off by more than the polynomial's
     # error shows in the sum, for arguments from 2^-8 to just below 2^8
