@@ -651,8 +651,8 @@ speca_status_t speca_layer_rope(speca_layer_t* layer, const void* q, int64_t q_r
  *   o_i = sum_j p_ij v_j,  p_i = softmax over the visible j of scale * <q_i, k_j>.
  * Visible are the first kv_len keys of the sequence, and with `causal` only j <= i + kv_len - q_len (the
  * queries are the sequence's last rows, so one query per sequence is a decoding step). A row that sees nothing gets
- * zeros (and lse = -inf). Keys and values behind kv_len are never used, whatever they hold; a value that
- * is visible to some rows of a tile but not to others must be finite to leave the others alone (0 * inf).
+ * zeros (and lse = -inf), whatever is hidden from it. Keys and values behind kv_len are never used, whatever they hold; a value that
+ * is visible to some rows of a tile must be finite to leave those others alone that see a part of the tile (0 * inf).
  *   q, o          device, [query rows, n_heads, head_dim];  k, v: [key rows, n_kv_heads, head_dim]. Strides of
  *                 rows and heads in elements. o may not overlap an input.
  *   dev_kv_len    device, n_seqs int32, or NULL: keys that hold data, per sequence (clamped to

@@ -660,6 +660,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                     tmem_wait_load<16>(o);
                 }
                 if (!live) continue;
+                if (total == 0.f) {  // sees nothing: zero, also where a weight of zero met a value that is not finite
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) o[k] = 0;
+                }
                 if (u.n_splits > 1) {
 #pragma unroll
                     for (int k = 0; k < 16; k += 4)

@@ -187,12 +187,13 @@ __global__ void __launch_bounds__(kSimtThreads) attention_f32_kernel(const __gri
             continue;
         }
         const int tok = u.q_start + pr / p.group, head = u.kv_head * p.group + pr % p.group;
-        const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+        const float inv = 1.f / l[r];
         float* o = reinterpret_cast<float*>(p.o) + tok * p.o_row + head * p.o_head;
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             const int col = tx * 4 + (c / 4) * 64 + c % 4;
-            if (col < hd) o[col] = acc[r][c] * inv;
+            // a row that sees nothing: zero, also where a weight of zero met a value that is not finite
+            if (col < hd) o[col] = l[r] == 0.f ? 0.f : acc[r][c] * inv;
         }
         if (p.lse != nullptr && tx == 0)
             p.lse[static_cast<int64_t>(head) * p.total_q + tok] = l[r] == 0.f ? -CUDART_INF_F : (m[r] + log2f(l[r])) * kLn2;

@@ -75,3 +75,19 @@ def test_rows_of_one_sequence_do_not_show_in_each_other(S, dt, group):
     assert torch.equal(got[::2], want[::2]) and torch.equal(lse[:, ::2], want_lse[:, ::2])
     assert not torch.equal(got[1::2], want[1::2])
     layer.check()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("q_len,kv,split", [(200, 40, False), (64, 10, False), (140, 130, False), (6, 3000, True)])
+def test_rows_that_see_nothing_are_zero_whatever_is_hidden_from_them(S, dt, q_len, kv, split):
+    # causal, more queries than keys that hold data: the first rows see nothing, while other rows of their block read the tile
+    fill = 4 if split else kv
+    q, k, v = make(9, dt, q_len, kv, 4, 2, 64)
+    v[:fill, 0, :] = float("inf")
+    v[1, 1, 3] = float("nan")
+    k[2, 1, 5] = float("nan")
+    layer = S.SpecaLayer([0, q_len], code(S, dt), kv_start=[0, kv], n_heads=4, n_kv_heads=2, head_dim=64, causal=True, device=DEV)
+    o, lse = call(layer, q, k, v, kv_len=torch.tensor([fill], dtype=torch.int32, device=DEV))
+    n = q_len - fill
+    assert n > 0 and bool((o[:n] == 0).all()) and bool((lse[:, :n] == -float("inf")).all())
+    layer.check()
