@@ -637,8 +637,7 @@ speca_status_t speca_layer_modulate(speca_layer_t* layer, int32_t dim, const voi
  *   (head_dim must be even.)
  *   positions           device fp32 [rows, n_axes], dense.
  *   q_weight, k_weight  device, head_dim elements, or NULL.
- * Errors: INVALID_ARG, STATE (a layer without axes), SHAPE (a stride below head_dim where there is more than
- * one head or row), ALIGNMENT (to the element), CUDA.
+ * Errors: INVALID_ARG, STATE (a layer without axes), SHAPE (an output whose rows or heads share memory), ALIGNMENT (to the element), CUDA.
  */
 speca_status_t speca_layer_rope(speca_layer_t* layer, const void* q, int64_t q_row_stride, int64_t q_head_stride, void* q_out,
                                 int64_t q_out_row_stride, int64_t q_out_head_stride, const void* k, int64_t k_row_stride,
@@ -662,7 +661,7 @@ speca_status_t speca_layer_rope(speca_layer_t* layer, const void* q, int64_t q_r
  *                 is formed by a polynomial).
  * bf16 runs on the tensor cores and needs q, k, v and o on 16-byte boundaries with strides of multiples
  * of 8 elements. Results do not depend on the launch: no atomics on values, a fixed order of sums.
- * Errors: INVALID_ARG, STATE (a layer without heads), SHAPE, ALIGNMENT, UNSUPPORTED (a stride the copy
+ * Errors: INVALID_ARG, STATE (a layer without heads), SHAPE (rows or heads of o share memory), ALIGNMENT, UNSUPPORTED (a stride the copy
  * engine cannot address: 2^40 bytes or more), CUDA.
  */
 speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,

@@ -259,6 +259,19 @@ inline bool on_elements(const speca_layer* c, const void* p) { return reinterpre
 inline void drop_stride(int64_t count, int64_t& stride) {
     if (count <= 1) stride = 0;
 }
+// Whether two of rows x heads pieces of `dim` elements with these strides share an element.
+bool meets_itself(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t dim) {
+    if (rows == 0 || (rows > 1 && row < dim) || (heads > 1 && head < dim)) return rows != 0;
+    if (rows <= 1 || heads <= 1) return false;
+    using Wide = __int128;
+    if (row >= Wide(heads - 1) * head + dim || head >= Wide(rows - 1) * row + dim) return false;
+    // pieces of different rows in turn: head j of a row against head 0 of the rows next to it
+    for (int64_t j = 1; j < heads; ++j) {
+        const Wide at = Wide(j) * head, r = at / row, behind = at - r * row;
+        if ((r < rows && behind < dim) || (r + 1 < rows && row - behind < dim)) return true;
+    }
+    return false;
+}
 // Rows that start on 16 bytes everywhere: an absent tensor does not stand in the way.
 inline bool on_16(const speca_layer* c, const void* p, int64_t s0, int64_t s1) {
     if (p == nullptr) return true;
@@ -414,8 +427,8 @@ speca_status_t speca_layer_rope(speca_layer_t* c, const void* q, int64_t q_row_s
         return fail(c, SPECA_ERR_INVALID_ARG, "rope: null tensor");
     if (q_row_stride < 0 || q_head_stride < 0 || k_row_stride < 0 || k_head_stride < 0)
         return fail(c, SPECA_ERR_SHAPE, "rope: negative stride");
-    if ((c->total_q > 1 && q_out_row_stride < c->head_dim) || (c->n_heads > 1 && q_out_head_stride < c->head_dim) ||
-        (k_out != nullptr && ((c->total_q > 1 && k_out_row_stride < c->head_dim) || (c->n_kv_heads > 1 && k_out_head_stride < c->head_dim))))
+    if (meets_itself(c->total_q, q_out_row_stride, c->n_heads, q_out_head_stride, c->head_dim) ||
+        (k_out != nullptr && meets_itself(c->total_q, k_out_row_stride, c->n_kv_heads, k_out_head_stride, c->head_dim)))
         return fail(c, SPECA_ERR_SHAPE, "rope: outputs overlap");
     if (!on_elements(c, q) || !on_elements(c, q_out) || !on_elements(c, k) || !on_elements(c, k_out) || !on_elements(c, q_weight) ||
         !on_elements(c, k_weight) || reinterpret_cast<uintptr_t>(positions) % 4 != 0)
@@ -470,7 +483,7 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
         return fail(c, SPECA_ERR_INVALID_ARG, "attention: null tensor");
     if (q_row_stride < 0 || q_head_stride < 0 || k_row_stride < 0 || k_head_stride < 0 || v_row_stride < 0 || v_head_stride < 0)
         return fail(c, SPECA_ERR_SHAPE, "attention: negative stride");
-    if ((c->total_q > 1 && o_row_stride < c->head_dim) || (c->n_heads > 1 && o_head_stride < c->head_dim))
+    if (meets_itself(c->total_q, o_row_stride, c->n_heads, o_head_stride, c->head_dim))
         return fail(c, SPECA_ERR_SHAPE, "attention: output rows overlap");
     if (!on_elements(c, q) || !on_elements(c, k) || !on_elements(c, v) || !on_elements(c, o) ||
         reinterpret_cast<uintptr_t>(dev_lse) % 4 != 0 || reinterpret_cast<uintptr_t>(dev_kv_len) % 4 != 0)

@@ -23,6 +23,10 @@ def load(folder):
     assert handle
     lib = ctypes.CDLL(so, handle=handle)
     lib.host_events.restype = ctypes.c_char_p
+    vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    lib.speca_layer_modulate.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp]
+    lib.speca_layer_rope.argtypes = [vp] + [vp, i64, i64] * 4 + [vp] * 5
+    lib.speca_layer_attention.argtypes = [vp] + [vp, i64, i64] * 4 + [vp] * 4
     return lib
 
 

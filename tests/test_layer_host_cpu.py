@@ -76,3 +76,46 @@ def test_modulate_dim_leaves_room_to_round_up(S, lib):
     assert call(MOST) == S.SPECA_OK            # counted by the runtime, not run
     assert call(MOST + 1) == S.SPECA_ERR_SHAPE
     assert call((1 << 31) - 1) == S.SPECA_ERR_SHAPE
+
+
+# ---- outputs that share memory: a race between blocks ---------------------------------------------------------------
+
+A, B, C, D = (1 << 20, 2 << 20, 3 << 20, 4 << 20)   # addresses; nothing is launched, nothing read
+
+
+def refused(S, lib, status, what):
+    lib.host_events_clear()
+    assert status() == what
+    assert lib.host_events() == (b"" if what != S.SPECA_OK else b"L")
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_outputs_that_overlap_themselves_are_refused(S, lib, dtype):
+    rows, h, hd = 6, 4, 16
+    layer, _mem = H.layer(S, lib, [0, rows], dtype, n_heads=h, n_kv_heads=h, head_dim=hd, axis_dims=(hd,))
+    dense = (h * hd, hd)
+
+    def attend(rs, hs):
+        return lambda: lib.speca_layer_attention(layer, A, *dense, B, *dense, C, *dense, D, rs, hs, None, None, None, None)
+
+    def rope(rs, hs):
+        return lambda: lib.speca_layer_rope(layer, A, *dense, B, rs, hs, None, 0, 0, None, 0, 0, C, None, None, None, None)
+
+    def rope_k(rs, hs):
+        return lambda: lib.speca_layer_rope(layer, A, *dense, A, *dense, B, *dense, C, rs, hs, D, None, None, None, None)
+
+    fine = [(h * hd, hd), (hd, rows * hd), (h * hd + 8, hd), (3 * hd, 18 * hd), (8 * hd, 2 * hd),
+            (16 * 8, 16 * 3),            # heads of different rows in turn, without meeting: 48 h + 128 r
+            (16 * 3, 16 * 20)]
+    shared = [(hd, hd), (2 * hd, hd), (hd, 2 * hd), (h * hd - 8, hd), (hd, rows * hd - 8), (3 * hd, 2 * hd), (2 * hd, 3 * hd),
+              (16 * 4 + 8, 16 * 4), (hd - 8, h * hd), (h * hd, hd - 8)]
+    for strides in fine + shared:
+        places = sorted(r * strides[0] + j * strides[1] for r in range(rows) for j in range(h))
+        meets = any(b - a < hd for a, b in zip(places, places[1:]))
+        assert meets == (strides in shared), strides
+        for call in (attend, rope, rope_k):
+            refused(S, lib, call(*strides), S.SPECA_ERR_SHAPE if meets else S.SPECA_OK)
+    # one row, or one head: that stride says nothing
+    one, _m = H.layer(S, lib, [0, 1], dtype, n_heads=h, n_kv_heads=h, head_dim=hd, axis_dims=(hd,))
+    refused(S, lib, lambda: lib.speca_layer_attention(one, A, 0, hd, B, 0, hd, C, 0, hd, D, 0, hd, None, None, None, None), S.SPECA_OK)
+    refused(S, lib, lambda: lib.speca_layer_attention(one, A, 0, hd, B, 0, hd, C, 0, hd, D, hd, hd - 8, None, None, None, None), S.SPECA_ERR_SHAPE)
