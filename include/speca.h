@@ -613,8 +613,8 @@ speca_status_t speca_layer_destroy(speca_layer_t* layer);
  *   y  = (x' - mean(x')) / sqrt(var(x') + norm_eps) * (1 + scale_s) + shift_s
  * with s the row's sequence. y is computed from the unrounded x'.
  *   x, branch, x_out, y   device, [rows, dim], row strides in elements. branch may be NULL; x_out may be
- *                         NULL (x' is then not stored) and may be x itself; y may be x or branch unless
- *                         x_out names that tensor too.
+ *                         NULL (x' is then not stored). Each output may be x or branch itself, with the same
+ *                         stride, but y and x_out not the same tensor; otherwise nothing may overlap an output.
  *   gate, scale, shift    device, [n_seqs, dim], row stride mod_stride; each may be NULL (gate: 1; scale,
  *                         shift: 0). gate needs branch.
  * Rows whose addresses and strides are multiples of 16 bytes take the vector path.
@@ -633,7 +633,8 @@ speca_status_t speca_layer_modulate(speca_layer_t* layer, int32_t dim, const voi
  * Axes take the pairs in order: the first axis_dims[0] / 2 pairs, and so on. The angle is reduced in fp64, so a
  * position of any size costs no accuracy.
  *   q, q_out, k, k_out  device, [rows, n_heads (k: n_kv_heads), head_dim], strides of rows and heads in
- *                       elements. k and k_out may both be NULL. q_out may be q, k_out may be k, with the same strides.
+ *                       elements. k and k_out may both be NULL. q_out may be q, k_out may be k, with the same strides;
+ *                       otherwise nothing may overlap an output.
  *   (head_dim must be even.)
  *   positions           device fp32 [rows, n_axes], dense.
  *   q_weight, k_weight  device, head_dim elements, or NULL.

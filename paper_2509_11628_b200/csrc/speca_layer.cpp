@@ -380,6 +380,11 @@ speca_status_t speca_layer_modulate(speca_layer_t* c, int32_t dim, const void* x
         return fail(c, SPECA_ERR_SHAPE, "modulate: negative stride");
     if (c->total_q > 1 && (y_stride < dim || (x_out != nullptr && x_out_stride < dim)))
         return fail(c, SPECA_ERR_SHAPE, "modulate: output rows overlap");
+    // in place each thread writes what it alone has read, which takes the same strides
+    if (c->total_q > 0 && ((y == x && y_stride != x_stride) || (y == branch && y_stride != branch_stride) || y == x_out ||
+                           (x_out == x && x_out_stride != x_stride) ||
+                           (x_out != nullptr && x_out == branch && x_out_stride != branch_stride)))
+        return fail(c, SPECA_ERR_INVALID_ARG, "modulate: in place needs the strides of the input, and y and x_out apart");
     if (!on_elements(c, x) || !on_elements(c, branch) || !on_elements(c, gate) || !on_elements(c, scale) || !on_elements(c, shift) ||
         !on_elements(c, x_out) || !on_elements(c, y))
         return fail(c, SPECA_ERR_ALIGNMENT, "modulate: a tensor is not aligned to the element size");
@@ -430,6 +435,11 @@ speca_status_t speca_layer_rope(speca_layer_t* c, const void* q, int64_t q_row_s
     if (meets_itself(c->total_q, q_out_row_stride, c->n_heads, q_out_head_stride, c->head_dim) ||
         (k_out != nullptr && meets_itself(c->total_q, k_out_row_stride, c->n_kv_heads, k_out_head_stride, c->head_dim)))
         return fail(c, SPECA_ERR_SHAPE, "rope: outputs overlap");
+    // in place each lane writes what it alone has read, which takes the same strides
+    if (c->total_q > 0 && ((q_out == q && (q_out_row_stride != q_row_stride || q_out_head_stride != q_head_stride)) ||
+                           (k != nullptr && k_out == k && (k_out_row_stride != k_row_stride || k_out_head_stride != k_head_stride)) ||
+                           (k != nullptr && (q_out == k_out || q_out == k || k_out == q))))
+        return fail(c, SPECA_ERR_INVALID_ARG, "rope: in place needs the strides of the input, and q and k apart");
     if (!on_elements(c, q) || !on_elements(c, q_out) || !on_elements(c, k) || !on_elements(c, k_out) || !on_elements(c, q_weight) ||
         !on_elements(c, k_weight) || reinterpret_cast<uintptr_t>(positions) % 4 != 0)
         return fail(c, SPECA_ERR_ALIGNMENT, "rope: a tensor is not aligned to the element size");
@@ -485,6 +495,8 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
         return fail(c, SPECA_ERR_SHAPE, "attention: negative stride");
     if (meets_itself(c->total_q, o_row_stride, c->n_heads, o_head_stride, c->head_dim))
         return fail(c, SPECA_ERR_SHAPE, "attention: output rows overlap");
+    if (c->total_q > 0 && (o == q || o == k || o == v))
+        return fail(c, SPECA_ERR_INVALID_ARG, "attention: the output overlaps an input");
     if (!on_elements(c, q) || !on_elements(c, k) || !on_elements(c, v) || !on_elements(c, o) ||
         reinterpret_cast<uintptr_t>(dev_lse) % 4 != 0 || reinterpret_cast<uintptr_t>(dev_kv_len) % 4 != 0)
         return fail(c, SPECA_ERR_ALIGNMENT, "attention: a tensor is not aligned to the element size");

@@ -119,3 +119,46 @@ def test_outputs_that_overlap_themselves_are_refused(S, lib, dtype):
     one, _m = H.layer(S, lib, [0, 1], dtype, n_heads=h, n_kv_heads=h, head_dim=hd, axis_dims=(hd,))
     refused(S, lib, lambda: lib.speca_layer_attention(one, A, 0, hd, B, 0, hd, C, 0, hd, D, 0, hd, None, None, None, None), S.SPECA_OK)
     refused(S, lib, lambda: lib.speca_layer_attention(one, A, 0, hd, B, 0, hd, C, 0, hd, D, hd, hd - 8, None, None, None, None), S.SPECA_ERR_SHAPE)
+
+
+def test_rope_in_place_needs_the_strides_of_its_input(S, lib):
+    rows, h, hd = 6, 4, 16
+    layer, _mem = H.layer(S, lib, [0, rows], S.SPECA_F32, n_heads=h, n_kv_heads=h, head_dim=hd, axis_dims=(hd,))
+    dense, other = (h * hd, hd), (hd, rows * hd)
+
+    def call(q, qs, qo, qos, k=None, ks=(0, 0), ko=None, kos=(0, 0)):
+        return lambda: lib.speca_layer_rope(layer, q, *qs, qo, *qos, k, *ks, ko, *kos, 64, None, None, None, None)
+
+    refused(S, lib, call(A, dense, A, dense), S.SPECA_OK)
+    refused(S, lib, call(A, dense, A, other), S.SPECA_ERR_INVALID_ARG)
+    refused(S, lib, call(A, (0, hd), A, dense), S.SPECA_ERR_INVALID_ARG)      # broadcast rows
+    refused(S, lib, call(A, dense, B, other), S.SPECA_OK)
+    refused(S, lib, call(A, dense, A, dense, B, dense, B, dense), S.SPECA_OK)
+    refused(S, lib, call(A, dense, A, dense, B, dense, B, other), S.SPECA_ERR_INVALID_ARG)
+    refused(S, lib, call(A, dense, C, dense, B, dense, C, dense), S.SPECA_ERR_INVALID_ARG)   # one place for both
+    refused(S, lib, call(A, dense, B, dense, B, dense, C, dense), S.SPECA_ERR_INVALID_ARG)   # q over k
+    refused(S, lib, call(A, dense, C, dense, B, dense, A, dense), S.SPECA_ERR_INVALID_ARG)   # k over q
+
+
+def test_attention_does_not_write_over_its_inputs(S, lib):
+    layer, _mem = H.layer(S, lib, [0, 6], S.SPECA_BF16, n_heads=4, n_kv_heads=4, head_dim=16)
+    dense = (64, 16)
+    for o, status in ((A, "INVALID_ARG"), (B, "INVALID_ARG"), (C, "INVALID_ARG"), (D, None)):
+        refused(S, lib, lambda: lib.speca_layer_attention(layer, A, *dense, B, *dense, C, *dense, o, *dense, None, None, None, None),
+                S.SPECA_OK if status is None else S.SPECA_ERR_INVALID_ARG)
+
+
+def test_modulate_in_place_needs_the_strides_of_its_input(S, lib):
+    layer, _mem = H.layer(S, lib, [0, 6], S.SPECA_F32)
+
+    def call(x, xs, b, bs, xo, xos, y, ys):
+        return lambda: lib.speca_layer_modulate(layer, 32, x, xs, b, bs, None, None, None, 0, None, xo, xos, y, ys, None)
+
+    refused(S, lib, call(A, 32, None, 0, None, 0, A, 32), S.SPECA_OK)
+    refused(S, lib, call(A, 32, None, 0, None, 0, A, 64), S.SPECA_ERR_INVALID_ARG)
+    refused(S, lib, call(A, 0, None, 0, None, 0, A, 32), S.SPECA_ERR_INVALID_ARG)     # one row for all
+    refused(S, lib, call(A, 32, B, 32, A, 32, B, 32), S.SPECA_OK)                     # both in place
+    refused(S, lib, call(A, 32, B, 40, C, 32, B, 32), S.SPECA_ERR_INVALID_ARG)
+    refused(S, lib, call(A, 32, B, 32, A, 40, C, 32), S.SPECA_ERR_INVALID_ARG)
+    refused(S, lib, call(A, 32, B, 32, B, 32, C, 32), S.SPECA_OK)
+    refused(S, lib, call(A, 32, B, 32, C, 32, C, 32), S.SPECA_ERR_INVALID_ARG)        # one place for both outputs
