@@ -164,6 +164,14 @@ def _dev_ptr(x) -> Optional[int]:
     return int(x)
 
 
+def _indexed(device) -> torch.device:
+    """The device with its index: ``"cuda"`` alone means the current one, as it does where its memory is allocated."""
+    device = torch.device(device)
+    if device.type == "cuda" and device.index is None:
+        device = torch.device("cuda", torch.cuda.current_device())
+    return device
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
         return torch.cuda.current_stream().cuda_stream or None
@@ -453,7 +461,10 @@ def speca_layer_create(q_start, dtype, workspace, kv_start=None, n_heads=0, n_kv
     """Returns the opaque handle (an integer address). ``workspace`` is a CUDA uint8 tensor the caller keeps alive, or
     a raw device address together with ``workspace_bytes``."""
     if isinstance(workspace, torch.Tensor):
+        _dev_ptr(workspace)     # on a GPU
         device = workspace.device.index if device is None else device
+        if workspace.device.index != device:
+            raise ValueError("the workspace is on %s, the layer on device %d" % (workspace.device, device))
         workspace_bytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
     cfg = _layer_config(q_start, dtype, kv_start, n_heads, n_kv_heads, head_dim, causal, scale, norm_eps, axis_dims, theta, pairing)
     cfg.workspace, cfg.workspace_bytes, cfg.device = _dev_ptr(workspace), workspace_bytes or 0, device or 0
@@ -640,7 +651,7 @@ class SpecaLayer:
     def __init__(self, q_start, dtype, kv_start=None, n_heads=0, n_kv_heads=0, head_dim=0, causal=False, scale=0.0, norm_eps=0.0,
                  axis_dims=(), theta=10000.0, pairing=SPECA_ROPE_INTERLEAVED, device="cuda:0"):
         self.handle = None
-        self.device = torch.device(device)
+        self.device = _indexed(device)
         self.n_seqs, self.n_heads, self.n_kv_heads, self.head_dim = len(q_start) - 1, n_heads, n_kv_heads, head_dim
         self.rows = int(q_start[-1])
         self.kv_rows = int(kv_start[-1]) if kv_start is not None else self.rows

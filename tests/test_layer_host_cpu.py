@@ -162,3 +162,41 @@ def test_modulate_in_place_needs_the_strides_of_its_input(S, lib):
     refused(S, lib, call(A, 32, B, 32, A, 40, C, 32), S.SPECA_ERR_INVALID_ARG)
     refused(S, lib, call(A, 32, B, 32, B, 32, C, 32), S.SPECA_OK)
     refused(S, lib, call(A, 32, B, 32, C, 32, C, 32), S.SPECA_ERR_INVALID_ARG)        # one place for both outputs
+
+
+# ---- the device of a handle ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("asked,current,index", [("cuda", 1, 1), ("cuda", 0, 0), ("cuda:1", 0, 1), ("cuda:0", 1, 0)])
+def test_workspace_and_handle_are_on_one_device(S, monkeypatch, asked, current, index):
+    import torch
+    seen = {}
+
+    def empty(n, dtype, device):
+        device = torch.device(device)
+        seen["workspace"] = current if device.index is None else device.index
+        return object()
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+    monkeypatch.setattr(S.torch, "empty", empty)
+    monkeypatch.setattr(S, "speca_layer_create", lambda q, dt, ws, device=None, **kw: seen.update(handle=device) or 0)
+    layer = S.SpecaLayer([0, 4], S.SPECA_BF16, device=asked, **HEADS)
+    assert seen == {"workspace": index, "handle": index}
+    assert layer.device == torch.device("cuda", index) and layer.index == index
+
+
+def test_create_refuses_a_workspace_of_another_device(S, monkeypatch):
+    import torch
+
+    class There(torch.Tensor):
+        """A CPU tensor that says it lives on cuda:1."""
+        is_cuda = True
+        device = torch.device("cuda", 1)
+
+    ws = torch.empty(1 << 16, dtype=torch.uint8).as_subclass(There)
+    called = []
+    monkeypatch.setattr(S, "_lib", lambda: called.append(1))
+    with pytest.raises(ValueError, match="cuda:1"):
+        S.speca_layer_create([0, 4], S.SPECA_BF16, ws, device=0)
+    with pytest.raises(TypeError):      # host memory
+        S.speca_layer_create([0, 4], S.SPECA_BF16, torch.empty(1 << 16, dtype=torch.uint8), device=0)
+    assert not called
