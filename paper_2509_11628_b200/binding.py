@@ -529,13 +529,13 @@ class SpecaCache:
         self.entries = [(int(n), int(d)) for n, d in entries]
         self.batch, self.max_order, self.dtype, self.basis = batch, max_order, dtype, basis
         self.layout, self.path = layout, path
-        self.device = torch.device(device)
+        self.device = _indexed(device)
         self.verify_entry = verify_entry if verify_entry >= 0 else len(self.entries) - 1
         nbytes = speca_cache_arena_bytes(self.entries, batch, max_order, dtype, basis, verify_entry, path, layout)
         self.arena = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         assert self.arena.data_ptr() % 256 == 0
         self.handle = speca_cache_create(self.entries, batch, max_order, dtype, self.arena, basis, verify_entry,
-                                         eps, self.device.index or 0, path, layout=layout)
+                                         eps, self.device.index, path, layout=layout)
 
     def close(self):
         if self.handle:

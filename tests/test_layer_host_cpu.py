@@ -200,3 +200,24 @@ def test_create_refuses_a_workspace_of_another_device(S, monkeypatch):
     with pytest.raises(TypeError):      # host memory
         S.speca_layer_create([0, 4], S.SPECA_BF16, torch.empty(1 << 16, dtype=torch.uint8), device=0)
     assert not called
+
+
+@pytest.mark.parametrize("asked,current,index", [("cuda", 1, 1), ("cuda:1", 0, 1), ("cuda:0", 1, 0)])
+def test_arena_and_cache_are_on_one_device(S, monkeypatch, asked, current, index):
+    import torch
+    seen = {}
+
+    class Arena:
+        def data_ptr(self):
+            return 256
+
+    def empty(n, dtype, device):
+        device = torch.device(device)
+        seen["arena"] = current if device.index is None else device.index
+        return Arena()
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current)
+    monkeypatch.setattr(S.torch, "empty", empty)
+    monkeypatch.setattr(S, "speca_cache_create", lambda e, b, m, dt, arena, basis, ve, eps, device, path, **kw: seen.update(handle=device) or 0)
+    cache = S.SpecaCache([(4, 8)], 1, 1, S.SPECA_BF16, device=asked)
+    assert seen == {"arena": index, "handle": index} and cache.device == torch.device("cuda", index)
