@@ -464,7 +464,7 @@ def speca_layer_create(q_start, dtype, workspace, kv_start=None, n_heads=0, n_kv
         _dev_ptr(workspace)     # on a GPU
         device = workspace.device.index if device is None else device
         if workspace.device.index != device:
-            raise ValueError("the workspace is on %s, the layer on device %d" % (workspace.device, device))
+            raise SpecaError(SPECA_ERR_INVALID_ARG, "the workspace is on %s, the layer on device %d" % (workspace.device, device))
         workspace_bytes = workspace.numel() * workspace.element_size() if workspace_bytes is None else workspace_bytes
     cfg = _layer_config(q_start, dtype, kv_start, n_heads, n_kv_heads, head_dim, causal, scale, norm_eps, axis_dims, theta, pairing)
     cfg.workspace, cfg.workspace_bytes, cfg.device = _dev_ptr(workspace), workspace_bytes or 0, device or 0

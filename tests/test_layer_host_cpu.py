@@ -184,7 +184,7 @@ def test_workspace_and_handle_are_on_one_device(S, monkeypatch, asked, current, 
     assert layer.device == torch.device("cuda", index) and layer.index == index
 
 
-def test_create_refuses_a_workspace_of_another_device(S, monkeypatch):
+def test_create_refuses_a_workspace_of_another_device(S):
     import torch
 
     class There(torch.Tensor):
@@ -193,13 +193,11 @@ def test_create_refuses_a_workspace_of_another_device(S, monkeypatch):
         device = torch.device("cuda", 1)
 
     ws = torch.empty(1 << 16, dtype=torch.uint8).as_subclass(There)
-    called = []
-    monkeypatch.setattr(S, "_lib", lambda: called.append(1))
-    with pytest.raises(ValueError, match="cuda:1"):
+    with pytest.raises(S.SpecaError, match="cuda:1") as e:
         S.speca_layer_create([0, 4], S.SPECA_BF16, ws, device=0)
+    assert e.value.status == S.SPECA_ERR_INVALID_ARG
     with pytest.raises(TypeError):      # host memory
         S.speca_layer_create([0, 4], S.SPECA_BF16, torch.empty(1 << 16, dtype=torch.uint8), device=0)
-    assert not called
 
 
 @pytest.mark.parametrize("asked,current,index", [("cuda", 1, 1), ("cuda:1", 0, 1), ("cuda:0", 1, 0)])
