@@ -661,9 +661,9 @@ speca_status_t speca_layer_rope(speca_layer_t* layer, const void* q, int64_t q_r
  *                 before any rounding to bf16 (in bf16 to 8e-5 beside the scores' own error: one exponential in four
  *                 is formed by a polynomial).
  * bf16 runs on the tensor cores and needs q, k, v and o on 16-byte boundaries with strides of multiples
- * of 8 elements. Results do not depend on the launch: no atomics on values, a fixed order of sums.
- * Errors: INVALID_ARG, STATE (a layer without heads), SHAPE (rows or heads of o share memory), ALIGNMENT, UNSUPPORTED (a stride the copy
- * engine cannot address: 2^40 bytes or more), CUDA.
+ * of 8 elements, none of them zero but that of the key heads of k and v. Results do not depend on the launch: no atomics on values, a fixed order of sums.
+ * Errors: INVALID_ARG, STATE (a layer without heads), SHAPE (rows or heads of o share memory), ALIGNMENT, UNSUPPORTED (bf16: a stride the copy
+ * engine cannot address: zero over rows or query heads, 2^40 bytes or more), CUDA.
  */
 speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_t q_row_stride, int64_t q_head_stride,
                                      const void* k, int64_t k_row_stride, int64_t k_head_stride, const void* v,

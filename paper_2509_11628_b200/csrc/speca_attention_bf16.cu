@@ -346,6 +346,7 @@ __device__ __forceinline__ bool load_tiles(const AttnParams& p, const CUtensorMa
         const AttnUnit u = load_unit(p.units, i);
         Work w;
         if (!unit_work(p, u, block_rows, w)) continue;
+        const int k_head = u.kv_head * p.k_step, v_head = u.kv_head * p.v_step;
         // tiles of block 0's keys and, in a narrow unit, of block 1's
         const int n0 = u.narrow ? w.n[0] : max(w.n[0], w.n[1]), n1 = u.narrow ? w.n[1] : 0;
 #pragma unroll
@@ -360,14 +361,14 @@ __device__ __forceinline__ bool load_tiles(const AttnParams& p, const CUtensorMa
                     q_phase ^= 1u << b;
                 }
             }
-            if ((b == 0 ? n0 : n1) > 0) ok = ok && load_tile(map_k, u.kv_head, u.kv_start + w.t0[b] * kTileKeys);
+            if ((b == 0 ? n0 : n1) > 0) ok = ok && load_tile(map_k, k_head, u.kv_start + w.t0[b] * kTileKeys);
         }
         for (int j = 0; j < max(n0, n1) && ok; ++j) {
             const int row0 = u.kv_start + (w.t0[0] + j) * kTileKeys, row1 = u.kv_start + (w.t0[1] + j) * kTileKeys;
-            if (j < n0) ok = load_tile(map_v, u.kv_head, row0);
-            if (j < n1) ok = ok && load_tile(map_v, u.kv_head, row1);
-            if (j + 1 < n0) ok = ok && load_tile(map_k, u.kv_head, row0 + kTileKeys);
-            if (j + 1 < n1) ok = ok && load_tile(map_k, u.kv_head, row1 + kTileKeys);
+            if (j < n0) ok = load_tile(map_v, v_head, row0);
+            if (j < n1) ok = ok && load_tile(map_v, v_head, row1);
+            if (j + 1 < n0) ok = ok && load_tile(map_k, k_head, row0 + kTileKeys);
+            if (j + 1 < n1) ok = ok && load_tile(map_k, k_head, row1 + kTileKeys);
         }
     }
     if (ok) return true;
@@ -746,8 +747,8 @@ cudaError_t launch_attention_bf16(const AttnParams& p, int64_t total_kv, int sm_
     const char* vb = total_kv > 0 ? p.v : p.q;
     const int64_t kv_rows = total_kv > 0 ? total_kv : 1;
     if (!encode(&q, p.q, p.head_dim, p.n_heads, p.total_q, p.q_row, p.q_head, p.group, kBlockRows / p.group) ||
-        !encode(&k, kb, p.head_dim, p.n_kv_heads, kv_rows, p.k_row, p.k_head, 1, kTileKeys) ||
-        !encode(&v, vb, p.head_dim, p.n_kv_heads, kv_rows, p.v_row, p.v_head, 1, kTileKeys))
+        !encode(&k, kb, p.head_dim, p.k_step ? p.n_kv_heads : 1, kv_rows, p.k_row, p.k_head, 1, kTileKeys) ||
+        !encode(&v, vb, p.head_dim, p.v_step ? p.n_kv_heads : 1, kv_rows, p.v_row, p.v_head, 1, kTileKeys))
         return cudaErrorNotSupported;
     using Kernel = void (*)(AttnParams, CUtensorMap, CUtensorMap, CUtensorMap);
     static const Kernel kernels[] = {attention_bf16_kernel<1>, attention_bf16_kernel<2>, attention_bf16_kernel<3>, attention_bf16_kernel<4>,

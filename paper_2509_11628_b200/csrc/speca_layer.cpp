@@ -504,6 +504,9 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
                       on_16(c, v, v_row_stride, v_head_stride) && on_16(c, o, o_row_stride, o_head_stride);
     if (c->dtype == SPECA_BF16 && !wide)
         return fail(c, SPECA_ERR_ALIGNMENT, "attention: bf16 tensors start on 16 bytes, with strides of multiples of 8 elements");
+    if (c->dtype == SPECA_BF16 && ((c->total_q > 1 && q_row_stride == 0) || (c->n_heads > 1 && q_head_stride == 0) ||
+                                   (c->total_kv > 1 && (k_row_stride == 0 || v_row_stride == 0))))
+        return fail(c, SPECA_ERR_UNSUPPORTED, "attention: the copy engine cannot step by zero over queries or rows");
     AttnParams p;
     p.units = reinterpret_cast<const AttnUnit*>(c->ws + c->units_off);
     p.joins = reinterpret_cast<const JoinBlock*>(c->ws + c->joins_off);
@@ -516,6 +519,8 @@ speca_status_t speca_layer_attention(speca_layer_t* c, const void* q, int64_t q_
     p.head_dim = c->head_dim;
     p.causal = c->causal;
     p.total_q = static_cast<int32_t>(c->total_q);
+    p.k_step = k_head_stride != 0;
+    p.v_step = v_head_stride != 0;
     p.vectors = wide && c->head_dim % 4 == 0;
     p.scale_log2 = static_cast<float>(c->scale * 1.4426950408889634);
     p.q = static_cast<const char*>(q);

@@ -70,6 +70,7 @@ struct AttnParams {
     int32_t n_units, n_joins, join_rows;  // join_rows: the most rows of a block
     int32_t n_heads, n_kv_heads, group, head_dim;
     int32_t causal, total_q;
+    int32_t k_step, v_step;  // 0: all key heads are one in memory, else 1
     int32_t vectors;   // every row starts on 16 bytes and holds a multiple of 4 elements
     float scale_log2;  // scale * log2(e)
     const char *q, *k, *v;

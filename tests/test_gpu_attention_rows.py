@@ -91,3 +91,16 @@ def test_rows_that_see_nothing_are_zero_whatever_is_hidden_from_them(S, dt, q_le
     n = q_len - fill
     assert n > 0 and bool((o[:n] == 0).all()) and bool((lse[:, :n] == -float("inf")).all())
     layer.check()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("group", [1, 3])
+def test_keys_and_values_expanded_over_heads(S, dt, group):
+    q, k, v = make(11, dt, 90, 300, 4 * group, 4, 64)
+    layer = S.SpecaLayer([0, 40, 90], code(S, dt), kv_start=[0, 150, 300], n_heads=4 * group, n_kv_heads=4, head_dim=64, device=DEV)
+    for wide_k, wide_v in ((True, True), (True, False), (False, True)):
+        kk = k[:, 1:2].expand(-1, 4, -1) if wide_k else k
+        vv = v[:, 2:3].expand(-1, 4, -1) if wide_v else v
+        got, want = call(layer, q, kk, vv), call(layer, q, kk.contiguous(), vv.contiguous())
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    layer.check()

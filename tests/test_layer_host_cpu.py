@@ -219,3 +219,20 @@ def test_arena_and_cache_are_on_one_device(S, monkeypatch, asked, current, index
     monkeypatch.setattr(S, "speca_cache_create", lambda e, b, m, dt, arena, basis, ve, eps, device, path, **kw: seen.update(handle=device) or 0)
     cache = S.SpecaCache([(4, 8)], 1, 1, S.SPECA_BF16, device=asked)
     assert seen == {"arena": index, "handle": index} and cache.device == torch.device("cuda", index)
+
+
+# ---- broadcast operands of the bf16 attention ------------------------------------------------------------------------
+
+def test_operands_that_the_copy_engine_cannot_repeat_are_refused(S, lib):
+    # a tensor map steps by a multiple of 16 bytes that is not zero; heads that share one key head's memory need no step
+    rows, h, hd = 6, 4, 16
+    dense, one_row, one_head = (h * hd, hd), (0, hd), (hd, 0)
+    for dtype in (S.SPECA_F32, S.SPECA_BF16):
+        layer, _mem = H.layer(S, lib, [0, rows], dtype, n_heads=h, n_kv_heads=h, head_dim=hd)
+        for q, k, v, fine in ((dense, dense, dense, True), (dense, one_head, dense, True), (dense, dense, one_head, True),
+                              (dense, one_row, dense, False), (dense, dense, one_row, False), (one_row, dense, dense, False),
+                              (one_head, dense, dense, False), ((0, 0), dense, dense, False), (dense, (0, 0), dense, False)):
+            refused(S, lib, lambda: lib.speca_layer_attention(layer, A, *q, B, *k, C, *v, D, *dense, None, None, None, None),
+                    S.SPECA_OK if fine or dtype == S.SPECA_F32 else S.SPECA_ERR_UNSUPPORTED)
+        one, _m = H.layer(S, lib, [0, 1], dtype, n_heads=1, n_kv_heads=1, head_dim=hd)     # strides that say nothing
+        refused(S, lib, lambda: lib.speca_layer_attention(one, A, 0, 0, B, 0, 0, C, 0, 0, D, 0, 0, None, None, None, None), S.SPECA_OK)
