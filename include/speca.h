@@ -630,8 +630,8 @@ speca_status_t speca_layer_modulate(speca_layer_t* layer, int32_t dim, const voi
  * with the RMS norm over the head that such blocks put before it:
  *   u = x * rsqrt(mean(x^2) + norm_eps) * weight   (u = x when the weight is NULL)
  *   (a, b) -> (a cos w - b sin w, a sin w + b cos w) for every pair, w = position[axis of the pair] * its frequency.
- * Axes take the pairs in order: the first axis_dims[0] / 2 pairs, and so on. The angle is reduced in fp64, so a
- * position of any size costs no accuracy.
+ * Axes take the pairs in order: the first axis_dims[0] / 2 pairs, and so on. The angle is reduced in fp64: up to
+ * |position| = 2^26 it is good to fp32 (behind that its error grows with the position).
  *   q, q_out, k, k_out  device, [rows, n_heads (k: n_kv_heads), head_dim], strides of rows and heads in
  *                       elements. k and k_out may both be NULL. q_out may be q, k_out may be k, with the same strides;
  *                       otherwise nothing may overlap an output.
