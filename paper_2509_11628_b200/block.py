@@ -5,7 +5,8 @@ layer norm, projections, rotary positions with the heads' RMS norm, attention ov
 residuals, MLP -- built from ``speca_layer_modulate``, ``speca_layer_rope`` and ``speca_layer_attention`` with plain
 matrix products in between. ``BlockStack`` runs L of them with random weights as the sampler's model: a full step computes and
 caches every block's output; a speculative step computes the last block alone, on the forecast of its input, which
-is the fresh feature that verification compares with the forecast of its output.
+is the fresh feature that verification compares with the forecast of its output. The layer calls skip samples that are not
+active; the products in between run over all rows.
 
     python -m paper_2509_11628_b200.block        # a sampler run over a small stack, per-step decisions and counts
 """

@@ -9,17 +9,18 @@
 //   warps 9, 10      issue the products of block 0 and block 1 (warp 11 completes the warpgroup)
 // Products of one thread run in the order of issue, so S_b(j+1) may overwrite P_b(j) right behind the product
 // that reads it, and S_b(j+1) being ready says that O_b is at rest: the softmax threads themselves rescale O in the
-// rare tile that raises a row's maximum by more than 2^8 (sums and P are exact to a common factor; it keeps
-// P <= 2^8, far inside bf16's range).
+// rare tile that raises a row's largest weight by more than 2^8 (sums and P are exact to a common factor; it keeps
+// P <= 2^8, far inside bf16's range). The weights are rounded to bf16 because the tensor cores take them so: an error of up
+// to 2^-8 of each, independent from key to key, of which the largest of a tile is taken into the divisor.
 // Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
 //
 // What bounds it: products and exponentials of a tile take as long as each other (128 x 128 x 128 twice is 1024 cycles of
 // the tensor pipe, 128 x 128 exponentials are 1024 of the special function units), and a block's chain
-// scores -> weights -> product -> next scores leaves each pipe idle in between: tensor pipe 54 % active, special function
-// units 42 %, about 3500 cycles per tile of both blocks. In a loop the card runs into its power limit
-// (990 W, 1740 MHz) before anything else. Measured: 4608 rows x 24 heads of 128, 215 to 278 us over several cards (0.94 to
-// 1.21 PFLOP/s), 20926 rows 4.85 to 5.36 ms (1.0 to 1.1). Tried and not kept, 4608 rows on one card: 64-key tiles with
-// the scores double buffered 238 us, the same with two warpgroups taking turns at the tiles 245, one score buffer
+// scores -> weights -> product -> next scores leaves each pipe idle in between: tensor pipe 56 % active, special function
+// units 42 %, about 3500 cycles per tile of both blocks. In a loop the card also runs into its power limit
+// (990 W, 1740 MHz). Measured: 4608 rows x 24 heads of 128, 250 to 270 us over several cards (0.97 to 1.04 PFLOP/s),
+// 20926 rows 4.76 to 5.09 ms (1.05 to 1.12). Tried and not kept, 4608 rows on one card, all under an earlier softmax: 64-key
+// tiles with the scores double buffered 238 us, the same with two warpgroups taking turns at the tiles 245, one score buffer
 // and P beside it 240 to 265, against 221 of this form.
 #include <cuda.h>
 
@@ -597,6 +598,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 const float m_ex2 = max3(top[0], top[1], top[2]), m = max3(top[3], m_ex2, m_ex2);
                 // Each row goes by its own scores, so that its weights round the same whatever shares the warp. Rows that are not
                 // live (other sequences' queries, or what shared memory held) have no say. Also from -inf, unless m is -inf too.
+                // (Equal forms of this update took 4.99 to 5.65 ms for 20926 rows x 24 heads on one card; this is among the fastest.)
                 const float mine = live ? m : -CUDART_INF_F;
                 const bool grow = (mine - ref) * p.scale_log2 > kRescale;
                 if (j == 0) {

@@ -11,7 +11,8 @@ namespace {
 // 32 packed rows against tiles of 64 keys: 128 threads, each with 4 rows x 4 keys of the scores and 4 rows x 8
 // columns of the output in registers; running maximum and sum per row, so scores never leave the chip. Bound by latency:
 // two samples of 64 rows x 6 heads of 64 take 11.6 us (one tile per block: four rounds of loads, then one pass), 2000 rows
-// x 6 heads of 128 run at 14 TFLOP/s.
+// x 6 heads of 128 run at 14 TFLOP/s, and 4 single rows x 24 heads of 128 against 8192 keys take 656 us (1.2 TB/s: a block
+// computes 32 rows of which one is there).
 constexpr int kSimtThreads = 128;
 constexpr int kSimtPitch = SPECA_MAX_HEAD_DIM + 4;  // floats; rows 4 banks apart: 16-byte reads of 8 rows do not collide
 
