@@ -671,6 +671,78 @@ speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_
                                      int64_t o_head_stride, const int32_t* dev_kv_len, const uint8_t* dev_active_mask,
                                      float* dev_lse, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * The block in 8 bits: norms that write 8 bits, rows and weights into 8 bits, and the matrix products between them.
+ *
+ * A matrix in 8 bits holds rows of e4m3 codes and one scale, a power of two, for each SPECA_BLOCK8 consecutive elements of a
+ * row (the last block of a row may be shorter):
+ *   value(r, c) = e4m3(codes[r * code_stride + c]) * 2^(s - 127),
+ *   s = scales[(c / 512) * scale_stride + 4 * r + c / 128 % 4]
+ * so the scale bytes of four blocks of a row lie together, rows of such a group of 512 columns one after another; bytes behind
+ * the last block are neither read nor written. Writing a block takes the smallest power of two 2^(s - 127), 1 <= s <= 254, that brings
+ * its largest finite magnitude to 448 or less (s = 127 for a block of zeros) and rounds the quotients to nearest even.
+ * e4m3 has no infinity: a value that is not finite becomes NaN, and the others of its block keep their scale.
+ */
+#define SPECA_BLOCK8 128 /* elements that share a scale */
+typedef struct {
+    void* codes;          /* device, rows of bytes */
+    int64_t code_stride;  /* bytes between rows */
+    void* scales;         /* device, 4-byte aligned: [ceil(columns / 512)][rows][4] */
+    int64_t scale_stride; /* bytes between groups, a multiple of 4, at least 4 * rows */
+} speca_matrix8_t;
+
+typedef enum { SPECA_NORM_LAYER = 0, SPECA_NORM_RMS = 1 } speca_norm_t;
+/* GELU is the tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))); SILU is x / (1 + exp(-x)). */
+typedef enum { SPECA_ACT_NONE = 0, SPECA_ACT_GELU = 1, SPECA_ACT_SILU = 2 } speca_activation_t;
+
+/*
+ * [rows, dim] of F32 or BF16 into 8 bits: weights, when a model is loaded. Needs no handle, so no mask: all rows are written.
+ *   x       device, row stride in elements;  out: host struct, read before the call returns. Codes and scales may not overlap x.
+ * Rows of a multiple of 8 elements that start on 16 bytes, with codes on 8, take the vector path.
+ * Errors: INVALID_ARG (null, dtype, device), SHAPE, ALIGNMENT, UNSUPPORTED (not an sm_100 device), CUDA.
+ */
+speca_status_t speca_quantize8(int64_t rows, int32_t dim, const void* x, int64_t x_stride, int32_t dtype, const speca_matrix8_t* out,
+                               int32_t device, void* stream);
+
+/* The same for the layer's query rows, in its type and under its mask: activations, such as the attention's output. */
+speca_status_t speca_layer_quantize8(speca_layer_t* layer, int32_t dim, const void* x, int64_t x_stride,
+                                     const uint8_t* dev_active_mask, const speca_matrix8_t* out, void* stream);
+
+/*
+ * Norm over rows of `dim` elements with the residual's addition, into 8 bits:
+ *   x' = x + gate_s * branch             (x' = x when branch is NULL)
+ *   u  = x' / sqrt(mean(x'^2) + norm_eps)                           SPECA_NORM_RMS
+ *   u  = (x' - mean(x')) / sqrt(var(x') + norm_eps)                 SPECA_NORM_LAYER
+ *   out = 8 bits of u * weight * (1 + scale_s) + shift_s, computed from the unrounded x' and rounded once, to its codes
+ * x, branch, gate, scale, shift, x_out: as in speca_layer_modulate. weight: dim elements, or NULL (1). out: host struct, read before
+ * the call returns; its codes and scales may not overlap another tensor.
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT (to the element; scales to 4), CUDA.
+ */
+speca_status_t speca_layer_norm8(speca_layer_t* layer, int32_t kind, int32_t dim, const void* x, int64_t x_stride, const void* branch,
+                                 int64_t branch_stride, const void* gate, const void* scale, const void* shift, int64_t mod_stride,
+                                 const void* weight, const uint8_t* dev_active_mask, void* x_out, int64_t x_out_stride,
+                                 const speca_matrix8_t* out, void* stream);
+
+/*
+ * Product of the layer's query rows with a weight matrix, both in 8 bits, sums in fp32:
+ *   t[i, j] = act(sum_k a[i, k] * w[j, k] + bias[j])
+ *   out[i, j] = residual[i, j] + gate_s[j] * t[i, j]      in the layer's type, or
+ *   out_8bit  = 8 bits of t, a scale for each 128 columns
+ *   a             [rows, k], w: [n, k]; host structs, read before the call returns. Rows of codes start on 16 bytes (address and
+ *                 stride). What lies behind column k of a row, up to the stride, is not used.
+ *   bias          device, n elements of the layer's type, or NULL.  residual: [rows, n] or NULL (0); may be out itself with the
+ *                 same stride.  gate: [n_seqs, n], row stride gate_stride, or NULL (1).
+ *   out, out_8bit exactly one of them; nothing else may overlap the output. residual and gate go with out alone.
+ * Rows of inactive sequences are not written, and tiles of rows that hold no others are not computed. A NaN (code 0x7f or 0xff, or a scale byte
+ * of 255) makes its row or column of the product NaN. Results do not depend on the mask or on the launch: no atomics on values, a fixed
+ * order of sums.
+ * Errors: INVALID_ARG, SHAPE, ALIGNMENT, UNSUPPORTED (a stride of 2^40 bytes or more), CUDA.
+ */
+speca_status_t speca_layer_matmul8(speca_layer_t* layer, int32_t n, int32_t k, const speca_matrix8_t* a, const speca_matrix8_t* w,
+                                   const void* bias, int32_t activation, const void* residual, int64_t residual_stride,
+                                   const void* gate, int64_t gate_stride, const uint8_t* dev_active_mask, void* out,
+                                   int64_t out_stride, const speca_matrix8_t* out_8bit, void* stream);
+
 /* Waits for `stream` and reports (and clears) a bounded wait that a kernel of this layer gave up on, in which
  * case results since the last check are incomplete: CUDA. Errors: INVALID_ARG, CUDA. */
 speca_status_t speca_layer_check(speca_layer_t* layer, void* stream);

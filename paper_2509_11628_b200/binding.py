@@ -27,6 +27,9 @@ SPECA_LAYOUT_TABLES, SPECA_LAYOUT_HISTORY = 0, 1
 SPECA_FEATURE_IN_PLACE = 1   # as feats[entry]: the features already sit in the planes speca_cache_next_slot names
 SPECA_MAX_ORDER, SPECA_MAX_BATCH, SPECA_MAX_ENTRIES, SPECA_MAX_HORIZON = 4, 64, 512, 8
 SPECA_ROPE_INTERLEAVED, SPECA_ROPE_HALVES = 0, 1
+SPECA_NORM_LAYER, SPECA_NORM_RMS = 0, 1
+SPECA_ACT_NONE, SPECA_ACT_GELU, SPECA_ACT_SILU = 0, 1, 2
+SPECA_BLOCK8 = 128
 SPECA_MAX_SEQS, SPECA_MAX_ROWS, SPECA_MAX_HEAD_DIM, SPECA_MAX_GROUP, SPECA_MAX_AXES = 512, (1 << 31) - (1 << 16), 128, 128, 4
 
 EXPORTS = [
@@ -39,6 +42,7 @@ EXPORTS = [
     "speca_forecast_sum", "speca_verify_select",
     "speca_layer_workspace_bytes", "speca_layer_create", "speca_layer_destroy", "speca_layer_modulate", "speca_layer_rope",
     "speca_layer_attention", "speca_layer_check", "speca_layer_last_error",
+    "speca_quantize8", "speca_layer_quantize8", "speca_layer_norm8", "speca_layer_matmul8",
 ]
 
 
@@ -79,6 +83,10 @@ class LayerConfig(ctypes.Structure):
         ("theta", ctypes.c_double), ("pairing", ctypes.c_int32), ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_size_t), ("device", ctypes.c_int32),
     ]
+
+
+class Matrix8Desc(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("code_stride", ctypes.c_int64), ("scales", ctypes.c_void_p), ("scale_stride", ctypes.c_int64)]
 
 
 _LIB = None
@@ -134,6 +142,11 @@ def _lib() -> ctypes.CDLL:
     L.speca_layer_modulate.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp]
     L.speca_layer_rope.argtypes = [vp] + [vp, i64, i64] * 4 + [vp] * 5
     L.speca_layer_attention.argtypes = [vp] + [vp, i64, i64] * 4 + [vp] * 4
+    m8 = ctypes.POINTER(Matrix8Desc)
+    L.speca_quantize8.argtypes = [i64, i32, vp, i64, i32, m8, i32, vp]
+    L.speca_layer_quantize8.argtypes = [vp, i32, vp, i64, vp, m8, vp]
+    L.speca_layer_norm8.argtypes = [vp, i32, i32, vp, i64, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, m8, vp]
+    L.speca_layer_matmul8.argtypes = [vp, i32, i32, m8, m8, vp, i32, vp, i64, vp, i64, vp, vp, i64, m8, vp]
     L.speca_layer_check.argtypes = [vp, vp]
     L.speca_layer_last_error.argtypes = [vp]
     L.speca_layer_last_error.restype = ctypes.c_char_p
@@ -501,6 +514,29 @@ def speca_layer_attention(layer, q, k, v, o, dev_kv_len, dev_active_mask, dev_ls
                                               _stream_ptr(stream)), layer)
 
 
+def speca_quantize8(rows, dim, x, x_stride, dtype, out, device, stream=None) -> None:
+    """``out``: a ``Matrix8Desc``; ``quantize8`` takes tensors."""
+    _check(_lib().speca_quantize8(rows, dim, x, x_stride, dtype, ctypes.byref(out), device, _stream_ptr(stream)))
+
+
+def speca_layer_quantize8(layer, dim, x, x_stride, dev_active_mask, out, stream=None) -> None:
+    _check_layer(_lib().speca_layer_quantize8(layer, dim, x, x_stride, dev_active_mask, ctypes.byref(out), _stream_ptr(stream)), layer)
+
+
+def speca_layer_norm8(layer, kind, dim, x, x_stride, branch, branch_stride, gate, scale, shift, mod_stride, weight, dev_active_mask,
+                      x_out, x_out_stride, out, stream=None) -> None:
+    _check_layer(_lib().speca_layer_norm8(layer, kind, dim, x, x_stride, branch, branch_stride, gate, scale, shift, mod_stride, weight,
+                                          dev_active_mask, x_out, x_out_stride, ctypes.byref(out), _stream_ptr(stream)), layer)
+
+
+def speca_layer_matmul8(layer, n, k, a, w, bias, activation, residual, residual_stride, gate, gate_stride, dev_active_mask, out,
+                        out_stride, out_8bit, stream=None) -> None:
+    """a, w, out_8bit: ``Matrix8Desc`` (out_8bit or out is None); ``SpecaLayer.matmul8`` takes tensors."""
+    _check_layer(_lib().speca_layer_matmul8(layer, n, k, ctypes.byref(a), ctypes.byref(w), bias, activation, residual, residual_stride,
+                                            gate, gate_stride, dev_active_mask, out, out_stride,
+                                            None if out_8bit is None else ctypes.byref(out_8bit), _stream_ptr(stream)), layer)
+
+
 def speca_layer_check(layer, stream=None) -> None:
     _check_layer(_lib().speca_layer_check(layer, _stream_ptr(stream)), layer)
 
@@ -643,6 +679,52 @@ class SpecaCache:
         return self.arena[off: off + n * d * (2 if self.dtype == SPECA_BF16 else 4)].view(tdt).view(n, d)
 
 
+class Matrix8:
+    """A matrix in 8 bits: ``codes`` float8_e4m3fn ``[rows, dim]`` (rows may be strided, the last dimension is dense) and
+    ``scales`` float8_e8m0fnu ``[ceil(dim / 512), rows, 4]``: the scale of column c of row r is ``scales[c // 512, r, c // 128 % 4]``.
+    Rows of codes that start on multiples of 16 bytes, as ``empty`` lays them out, can enter a product."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.float8_e8m0fnu:
+            raise TypeError("codes are float8_e4m3fn and scales float8_e8m0fnu, not %s and %s" % (codes.dtype, scales.dtype))
+        if codes.dim() != 2 or scales.shape != (-(-codes.shape[1] // (4 * SPECA_BLOCK8)), codes.shape[0], 4):
+            raise ValueError("codes %s and scales %s do not go together" % (tuple(codes.shape), tuple(scales.shape)))
+        if codes.device != scales.device:
+            raise TypeError("codes on %s, scales on %s" % (codes.device, scales.device))
+        rows, dim = codes.shape
+        if (dim > 1 and codes.stride(1) != 1) or (rows > 0 and scales.shape[0] > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 4))):
+            raise TypeError("the last dimension of codes, and the last two of scales, must be dense")
+        self.codes, self.scales, self.shape, self.device = codes, scales, codes.shape, codes.device
+        self.index = codes.get_device()
+        self.desc = Matrix8Desc(codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0))
+
+    @classmethod
+    def empty(cls, rows: int, dim: int, device="cuda:0") -> "Matrix8":
+        """Zeros, with rows of codes a multiple of 16 bytes apart."""
+        codes = torch.zeros(rows, -(-dim // 16) * 16, dtype=torch.uint8, device=device)[:, :dim].view(torch.float8_e4m3fn)
+        scales = torch.zeros(-(-dim // (4 * SPECA_BLOCK8)), rows, 4, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu)
+        return cls(codes, scales)
+
+
+def quantize8(x: torch.Tensor, out: Optional[Matrix8] = None, stream=None) -> Matrix8:
+    """Weights ``[rows, dim]`` (fp32 or bf16, on a GPU) into 8 bits."""
+    dtype = {t: code for code, t in _TORCH_DTYPES.items()}.get(x.dtype)
+    if dtype is None:
+        raise TypeError("fp32 or bf16 is expected, not %s" % x.dtype)
+    if not x.is_cuda:
+        raise TypeError("a tensor on a GPU is expected")
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("a matrix with a dense last dimension is expected")
+    out = Matrix8.empty(*x.shape, x.device) if out is None else out
+    if out.shape != x.shape:
+        raise ValueError("out: shape %s is expected, not %s" % (tuple(x.shape), tuple(out.shape)))
+    if out.index != x.get_device():
+        raise TypeError("out: a matrix on %s is expected" % x.device)
+    speca_quantize8(x.shape[0], x.shape[1], x.data_ptr(), x.stride(0), dtype, out.desc, out.index,
+                    torch._C._cuda_getCurrentRawStream(out.index) if stream is None else stream)
+    return out
+
+
 class SpecaLayer:
     """The parts of a verification layer that are not plain matrix products, over packed sequences: sequence s of a
     ``[rows, ...]`` tensor is rows ``q_start[s]`` to ``q_start[s + 1] - 1``. Owns the workspace and the handle. Tensors
@@ -708,23 +790,28 @@ class SpecaLayer:
         """The stream's address; of the device's current stream without the Stream object around it (2 us a call)."""
         return torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream
 
-    def modulate(self, x, y, branch=None, gate=None, scale=None, shift=None, x_out=None, active=None, stream=None):
-        """x' = x + gate * branch; y = layer norm of x' * (1 + scale) + shift, the modulations by sequence."""
-        dim, dt = x.shape[-1], self.torch_dtype
-        shape, mod_shape = (self.rows, dim), (self.n_seqs, dim)
-        px, sx = self._tensor(x, "x", shape, dt)
-        py, sy = self._tensor(y, "y", shape, dt)
-        pb, sb = (None, (0,)) if branch is None else self._tensor(branch, "branch", shape, dt)
-        po, so = (None, (0,)) if x_out is None else self._tensor(x_out, "x_out", shape, dt)
+    def _modulations(self, tensors, dim):
+        """Addresses of gate, scale and shift ([n_seqs, dim] or None) and their one row stride."""
         mods, mod_stride = [None, None, None], None
-        for i, m in enumerate((gate, scale, shift)):
+        for i, m in enumerate(tensors):
             if m is not None:
-                mods[i], s = self._tensor(m, ("gate", "scale", "shift")[i], mod_shape, dt)
+                mods[i], s = self._tensor(m, ("gate", "scale", "shift")[i], (self.n_seqs, dim), self.torch_dtype)
                 if mod_stride is None:
                     mod_stride = s[0]
                 elif s[0] != mod_stride and self.n_seqs > 1:
                     raise ValueError("gate, scale and shift must share one row stride")
-        speca_layer_modulate(self.handle, dim, px, sx[0], pb, sb[0], mods[0], mods[1], mods[2], mod_stride or 0,
+        return mods, mod_stride or 0
+
+    def modulate(self, x, y, branch=None, gate=None, scale=None, shift=None, x_out=None, active=None, stream=None):
+        """x' = x + gate * branch; y = layer norm of x' * (1 + scale) + shift, the modulations by sequence."""
+        dim, dt = x.shape[-1], self.torch_dtype
+        shape = (self.rows, dim)
+        px, sx = self._tensor(x, "x", shape, dt)
+        py, sy = self._tensor(y, "y", shape, dt)
+        pb, sb = (None, (0,)) if branch is None else self._tensor(branch, "branch", shape, dt)
+        po, so = (None, (0,)) if x_out is None else self._tensor(x_out, "x_out", shape, dt)
+        mods, mod_stride = self._modulations((gate, scale, shift), dim)
+        speca_layer_modulate(self.handle, dim, px, sx[0], pb, sb[0], mods[0], mods[1], mods[2], mod_stride,
                              self._vector(active, "active", self.n_seqs, torch.uint8), po, so[0], py, sy[0], self._stream(stream))
 
     def rope(self, q, q_out, k, k_out, positions, q_weight=None, k_weight=None, active=None, stream=None):
@@ -750,6 +837,50 @@ class SpecaLayer:
             self.handle, self._heads(q, "q", self.q_shape), self._heads(k, "k", self.k_shape), self._heads(v, "v", self.k_shape),
             self._heads(out, "out", self.q_shape), self._vector(kv_len, "kv_len", self.n_seqs, torch.int32),
             self._vector(active, "active", self.n_seqs, torch.uint8), p_lse, self._stream(stream))
+
+    def _matrix8(self, m, name, shape):
+        if not isinstance(m, Matrix8):
+            raise TypeError("%s: a Matrix8 is expected" % name)
+        if m.index != self.index:
+            raise TypeError("%s: a matrix on %s is expected" % (name, self.device))
+        if m.shape != shape:
+            raise ValueError("%s: shape %s is expected, not %s" % (name, tuple(shape), tuple(m.shape)))
+        return m.desc
+
+    def quantize8(self, x, out, active=None, stream=None):
+        """The rows of x in 8 bits."""
+        shape = (self.rows, x.shape[-1])
+        px, sx = self._tensor(x, "x", shape, self.torch_dtype)
+        speca_layer_quantize8(self.handle, shape[1], px, sx[0], self._vector(active, "active", self.n_seqs, torch.uint8),
+                              self._matrix8(out, "out", shape), self._stream(stream))
+
+    def norm8(self, x, out, kind=SPECA_NORM_RMS, branch=None, gate=None, scale=None, shift=None, weight=None, x_out=None, active=None,
+              stream=None):
+        """x' = x + gate * branch; out = 8 bits of norm(x') * weight * (1 + scale) + shift, the modulations by sequence."""
+        dim, dt = x.shape[-1], self.torch_dtype
+        shape = (self.rows, dim)
+        px, sx = self._tensor(x, "x", shape, dt)
+        pb, sb = (None, (0,)) if branch is None else self._tensor(branch, "branch", shape, dt)
+        po, so = (None, (0,)) if x_out is None else self._tensor(x_out, "x_out", shape, dt)
+        mods, mod_stride = self._modulations((gate, scale, shift), dim)
+        speca_layer_norm8(self.handle, kind, dim, px, sx[0], pb, sb[0], *mods, mod_stride, self._vector(weight, "weight", dim, dt),
+                          self._vector(active, "active", self.n_seqs, torch.uint8), po, so[0], self._matrix8(out, "out", shape),
+                          self._stream(stream))
+
+    def matmul8(self, a, w, out, bias=None, activation=SPECA_ACT_NONE, residual=None, gate=None, active=None, stream=None):
+        """out = residual + gate * act(a w^T + bias), the gate by sequence; ``out``: a tensor of the layer's type, or a Matrix8 (which
+        takes no residual and no gate)."""
+        if not isinstance(w, Matrix8):
+            raise TypeError("w: a Matrix8 is expected")
+        (n, k), dt = w.shape, self.torch_dtype
+        shape = (self.rows, n)
+        da, dw = self._matrix8(a, "a", (self.rows, k)), self._matrix8(w, "w", w.shape)
+        eight = self._matrix8(out, "out", shape) if isinstance(out, Matrix8) else None
+        po, so = (None, (0,)) if eight is not None else self._tensor(out, "out", shape, dt)
+        pr, sr = (None, (0,)) if residual is None else self._tensor(residual, "residual", shape, dt)
+        pg, sg = (None, (0,)) if gate is None else self._tensor(gate, "gate", (self.n_seqs, n), dt)
+        speca_layer_matmul8(self.handle, n, k, da, dw, self._vector(bias, "bias", n, dt), activation, pr, sr[0], pg, sg[0],
+                            self._vector(active, "active", self.n_seqs, torch.uint8), po, so[0], eight, self._stream(stream))
 
     def check(self, stream=None):
         """Waits for `stream` and raises if a kernel of this layer gave up on a bounded wait."""

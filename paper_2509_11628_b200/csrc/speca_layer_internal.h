@@ -96,4 +96,44 @@ cudaError_t launch_attention_join(const AttnParams& p, int dtype, cudaStream_t s
 // sums divide by (the same, but for the rounding of the largest weights to bf16).
 __host__ __device__ constexpr int64_t part_row_floats(int head_dim) { return (head_dim + 3) / 4 * 4 + 4; }
 
+// ---- 8-bit operators ----------------------------------------------------------------------------
+// Rows of e4m3 codes with one scale 2^(byte - 127) for each 128 elements; the bytes of four blocks of a row lie together, the
+// rows of such a group one after another.
+constexpr int kBlock8 = SPECA_BLOCK8;
+struct Out8 {
+    uint8_t *codes, *scales;
+    int64_t code_stride, scale_stride;  // bytes between rows of codes, between groups of scales
+};
+
+struct Norm8Params {
+    const uint16_t* row_seq;  // NULL: rows of no sequence, all of them live
+    const uint8_t* dev_mask;
+    const char *x, *branch, *gate, *scale, *shift, *weight;
+    char* x_out;
+    Out8 out;
+    int64_t x_stride, branch_stride, mod_stride, x_out_stride;  // elements
+    int32_t rows, dim;
+    int32_t norm;  // 0: none, the rows as they are
+    int32_t centre;  // the mean is taken off
+    float eps;
+};
+// `vectors`: rows of a multiple of 8 elements that start on 16 bytes everywhere, and codes on 8
+cudaError_t launch_norm8(const Norm8Params& p, int dtype, bool vectors, cudaStream_t stream);
+
+struct Matmul8Params {
+    const uint16_t* row_seq;
+    const uint8_t* dev_mask;
+    const uint8_t *a, *w, *a_scales, *w_scales;
+    int64_t a_stride, w_stride, a_scale_stride, w_scale_stride;  // bytes
+    int32_t m, n, k;
+    const char *bias, *residual, *gate;
+    char* out;  // NULL: to out8
+    Out8 out8;
+    int64_t residual_stride, gate_stride, out_stride;  // elements
+    int32_t act;
+    int32_t vectors;  // bias, residual, gate and out (or the codes) take four elements at once
+    uint32_t* gave_up;
+};
+cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
+
 }  // namespace speca
