@@ -22,9 +22,8 @@
 // 20926 rows 4.76 to 5.09 ms (1.05 to 1.12). Tried and not kept, 4608 rows on one card, all under an earlier softmax: 64-key
 // tiles with the scores double buffered 238 us, the same with two warpgroups taking turns at the tiles 245, one score buffer
 // and P beside it 240 to 265, against 221 of this form.
-#include <cuda.h>
-
 #include "speca_attention_common.cuh"
+#include "speca_tc.cuh"
 
 namespace speca {
 namespace {
@@ -38,7 +37,6 @@ constexpr int kLoadWarp = 8, kIssueWarp = 9;
 constexpr int kBlockRows = 128;
 constexpr int kTileKeys = 128;
 constexpr uint32_t kPanelBytes = 128 * 128;  // 128 rows of 64 bf16: one 128-byte swizzle span per row
-constexpr uint32_t kSpinLimit = 1u << 18;    // polls of one wait (each sleeps up to 1.5 us); a healthy wait needs a few
 constexpr float kRescale = 8.f;              // log2 growth of a row's maximum that is left in P
 constexpr uint32_t kTmemCols = 512;          // S_0, S_1 (P over them), O_0, O_1: 128 columns each
 
@@ -57,56 +55,6 @@ constexpr uint32_t smem_bytes(int panels) {
 }
 static_assert(smem_bytes(2) <= 232448 && smem_bytes(1) > 116224, "fits one SM, and no two blocks share one (tensor memory)");
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
-__device__ __forceinline__ void bar_init(uint64_t* bar, uint32_t count) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-__device__ __forceinline__ void bar_arrive(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-// False when the phase did not complete within the limit. One thread waits.
-__device__ __forceinline__ bool bar_wait(uint64_t* bar, uint32_t parity) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
-        if (bar_try(bar, parity)) return true;
-    return false;
-}
-// The same for a whole warp, whose lanes all get one answer. The lanes may wait for different barriers: a wait that is
-// already satisfied takes 100 to 250 cycles to say so, several at once no more.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin)
-        if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
-    return false;
-}
-// True in one lane of the converged warp. Unlike a comparison with a lane index it tells the compiler that one thread
-// is left, so the operands of the tensor instructions behind it go to uniform registers without a loop over lanes
-// (which cost 125 cycles an instruction).
-__device__ __forceinline__ bool elect_one() {
-    uint32_t yes;
-    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
-    return yes != 0;
-}
-template <int N>
-__device__ __forceinline__ void more_registers() {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ __forceinline__ void fewer_registers() {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -114,9 +62,6 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
         : "memory");
 }
 
-// ---- tcgen05 ------------------------------------------------------------------------------------
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -143,45 +88,6 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
         "l"(b), "r"(desc), "r"(accumulate)
         : "memory");
 }
-
-#define SPECA_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
-#define SPECA_I8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
-// 32 columns of this thread's lane (row).
-__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t* x) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
-        "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : SPECA_R8(x, 0), SPECA_R8(x, 8), SPECA_R8(x, 16), SPECA_R8(x, 24)
-        : "r"(addr));
-}
-__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* x) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
-        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::SPECA_I8(x, 0),
-        SPECA_I8(x, 8), SPECA_I8(x, 16), SPECA_I8(x, 24), "r"(addr)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t* x) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : SPECA_R8(x, 0), SPECA_R8(x, 8)
-        : "r"(addr));
-}
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* x) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::SPECA_I8(x, 0),
-        SPECA_I8(x, 8), "r"(addr)
-        : "memory");
-}
-// Waits for this warp's loads; the registers they fill pass through, so that no use is scheduled in front of the wait.
-#define SPECA_P8(x, i) "+r"(x[i]), "+r"(x[i + 1]), "+r"(x[i + 2]), "+r"(x[i + 3]), "+r"(x[i + 4]), "+r"(x[i + 5]), "+r"(x[i + 6]), "+r"(x[i + 7])
-template <int N>
-__device__ __forceinline__ void tmem_wait_load(uint32_t* x) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < N; i += 8) asm volatile("" : SPECA_P8(x, i));
-}
-__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -706,22 +612,6 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
     }
-}
-
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encoder() {
-    static const EncodeTiled fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult res;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &res) != cudaSuccess ||
-            res != cudaDriverEntryPointSuccess)
-            f = nullptr;
-        return reinterpret_cast<EncodeTiled>(f);
-    }();
-    return fn;
 }
 
 // [rows, heads, head_dim] as boxes of 64 columns x box_heads x box_rows, columns behind head_dim and rows behind

@@ -1,0 +1,634 @@
+// Matrix products in 8 bits on the tensor cores: D = A W^T, e4m3 with a power of two as scale per row and 128 elements of k.
+//
+// The scales go with the operands into the tensor cores (block-scaled tcgen05.mma), so sums over all of k stay in tensor memory in
+// fp32. A tile is 128 rows times CG by NT features; with CG = 2 the two SMs of a cluster share it: each holds its 128 rows of A, half of
+// the rows of W and its half of the sums, which halves what every SM reads of W. Blocks are persistent over tiles:
+//   warps 0-3, 4-7   epilogue of the left and the right half of the columns: one thread per row, its sums in registers
+//   warp 8           TMA loads of A and W, 128 elements of k a stage
+//   warp 9           issues the products (of both SMs, in the first of them)
+//   warp 10          scales: of 512 elements of k at once, from memory through registers into the order that the tensor memory takes
+// Sums alternate between two places in tensor memory, so that the epilogue of a tile runs beside the products of the next.
+// Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
+#include "speca_matmul8_common.cuh"
+#include "speca_tc.cuh"
+
+namespace speca {
+namespace {
+
+// Three warpgroups of 168 registers a thread at launch; the epilogue's two take 216 (half a row of sums stays in registers), the third
+// gives up what they take: 2 x 216 + 72 = 3 x 168.
+constexpr int kThreads = 384;
+constexpr int kLoadWarp = 8, kIssueWarp = 9, kScaleWarp = 10;
+constexpr int kRows = 128;                       // rows of a tile in one SM
+constexpr uint32_t kTmemCols = 512;
+constexpr int kScaleCol = 480;                   // two stages of 16 columns: 4 for A's scales, up to 8 for W's
+constexpr int kMaxTilesM = 2048;                 // tiles of rows of one launch, listed in shared memory where there is a mask
+constexpr int kGroupM = 8;                       // tiles of rows that run beside each other share their features in L2
+
+template <int CG, int NT>
+struct Shape {
+    static constexpr int kTileM = kRows * CG;
+    static constexpr int kRowsW = NT / CG;       // rows of W that one SM holds
+    static constexpr uint32_t kBytesA = kRows * 128, kBytesW = kRowsW * 128, kStage = kBytesA + kBytesW;
+    static constexpr int kPartsW = (NT + 127) / 128;
+    static constexpr uint32_t kScaleBytes = 512 * (1 + kPartsW);
+    static constexpr int kStages = kStage <= 24576 ? 8 : kStage <= 28672 ? 7 : kStage <= 32768 ? 6 : 4;
+    static constexpr int kCols = NT / 2;         // columns of one epilogue thread
+    // place of the second sums: behind the first, or as far behind as the scales leave room
+    static constexpr int kSecond = NT <= kScaleCol - NT ? NT : kScaleCol - NT;
+    static constexpr bool kOverlap = kSecond < NT;
+};
+
+template <int CG, int NT>
+struct Smem {
+    using S = Shape<CG, NT>;
+    uint8_t tiles[S::kStages][S::kStage];
+    uint8_t scales[2][S::kScaleBytes];
+    uint64_t full[S::kStages], empty[S::kStages];
+    uint64_t scales_full[2], scales_empty[2];
+    uint64_t sums_full[2], sums_free[2], overlap_free[2];
+    uint64_t tops[2], drain;
+    float top[2][2][kRows];
+    uint32_t tmem, abort, n_live;
+    uint32_t warp_count[kThreads / 32];
+    uint16_t live[kMaxTilesM];
+};
+
+// ---- the pair of SMs ----------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The first SM's barrier of this name.
+template <int CG>
+__device__ __forceinline__ uint32_t leaders(uint64_t* bar) {
+    uint32_t a = smem_u32(bar);
+    if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
+    return a;
+}
+template <int CG>
+__device__ __forceinline__ void arrive_at_leader(uint64_t* bar) {
+    if constexpr (CG == 1)
+        bar_arrive(bar);
+    else
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders<CG>(bar)) : "memory");
+}
+// A whole warp waits, for arrivals from both SMs.
+template <int CG>
+__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity) {
+    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+        uint32_t ok;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (__all_sync(0xffffffffu, ok != 0)) return true;
+    }
+    return false;
+}
+
+// ---- tensor cores -------------------------------------------------------------------------------
+template <int CG>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                dst),
+            "l"(map), "r"(x), "r"(y), "r"(bar)
+            : "memory");
+}
+// Arrives, when all products so far are done, at the barrier of this name in every SM of the tile.
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
+                     "h"(static_cast<uint16_t>(3))
+                     : "memory");
+}
+// 32 rows of 16 bytes into 4 columns of every quarter of the lanes: the scales of 128 rows.
+template <int CG>
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
+    // no swizzle, groups of 8 rows (128 bytes) one after another
+    const uint64_t desc = static_cast<uint64_t>((smem >> 4) & 0x3fff) | uint64_t(8) << 16 | uint64_t(8) << 32 | uint64_t(1) << 46;
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else
+        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// 128 bytes of k a row, with the 128-byte swizzle: 1024 bytes between groups of 8 rows.
+__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
+    return static_cast<uint64_t>((addr >> 4) & 0x3fff) | uint64_t(1) << 16 | uint64_t(64) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+// e4m3 x e4m3 -> fp32, scales of 8-bit exponents. The scale of block i (0 .. 3) is byte i of a column.
+template <int CG, int NT>
+__host__ __device__ constexpr uint32_t mma_desc8(uint32_t i) {
+    return i << 4 | static_cast<uint32_t>(NT >> 3) << 17 | 1u << 23 | static_cast<uint32_t>(kRows * CG >> 4) << 24 | i << 29;
+}
+template <int CG>
+__device__ __forceinline__ void mma8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
+    if constexpr (CG == 1)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(desc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+            "l"(a), "l"(b), "r"(desc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
+            : "memory");
+}
+
+// ---- tiles --------------------------------------------------------------------------------------
+struct Part {  // what one launch covers
+    int m_begin, n_begin;   // first row, first feature
+    int m_tiles, n_tiles;
+};
+struct Place {
+    int m, n;  // first row (of the pair) and feature of a tile
+};
+template <int CG, int NT>
+__device__ __forceinline__ Place place(const Part& part, const Smem<CG, NT>& sm, bool masked, int m_tiles, int i) {
+    const int per = kGroupM * part.n_tiles, g = i / per, in = i - g * per;
+    const int rows = min(kGroupM, m_tiles - g * kGroupM);
+    int m = g * kGroupM + in % rows;
+    if (masked) m = sm.live[m];
+    return Place{part.m_begin + m * Shape<CG, NT>::kTileM, part.n_begin + in / rows * NT};
+}
+// Whether any row of the tile belongs to an active sequence.
+__device__ __forceinline__ bool tile_live(const Matmul8Params& p, int first, int rows) {
+    const int last = min(first + rows, p.m) - 1;
+    for (int s = p.row_seq[first]; s <= p.row_seq[last]; ++s)
+        if (p.dev_mask[s] != 0) return true;
+    return false;
+}
+
+// ---- epilogue of one thread: `C` columns of a row ----
+template <typename T>
+__device__ __forceinline__ void load_eight(const char* base, int64_t row, int64_t stride, int c, int n, bool vectors, float (&out)[8]) {
+    const T* from = reinterpret_cast<const T*>(base) + row * stride + c;
+    if (vectors && c + 8 <= n) {
+        constexpr int E = 16 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < 8; i += E) {
+            const Pack<T, E> v = *reinterpret_cast<const Pack<T, E>*>(from + i);
+#pragma unroll
+            for (int e = 0; e < E; ++e) out[i + e] = to_float(v.e[e]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = c + e < n ? to_float(from[e]) : 0.f;
+}
+
+// Bias and activation, in place; zeros behind the last column.
+template <int DT, int C>
+__device__ __forceinline__ void finish_sums(const Matmul8Params& p, int n0, float (&v)[C]) {
+    using T = typename Type<DT>::T;
+#pragma unroll
+    for (int i = 0; i < C; i += 8) {
+        if (p.bias != nullptr) {
+            float b[8];
+            load_eight<T>(p.bias, 0, 0, n0 + i, p.n, p.vectors, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i + e] += b[e];
+        }
+        if (p.act != SPECA_ACT_NONE) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i + e] = activate(v[i + e], p.act);
+        }
+    }
+    if (n0 + C > p.n) {
+#pragma unroll
+        for (int i = 0; i < C; ++i) v[i] = n0 + i < p.n ? v[i] : 0.f;
+    }
+}
+
+template <int DT, int C>
+__device__ __forceinline__ void write_row(const Matmul8Params& p, int row, int seq, int n0, const float (&v)[C]) {
+    using T = typename Type<DT>::T;
+    T* out = reinterpret_cast<T*>(p.out) + row * p.out_stride;
+#pragma unroll
+    for (int i = 0; i < C; i += 8) {
+        const int c = n0 + i;
+        if (c >= p.n) break;
+        float t[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = v[i + e];
+        if (p.gate != nullptr) {
+            float g[8];
+            load_eight<T>(p.gate, seq, p.gate_stride, c, p.n, p.vectors, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] *= g[e];
+        }
+        if (p.residual != nullptr) {
+            float r[8];
+            load_eight<T>(p.residual, row, p.residual_stride, c, p.n, p.vectors, r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] += r[e];
+        }
+        if (p.vectors && c + 8 <= p.n) {
+            constexpr int E = 16 / sizeof(T);
+#pragma unroll
+            for (int k = 0; k < 8; k += E) {
+                Pack<T, E> o;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o.e[e] = from_float<T>(t[k + e]);
+                *reinterpret_cast<Pack<T, E>*>(out + c + k) = o;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (c + e < p.n) out[c + e] = from_float<T>(t[e]);
+        }
+    }
+}
+
+// Largest finite magnitude; infinities become NaN.
+template <int C>
+__device__ __forceinline__ float row_top(float (&v)[C]) {
+    const float inf = __uint_as_float(0x7f800000u);
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) top = fmaxf(top, fabsf(v[i]));
+    if (top == inf) {
+        top = 0.f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            if (fabsf(v[i]) == inf) v[i] = __uint_as_float(0x7fffffffu);
+            top = fmaxf(top, fabsf(v[i]));
+        }
+    }
+    return top;
+}
+
+template <int C>
+__device__ __forceinline__ void write_codes(const Matmul8Params& p, int row, int n0, float inv, const float (&v)[C]) {
+    uint8_t* to = p.out8.codes + row * p.out8.code_stride;
+#pragma unroll
+    for (int i = 0; i < C; i += 16) {
+        const int c = n0 + i;
+        if (c >= p.n) break;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            w[k] = pack_e4m3(v[i + 4 * k] * inv, v[i + 4 * k + 1] * inv, v[i + 4 * k + 2] * inv, v[i + 4 * k + 3] * inv);
+        if (p.vectors && c + 16 <= p.n) {
+            *reinterpret_cast<uint4*>(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (c + e < p.n) to[c + e] = static_cast<uint8_t>(w[e / 4] >> 8 * (e % 4));
+        }
+    }
+}
+
+// ---- the kernel ---------------------------------------------------------------------------------
+template <int DT, int CG, int NT>
+__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
+    matmul8_tc_kernel(const __grid_constant__ Matmul8Params p, const __grid_constant__ Part part, const __grid_constant__ CUtensorMap map_a,
+                      const __grid_constant__ CUtensorMap map_w) {
+    using S = Shape<CG, NT>;
+    extern __shared__ __align__(1024) char raw[];
+    Smem<CG, NT>& sm = *reinterpret_cast<Smem<CG, NT>*>(raw);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = CG == 1 ? 0 : cluster_rank();
+    const bool masked = p.dev_mask != nullptr;
+
+    if (smem_u32(raw) % 1024 != 0) {  // the swizzled tiles rely on it; the same in both SMs
+        if (threadIdx.x == 0) atomicExch(p.gave_up, 1u);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kStages; ++i) {
+            bar_init(&sm.full[i], 1);
+            bar_init(&sm.empty[i], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(&sm.scales_full[b], CG);
+            bar_init(&sm.scales_empty[b], 1);
+            bar_init(&sm.sums_full[b], 1);
+            bar_init(&sm.sums_free[b], 8 * CG);     // one arrival per warp
+            bar_init(&sm.overlap_free[b], 4 * CG);
+            bar_init(&sm.tops[b], 8);
+        }
+        bar_init(&sm.drain, 1);
+        sm.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kLoadWarp) {
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        }
+    }
+    // the tiles of rows that hold an active sequence, in order
+    int m_tiles = part.m_tiles;
+    if (masked) {
+        m_tiles = 0;
+        for (int first = 0; first < part.m_tiles; first += kThreads) {
+            const int i = first + threadIdx.x;
+            const bool live = i < part.m_tiles && tile_live(p, part.m_begin + i * S::kTileM, S::kTileM);
+            const uint32_t votes = __ballot_sync(0xffffffffu, live);
+            if (lane == 0) sm.warp_count[warp] = __popc(votes);
+            __syncthreads();
+            int before = m_tiles, all = 0;
+            for (int k = 0; k < kThreads / 32; ++k) {
+                const int n = sm.warp_count[k];
+                if (k < warp) before += n;
+                all += n;
+            }
+            if (live) sm.live[before + __popc(votes & ((1u << lane) - 1))] = static_cast<uint16_t>(i);
+            m_tiles += all;
+            __syncthreads();
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();  // the other SM's barriers are there
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&sm.tmem);
+    const int n_tiles = m_tiles * part.n_tiles, first_tile = blockIdx.x / CG, step = gridDim.x / CG;
+    const int k_blocks = (p.k + kBlock8 - 1) / kBlock8;
+
+    if (warp >= kLoadWarp) fewer_registers<72>();
+    if (warp == kLoadWarp) {
+        // ---- loads: one thread ----
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int i = first_tile; i < n_tiles && ok; i += step) {
+                const Place at = place<CG, NT>(part, sm, masked, m_tiles, i);
+                for (int k = 0; k < k_blocks; ++k) {
+                    ok = bar_wait(&sm.empty[stage], phase ^ 1);
+                    if (!ok) break;
+                    if (rank == 0) bar_expect(&sm.full[stage], CG * S::kStage);
+                    const uint32_t bar = leaders<CG>(&sm.full[stage]), to = smem_u32(sm.tiles[stage]);
+                    load_tile<CG>(to, &map_a, k * kBlock8, at.m + rank * kRows, bar);
+                    load_tile<CG>(to + S::kBytesA, &map_w, k * kBlock8, at.n + rank * S::kRowsW, bar);
+                    if (++stage == S::kStages) stage = 0, phase ^= 1;
+                }
+            }
+            if (!ok) {
+                sm.abort = 1;
+                // copies in flight must land before the block gives its shared memory back
+                if (rank == 0)
+                    for (int i = 0; i < S::kStages; ++i) bar_wait(&sm.full[i], i < stage ? phase : phase ^ 1);
+                else
+                    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+            }
+        }
+    } else if (warp == kIssueWarp) {
+        // ---- products: one thread of the first SM ----
+        if (rank == 0) {
+            int stage = 0, b = 0, scale_stage = 0;
+            uint32_t phase = 0, scale_phase = 0, free_phase[2] = {1, 1}, overlap_phase[2] = {0, 0};
+            bool ok = true;
+            for (int i = first_tile; i < n_tiles && ok; i += step) {
+                ok = pair_wait<CG>(&sm.sums_free[b], free_phase[b]);
+                free_phase[b] ^= 1;
+                if (S::kOverlap && i != first_tile && ok) {
+                    ok = pair_wait<CG>(&sm.overlap_free[b ^ 1], overlap_phase[b ^ 1]);
+                    overlap_phase[b ^ 1] ^= 1;
+                }
+                tc_fence_after();
+                const uint32_t sums = tmem + b * S::kSecond;
+                for (int k = 0; k < k_blocks && ok; ++k) {
+                    const uint32_t scales = tmem + kScaleCol + scale_stage * 16;
+                    if (k % 4 == 0) {
+                        ok = pair_wait<CG>(&sm.scales_full[scale_stage], scale_phase);
+                        if (!ok) break;
+                        if (elect_one()) {
+                            const uint32_t from = smem_u32(sm.scales[scale_stage]);
+                            copy_scales<CG>(scales, from);
+#pragma unroll
+                            for (int q = 0; q < S::kPartsW; ++q) copy_scales<CG>(scales + 4 + 4 * q, from + 512 + 512 * q);
+                        }
+                        __syncwarp();
+                    }
+                    ok = pair_wait<CG>(&sm.full[stage], phase);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t from = smem_u32(sm.tiles[stage]);
+                        const uint64_t a = tile_desc(from), w = tile_desc(from + S::kBytesA);
+                        const uint32_t desc = mma_desc8<CG, NT>(0) | static_cast<uint32_t>(k % 4) << 4 | static_cast<uint32_t>(k % 4) << 29;
+#pragma unroll
+                        for (int s = 0; s < 4; ++s) mma8<CG>(sums, a + 2 * s, w + 2 * s, desc, scales, scales + 4, k > 0 || s > 0);
+                        commit<CG>(&sm.empty[stage]);
+                        if (k % 4 == 3 || k + 1 == k_blocks) commit<CG>(&sm.scales_empty[scale_stage]);
+                        if (k + 1 == k_blocks) commit<CG>(&sm.sums_full[b]);
+                    }
+                    __syncwarp();
+                    if (++stage == S::kStages) stage = 0, phase ^= 1;
+                    if (k % 4 == 3 || k + 1 == k_blocks)
+                        if (++scale_stage == 2) scale_stage = 0, scale_phase ^= 1;
+                }
+                b ^= 1;
+            }
+            if (!ok) {
+                sm.abort = 1;
+                if (elect_one()) commit<CG>(&sm.drain);  // products in flight must end before tensor memory is given back
+                __syncwarp();
+                warp_wait(&sm.drain, 0);
+            }
+        }
+    } else if (warp == kScaleWarp) {
+        // ---- scales: lane i takes rows i, 32 + i, ... of a part of 128 rows ----
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int i = first_tile; i < n_tiles && ok; i += step) {
+            const Place at = place<CG, NT>(part, sm, masked, m_tiles, i);
+            const int a0 = at.m + rank * kRows + lane, w0 = at.n + lane;
+            for (int k = 0; k < k_blocks && ok; k += 4) {
+                uint32_t word[4 * (1 + S::kPartsW)];
+                const uint8_t *sa = p.a_scales + k / 4 * p.a_scale_stride, *sw = p.w_scales + k / 4 * p.w_scale_stride;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    word[j] = a0 + 32 * j < p.m ? __ldg(reinterpret_cast<const uint32_t*>(sa) + a0 + 32 * j) : 0x7f7f7f7fu;
+#pragma unroll
+                for (int j = 0; j < 4 * S::kPartsW; ++j)
+                    word[4 + j] = w0 + 32 * j < p.n ? __ldg(reinterpret_cast<const uint32_t*>(sw) + w0 + 32 * j) : 0x7f7f7f7fu;
+                ok = warp_wait(&sm.scales_empty[stage], phase ^ 1);
+                if (!ok) break;
+                uint4* to = reinterpret_cast<uint4*>(sm.scales[stage]) + lane;
+#pragma unroll
+                for (int q = 0; q < 1 + S::kPartsW; ++q) to[32 * q] = make_uint4(word[4 * q], word[4 * q + 1], word[4 * q + 2], word[4 * q + 3]);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_at_leader<CG>(&sm.scales_full[stage]);
+                if (++stage == 2) stage = 0, phase ^= 1;
+            }
+        }
+        if (!ok) sm.abort = 1;
+    } else if (warp < kLoadWarp) {
+        // ---- epilogue ----
+        more_registers<216>();
+        const int half = warp / 4, r = threadIdx.x % 128;
+        const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
+        int b = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int i = first_tile; i < n_tiles; i += step) {
+            const Place at = place<CG, NT>(part, sm, masked, m_tiles, i);
+            ok = warp_wait(&sm.sums_full[b], phase);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t from = tmem + lanes + b * S::kSecond + half * S::kCols;
+            uint32_t bits[S::kCols];
+            if constexpr (S::kOverlap) {
+                // first the columns that the next tile's sums will take: the last 32 of the first place, the first 32 of the second
+                static_assert(NT - S::kSecond == 32 && S::kCols == 128, "one load");
+                if (half != b) {
+                    const int c = b == 0 ? 96 : 0;
+                    uint32_t head[32];
+                    tmem_load32(from + c, head);
+                    tmem_wait_load<32>(head);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_at_leader<CG>(&sm.overlap_free[b]);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        if (b == 0) bits[96 + e] = head[e]; else bits[e] = head[e];
+                    }
+                    if (b == 0) {
+#pragma unroll
+                        for (int k = 0; k < 96; k += 32) tmem_load32(from + k, bits + k);
+                    } else {
+#pragma unroll
+                        for (int k = 32; k < 128; k += 32) tmem_load32(from + k, bits + k);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 128; k += 32) tmem_load32(from + k, bits + k);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < S::kCols; k += 32) tmem_load32(from + k, bits + k);
+            }
+            tmem_wait_load<S::kCols>(bits);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at_leader<CG>(&sm.sums_free[b]);
+
+            const int row = at.m + rank * kRows + r, n0 = at.n + half * S::kCols;
+            bool live = row < p.m;
+            int seq = 0;
+            if (live) {
+                seq = p.row_seq[row];
+                live = !masked || p.dev_mask[seq] != 0;
+            }
+            float v[S::kCols];
+#pragma unroll
+            for (int e = 0; e < S::kCols; ++e) v[e] = __uint_as_float(bits[e]);
+            finish_sums<DT, S::kCols>(p, n0, v);
+            if (p.out != nullptr) {
+                if (live) write_row<DT, S::kCols>(p, row, seq, n0, v);
+            } else {
+                float top = row_top<S::kCols>(v);
+                if constexpr (S::kCols == 64) {  // a block of 128 columns lies in two threads
+                    sm.top[b][half][r] = top;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sm.tops[b]);
+                    ok = warp_wait(&sm.tops[b], phase);
+                    if (!ok) break;
+                    top = fmaxf(top, sm.top[b][half ^ 1][r]);
+                }
+                const uint32_t byte = scale_byte(top);
+                if (live) {
+                    write_codes<S::kCols>(p, row, n0, inverse_of(byte), v);
+                    if (n0 % kBlock8 == 0 && n0 < p.n)
+                        p.out8.scales[n0 / (4 * kBlock8) * p.out8.scale_stride + 4 * static_cast<int64_t>(row) + n0 / kBlock8 % 4] =
+                            static_cast<uint8_t>(byte);
+                }
+            }
+            if (b == 1) phase ^= 1;
+            b ^= 1;
+        }
+        if (!ok) sm.abort = 1;
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t*>(&sm.abort) != 0) atomicExch(p.gave_up, 1u);
+    if constexpr (CG == 2) cluster_sync();  // the other SM may still read, or arrive at, what this one holds
+    if (warp == kLoadWarp) {
+        tc_fence_after();
+        if constexpr (CG == 1)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
+        else
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols));
+    }
+}
+
+// [rows, k] bytes as boxes of 128 bytes x box_rows; what lies behind either end reads as zero.
+bool encode8(CUtensorMap* map, const uint8_t* base, int k, int rows, int64_t stride, int box_rows) {
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
+    // a dimension of one element is never stepped through: any multiple of 16 will do
+    const cuuint64_t strides[1] = {rows > 1 ? static_cast<cuuint64_t>(stride) : 128};
+    const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DT, int CG, int NT>
+cudaError_t run(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
+    using S = Shape<CG, NT>;
+    if (encoder() == nullptr) return cudaErrorNotSupported;
+    CUtensorMap a, w;
+    if (!encode8(&a, p.a, p.k, p.m, p.a_stride, kRows) || !encode8(&w, p.w, p.k, p.n, p.w_stride, S::kRowsW)) return cudaErrorNotSupported;
+    constexpr uint32_t smem = sizeof(Smem<CG, NT>);
+    static_assert(smem <= 232448 && smem > 116224, "fits one SM, and no two blocks share one (tensor memory)");
+    const auto kernel = matmul8_tc_kernel<DT, CG, NT>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    // parts: what the list of tiles holds, and what counts in 32 bits
+    constexpr int64_t kMaxN = int64_t(1) << 18;
+    for (int64_t m0 = 0; m0 < p.m; m0 += int64_t(kMaxTilesM) * S::kTileM)
+        for (int64_t n0 = 0; n0 < p.n; n0 += kMaxN * NT) {
+            Part part;
+            part.m_begin = static_cast<int>(m0);
+            part.n_begin = static_cast<int>(n0);
+            part.m_tiles = static_cast<int>((min(p.m - m0, int64_t(kMaxTilesM) * S::kTileM) + S::kTileM - 1) / S::kTileM);
+            part.n_tiles = static_cast<int>((min(p.n - n0, kMaxN * NT) + NT - 1) / NT);
+            const int64_t tiles = static_cast<int64_t>(part.m_tiles) * part.n_tiles;
+            const int blocks = static_cast<int>(min(tiles, static_cast<int64_t>(sm_count / CG))) * CG;
+            kernel<<<blocks, kThreads, smem, stream>>>(p, part, a, w);
+            e = cudaGetLastError();
+            if (e != cudaSuccess) return e;
+        }
+    return cudaSuccess;
+}
+
+template <int DT>
+cudaError_t dispatch(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
+    return run<DT, 2, 256>(p, sm_count, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream) {
+    if (p.m == 0) return cudaSuccess;
+    return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, sm_count, stream) : dispatch<SPECA_F32>(p, sm_count, stream);
+}
+
+}  // namespace speca
