@@ -210,18 +210,17 @@ speca_status_t speca_layer_matmul8(speca_layer_t* c, int32_t n, int32_t k, const
     p.gate_stride = gate_stride;
     p.out_stride = out_stride;
     p.act = activation;
-    const bool codes4 = out_8bit == nullptr || (reinterpret_cast<uintptr_t>(mo.codes) % 16 == 0 && mo.code_stride % 16 == 0);
-    p.vectors = codes4 && on_16(c, bias, 0, 0) && on_16(c, residual, residual_stride, 0) && on_16(c, gate, gate_stride, 0) &&
-                on_16(c, out, out_stride, 0);
+    const bool out_on = out != nullptr ? on_16(c, out, out_stride, 0) : reinterpret_cast<uintptr_t>(mo.codes) % 16 == 0 && mo.code_stride % 16 == 0;
+    p.vectors = out_on && on_16(c, bias, 0, 0) && on_16(c, residual, residual_stride, 0) && on_16(c, gate, gate_stride, 0);
     p.gave_up = reinterpret_cast<uint32_t*>(c->ws + c->gave_up_off);
     DeviceGuard guard(c->device);
     if (!guard.ok) return fail(c, SPECA_ERR_CUDA, "cudaSetDevice failed");
     speca_status_t st = check_sticky(c);
     if (st != SPECA_OK) return st;
-    cudaError_t e = launch_matmul8(p, c->dtype, c->sm_count, static_cast<cudaStream_t>(stream));
-    if (e == cudaErrorNotSupported)
+    cudaError_t err = launch_matmul8(p, c->dtype, c->sm_count, static_cast<cudaStream_t>(stream));
+    if (err == cudaErrorNotSupported)
         return fail(c, SPECA_ERR_UNSUPPORTED, "matmul8: the copy engine cannot address a matrix with this stride");
-    return e == cudaSuccess ? SPECA_OK : cuda_fail(c, e, "matmul8");
+    return err == cudaSuccess ? SPECA_OK : cuda_fail(c, err, "matmul8");
 }
 
 }  // extern "C"

@@ -131,7 +131,8 @@ struct Matmul8Params {
     Out8 out8;
     int64_t residual_stride, gate_stride, out_stride;  // elements
     int32_t act;
-    int32_t vectors;  // bias, residual, gate and out (or the codes) take four elements at once
+    int32_t vectors;  // rows of bias, residual, gate and out (or the codes) start on 16 bytes
+    int32_t boxes;    // the copy engine can address the output (set by the launch)
     uint32_t* gave_up;
 };
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);

@@ -22,6 +22,8 @@ constexpr int kLoadWarp = 8, kIssueWarp = 9, kScaleWarp = 10;
 constexpr int kRows = 128;                       // rows of a tile in one SM
 constexpr uint32_t kTmemCols = 512;
 constexpr int kScaleCol = 480;                   // two stages of 16 columns: 4 for A's scales, up to 8 for W's
+constexpr int kScaleStages = 3;                  // in shared memory
+constexpr uint32_t kStageOut = 32 * 128;
 constexpr int kMaxTilesM = 2048;                 // tiles of rows of one launch, listed in shared memory where there is a mask
 constexpr int kGroupM = 8;                       // tiles of rows that run beside each other share their features in L2
 
@@ -32,7 +34,7 @@ struct Shape {
     static constexpr uint32_t kBytesA = kRows * 128, kBytesW = kRowsW * 128, kStage = kBytesA + kBytesW;
     static constexpr int kPartsW = (NT + 127) / 128;
     static constexpr uint32_t kScaleBytes = 512 * (1 + kPartsW);
-    static constexpr int kStages = kStage <= 24576 ? 8 : kStage <= 28672 ? 7 : kStage <= 32768 ? 6 : 4;
+    static constexpr int kStages = kStage <= 24576 ? 8 : kStage <= 28672 ? 6 : kStage <= 32768 ? 5 : 3;
     static constexpr int kCols = NT / 2;         // columns of one epilogue thread
     // place of the second sums: behind the first, or as far behind as the scales leave room
     static constexpr int kSecond = NT <= kScaleCol - NT ? NT : kScaleCol - NT;
@@ -43,9 +45,11 @@ template <int CG, int NT>
 struct Smem {
     using S = Shape<CG, NT>;
     uint8_t tiles[S::kStages][S::kStage];
-    uint8_t scales[2][S::kScaleBytes];
+    uint8_t out[kThreads / 32 - 4][kStageOut];   // of each epilogue warp: 32 rows on their way to memory
+    uint8_t scales[kScaleStages][S::kScaleBytes];
     uint64_t full[S::kStages], empty[S::kStages];
-    uint64_t scales_full[2], scales_empty[2];
+    uint64_t scales_full[kScaleStages], scales_empty[kScaleStages];
+    uint64_t scales_used[2];
     uint64_t sums_full[2], sums_free[2], overlap_free[2];
     uint64_t tops[2], drain;
     float top[2][2][kRows];
@@ -77,8 +81,16 @@ __device__ __forceinline__ void arrive_at_leader(uint64_t* bar) {
     else
         asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders<CG>(bar)) : "memory");
 }
-// A whole warp waits, for arrivals from both SMs.
-template <int CG>
+// One thread looks, or waits, for arrivals from both SMs.
+__device__ __forceinline__ bool pair_test(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity) {
     for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
         uint32_t ok;
@@ -87,10 +99,19 @@ __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity) {
             : "=r"(ok)
             : "r"(smem_u32(bar)), "r"(parity)
             : "memory");
-        if (__all_sync(0xffffffffu, ok != 0)) return true;
+        if (ok != 0) return true;
     }
     return false;
 }
+// A place in a ring.
+template <int N>
+struct Turn {
+    int stage = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++stage == N) stage = 0, phase ^= 1;
+    }
+};
 
 // ---- tensor cores -------------------------------------------------------------------------------
 template <int CG>
@@ -107,7 +128,14 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
             "l"(map), "r"(x), "r"(y), "r"(bar)
             : "memory");
 }
-// Arrives, when all products so far are done, at the barrier of this name in every SM of the tile.
+// Arrives, when all products so far are done, at this SM's barrier, or at the barrier of this name in every SM of the tile.
+template <int CG>
+__device__ __forceinline__ void commit_here(uint64_t* bar) {
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 template <int CG>
 __device__ __forceinline__ void commit(uint64_t* bar) {
     if constexpr (CG == 1)
@@ -176,98 +204,126 @@ __device__ __forceinline__ bool tile_live(const Matmul8Params& p, int first, int
     return false;
 }
 
-// ---- epilogue of one thread: `C` columns of a row ----
+// ---- epilogue of one thread: 32 columns of a row at a time ----
+// 32 elements of a row from column c on, as they lie in memory; zeros behind the last column.
 template <typename T>
-__device__ __forceinline__ void load_eight(const char* base, int64_t row, int64_t stride, int c, int n, bool vectors, float (&out)[8]) {
-    const T* from = reinterpret_cast<const T*>(base) + row * stride + c;
-    if (vectors && c + 8 <= n) {
-        constexpr int E = 16 / sizeof(T);
+struct Cols {
+    static constexpr int kWords = 8 * sizeof(T);
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const char* base, int64_t row, int64_t stride, int c, int n, bool vectors) {
+        const T* from = reinterpret_cast<const T*>(base) + row * stride + c;
+        if (vectors && c + 32 <= n) {
 #pragma unroll
-        for (int i = 0; i < 8; i += E) {
-            const Pack<T, E> v = *reinterpret_cast<const Pack<T, E>*>(from + i);
-#pragma unroll
-            for (int e = 0; e < E; ++e) out[i + e] = to_float(v.e[e]);
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(from) + i);
+                w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+            }
+            return;
         }
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            if (c + e >= n) continue;
+            if constexpr (sizeof(T) == 4)
+                w[e] = __float_as_uint(to_float(from[e]));
+            else
+                w[e / 2] |= static_cast<uint32_t>(__bfloat16_as_ushort(from[e])) << (e % 2 * 16);
+        }
+    }
+    __device__ __forceinline__ float at(int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+        return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    }
+};
+
+// Activation of 32 columns, in place; zeros behind the last column.
+__device__ __forceinline__ void finish_sums(const Matmul8Params& p, int c, float (&v)[32]) {
+    if (p.act == SPECA_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = gelu(v[i]);
+    } else if (p.act == SPECA_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = silu(v[i]);
+    }
+    if (c + 32 > p.n) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = c + i < p.n ? v[i] : 0.f;
+    }
+}
+
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// 32 columns of a row in the output's type, as they lie in memory.
+template <typename T>
+__device__ __forceinline__ void pack_row(const float (&v)[32], uint32_t (&w)[8 * sizeof(T)]) {
+#pragma unroll
+    for (int e = 0; e < static_cast<int>(8 * sizeof(T)); ++e) {
+        if constexpr (sizeof(T) == 2)
+            w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+        else
+            w[e] = __float_as_uint(v[e]);
+    }
+}
+// N words of a row straight to memory: where the copy engine cannot take the 32 rows of a warp together.
+template <typename T, int N>
+__device__ __forceinline__ void write_row(T* to, int c, int n, bool vectors, const uint32_t (&w)[N]) {
+    constexpr int kCols = 4 * N / sizeof(T);
+    if (vectors && c + kCols <= n) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) reinterpret_cast<uint4*>(to + c)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = c + e < n ? to_float(from[e]) : 0.f;
-}
-
-// Bias and activation, in place; zeros behind the last column.
-template <int DT, int C>
-__device__ __forceinline__ void finish_sums(const Matmul8Params& p, int n0, float (&v)[C]) {
-    using T = typename Type<DT>::T;
-#pragma unroll
-    for (int i = 0; i < C; i += 8) {
-        if (p.bias != nullptr) {
-            float b[8];
-            load_eight<T>(p.bias, 0, 0, n0 + i, p.n, p.vectors, b);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i + e] += b[e];
-        }
-        if (p.act != SPECA_ACT_NONE) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[i + e] = activate(v[i + e], p.act);
-        }
-    }
-    if (n0 + C > p.n) {
-#pragma unroll
-        for (int i = 0; i < C; ++i) v[i] = n0 + i < p.n ? v[i] : 0.f;
+    for (int e = 0; e < kCols; ++e) {
+        if (c + e >= n) continue;
+        if constexpr (sizeof(T) == 4)
+            to[c + e] = T(__uint_as_float(w[e]));
+        else if constexpr (sizeof(T) == 2)
+            reinterpret_cast<uint16_t*>(to)[c + e] = static_cast<uint16_t>(w[e / 2] >> 16 * (e % 2));
+        else
+            to[c + e] = static_cast<T>(w[e / 4] >> 8 * (e % 4));
     }
 }
-
-template <int DT, int C>
-__device__ __forceinline__ void write_row(const Matmul8Params& p, int row, int seq, int n0, const float (&v)[C]) {
-    using T = typename Type<DT>::T;
-    T* out = reinterpret_cast<T*>(p.out) + row * p.out_stride;
+// N words of this lane's row, from 16-byte piece `first` on, into a box of 32 rows of PITCH bytes with the swizzle of that width.
+template <int PITCH, int N>
+__device__ __forceinline__ void stage_row(uint8_t* box, int lane, int first, const uint32_t (&w)[N]) {
+    static_assert(PITCH == 64 || PITCH == 128, "a swizzle of this width");
+    const int turn = PITCH == 128 ? lane % 8 : lane / 2 % 4;
 #pragma unroll
-    for (int i = 0; i < C; i += 8) {
-        const int c = n0 + i;
-        if (c >= p.n) break;
-        float t[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] = v[i + e];
-        if (p.gate != nullptr) {
-            float g[8];
-            load_eight<T>(p.gate, seq, p.gate_stride, c, p.n, p.vectors, g);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] *= g[e];
-        }
-        if (p.residual != nullptr) {
-            float r[8];
-            load_eight<T>(p.residual, row, p.residual_stride, c, p.n, p.vectors, r);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] += r[e];
-        }
-        if (p.vectors && c + 8 <= p.n) {
-            constexpr int E = 16 / sizeof(T);
-#pragma unroll
-            for (int k = 0; k < 8; k += E) {
-                Pack<T, E> o;
-#pragma unroll
-                for (int e = 0; e < E; ++e) o.e[e] = from_float<T>(t[k + e]);
-                *reinterpret_cast<Pack<T, E>*>(out + c + k) = o;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (c + e < p.n) out[c + e] = from_float<T>(t[e]);
-        }
+    for (int i = 0; i < N; i += 4)
+        *reinterpret_cast<uint4*>(box + lane * PITCH + ((first + i / 4) ^ turn) * 16) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+}
+// What the warp staged goes out, by one lane; x, y: column and row of the box.
+__device__ __forceinline__ void send_box(const CUtensorMap* map, const uint8_t* box, int x, int y, int lane) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(box))
+                     : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
+}
+// All but the last N boxes have been read out of shared memory.
+template <int N>
+__device__ __forceinline__ void boxes_read(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+    __syncwarp();
 }
 
 // Largest finite magnitude; infinities become NaN.
-template <int C>
-__device__ __forceinline__ float row_top(float (&v)[C]) {
+__device__ __forceinline__ float row_top(float (&v)[32]) {
     const float inf = __uint_as_float(0x7f800000u);
     float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < C; ++i) top = fmaxf(top, fabsf(v[i]));
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(v[i]));
     if (top == inf) {
         top = 0.f;
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
+        for (int i = 0; i < 32; ++i) {
             if (fabsf(v[i]) == inf) v[i] = __uint_as_float(0x7fffffffu);
             top = fmaxf(top, fabsf(v[i]));
         }
@@ -275,33 +331,18 @@ __device__ __forceinline__ float row_top(float (&v)[C]) {
     return top;
 }
 
-template <int C>
-__device__ __forceinline__ void write_codes(const Matmul8Params& p, int row, int n0, float inv, const float (&v)[C]) {
-    uint8_t* to = p.out8.codes + row * p.out8.code_stride;
+__device__ __forceinline__ void pack_codes(const float (&v)[32], float inv, uint32_t (&w)[8]) {
 #pragma unroll
-    for (int i = 0; i < C; i += 16) {
-        const int c = n0 + i;
-        if (c >= p.n) break;
-        uint32_t w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            w[k] = pack_e4m3(v[i + 4 * k] * inv, v[i + 4 * k + 1] * inv, v[i + 4 * k + 2] * inv, v[i + 4 * k + 3] * inv);
-        if (p.vectors && c + 16 <= p.n) {
-            *reinterpret_cast<uint4*>(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (c + e < p.n) to[c + e] = static_cast<uint8_t>(w[e / 4] >> 8 * (e % 4));
-        }
-    }
+    for (int k = 0; k < 8; ++k) w[k] = pack_e4m3(v[4 * k] * inv, v[4 * k + 1] * inv, v[4 * k + 2] * inv, v[4 * k + 3] * inv);
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------
 template <int DT, int CG, int NT>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     matmul8_tc_kernel(const __grid_constant__ Matmul8Params p, const __grid_constant__ Part part, const __grid_constant__ CUtensorMap map_a,
-                      const __grid_constant__ CUtensorMap map_w) {
+                      const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_out) {
     using S = Shape<CG, NT>;
+    using T = typename Type<DT>::T;
     extern __shared__ __align__(1024) char raw[];
     Smem<CG, NT>& sm = *reinterpret_cast<Smem<CG, NT>*>(raw);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -317,9 +358,12 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             bar_init(&sm.full[i], 1);
             bar_init(&sm.empty[i], 1);
         }
+        for (int i = 0; i < kScaleStages; ++i) {
+            bar_init(&sm.scales_full[i], CG);
+            bar_init(&sm.scales_empty[i], 1);
+        }
         for (int b = 0; b < 2; ++b) {
-            bar_init(&sm.scales_full[b], CG);
-            bar_init(&sm.scales_empty[b], 1);
+            bar_init(&sm.scales_used[b], 1);
             bar_init(&sm.sums_full[b], 1);
             bar_init(&sm.sums_free[b], 8 * CG);     // one arrival per warp
             bar_init(&sm.overlap_free[b], 4 * CG);
@@ -396,87 +440,102 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             }
         }
     } else if (warp == kIssueWarp) {
-        // ---- products: one thread of the first SM ----
-        if (rank == 0) {
-            int stage = 0, b = 0, scale_stage = 0;
-            uint32_t phase = 0, scale_phase = 0, free_phase[2] = {1, 1}, overlap_phase[2] = {0, 0};
-            bool ok = true;
+        // ---- products: one thread of the first SM. It looks for the next stage before it issues this one's: a wait that is
+        // already satisfied takes some 200 cycles to say so, and a stage's products take 512. ----
+        if (rank == 0 && elect_one()) {
+            Turn<S::kStages> at;
+            Turn<kScaleStages> in;
+            Turn<2> held, sums_at;
+            uint32_t overlap_phase[2] = {0, 0};
+            bool ok = true, ready = false, scales_ready = false;
             for (int i = first_tile; i < n_tiles && ok; i += step) {
-                ok = pair_wait<CG>(&sm.sums_free[b], free_phase[b]);
-                free_phase[b] ^= 1;
+                const int b = sums_at.stage;
+                ok = pair_wait(&sm.sums_free[b], sums_at.phase ^ 1);
                 if (S::kOverlap && i != first_tile && ok) {
-                    ok = pair_wait<CG>(&sm.overlap_free[b ^ 1], overlap_phase[b ^ 1]);
+                    ok = pair_wait(&sm.overlap_free[b ^ 1], overlap_phase[b ^ 1]);
                     overlap_phase[b ^ 1] ^= 1;
                 }
-                tc_fence_after();
                 const uint32_t sums = tmem + b * S::kSecond;
                 for (int k = 0; k < k_blocks && ok; ++k) {
-                    const uint32_t scales = tmem + kScaleCol + scale_stage * 16;
+                    const uint32_t scales = tmem + kScaleCol + held.stage * 16;
                     if (k % 4 == 0) {
-                        ok = pair_wait<CG>(&sm.scales_full[scale_stage], scale_phase);
+                        ok = (scales_ready || pair_wait(&sm.scales_full[in.stage], in.phase)) && pair_wait(&sm.scales_used[held.stage], held.phase ^ 1);
                         if (!ok) break;
-                        if (elect_one()) {
-                            const uint32_t from = smem_u32(sm.scales[scale_stage]);
-                            copy_scales<CG>(scales, from);
+                        tc_fence_after();
+                        const uint32_t from = smem_u32(sm.scales[in.stage]);
+                        copy_scales<CG>(scales, from);
 #pragma unroll
-                            for (int q = 0; q < S::kPartsW; ++q) copy_scales<CG>(scales + 4 + 4 * q, from + 512 + 512 * q);
-                        }
-                        __syncwarp();
+                        for (int q = 0; q < S::kPartsW; ++q) copy_scales<CG>(scales + 4 + 4 * q, from + 512 + 512 * q);
+                        commit<CG>(&sm.scales_empty[in.stage]);
+                        in.next();
                     }
-                    ok = pair_wait<CG>(&sm.full[stage], phase);
+                    ok = ready || pair_wait(&sm.full[at.stage], at.phase);
                     if (!ok) break;
+                    const int stage = at.stage;
+                    at.next();
+                    ready = pair_test(&sm.full[at.stage], at.phase);
+                    scales_ready = pair_test(&sm.scales_full[in.stage], in.phase);
                     tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t from = smem_u32(sm.tiles[stage]);
-                        const uint64_t a = tile_desc(from), w = tile_desc(from + S::kBytesA);
-                        const uint32_t desc = mma_desc8<CG, NT>(0) | static_cast<uint32_t>(k % 4) << 4 | static_cast<uint32_t>(k % 4) << 29;
+                    const uint32_t from = smem_u32(sm.tiles[stage]);
+                    const uint64_t a = tile_desc(from), w = tile_desc(from + S::kBytesA);
+                    const uint32_t desc = mma_desc8<CG, NT>(0) | static_cast<uint32_t>(k % 4) << 4 | static_cast<uint32_t>(k % 4) << 29;
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) mma8<CG>(sums, a + 2 * s, w + 2 * s, desc, scales, scales + 4, k > 0 || s > 0);
-                        commit<CG>(&sm.empty[stage]);
-                        if (k % 4 == 3 || k + 1 == k_blocks) commit<CG>(&sm.scales_empty[scale_stage]);
-                        if (k + 1 == k_blocks) commit<CG>(&sm.sums_full[b]);
+                    for (int s = 0; s < 4; ++s) mma8<CG>(sums, a + 2 * s, w + 2 * s, desc, scales, scales + 4, k > 0 || s > 0);
+                    commit<CG>(&sm.empty[stage]);
+                    if (k % 4 == 3 || k + 1 == k_blocks) {
+                        commit_here<CG>(&sm.scales_used[held.stage]);
+                        held.next();
                     }
-                    __syncwarp();
-                    if (++stage == S::kStages) stage = 0, phase ^= 1;
-                    if (k % 4 == 3 || k + 1 == k_blocks)
-                        if (++scale_stage == 2) scale_stage = 0, scale_phase ^= 1;
+                    if (k + 1 == k_blocks) commit<CG>(&sm.sums_full[b]);
                 }
-                b ^= 1;
+                sums_at.next();
             }
             if (!ok) {
                 sm.abort = 1;
-                if (elect_one()) commit<CG>(&sm.drain);  // products in flight must end before tensor memory is given back
-                __syncwarp();
-                warp_wait(&sm.drain, 0);
+                commit<CG>(&sm.drain);  // products in flight must end before tensor memory is given back
+                bar_wait(&sm.drain, 0);
             }
         }
+        __syncwarp();
     } else if (warp == kScaleWarp) {
-        // ---- scales: lane i takes rows i, 32 + i, ... of a part of 128 rows ----
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        for (int i = first_tile; i < n_tiles && ok; i += step) {
-            const Place at = place<CG, NT>(part, sm, masked, m_tiles, i);
+        // ---- scales: lane i takes rows i, 32 + i, ... of a part of 128 rows. Those of the next group are on their way from memory while
+        // this one waits for room ----
+        constexpr int kParts = 1 + S::kPartsW;
+        Turn<kScaleStages> to;
+        uint32_t word[4 * kParts];
+        int tile = first_tile, k = 0;
+        Place at{0, 0};
+        auto fetch = [&] {
             const int a0 = at.m + rank * kRows + lane, w0 = at.n + lane;
-            for (int k = 0; k < k_blocks && ok; k += 4) {
-                uint32_t word[4 * (1 + S::kPartsW)];
-                const uint8_t *sa = p.a_scales + k / 4 * p.a_scale_stride, *sw = p.w_scales + k / 4 * p.w_scale_stride;
+            const uint32_t* sa = reinterpret_cast<const uint32_t*>(p.a_scales + k / 4 * p.a_scale_stride);
+            const uint32_t* sw = reinterpret_cast<const uint32_t*>(p.w_scales + k / 4 * p.w_scale_stride);
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    word[j] = a0 + 32 * j < p.m ? __ldg(reinterpret_cast<const uint32_t*>(sa) + a0 + 32 * j) : 0x7f7f7f7fu;
+            for (int j = 0; j < 4; ++j) word[j] = a0 + 32 * j < p.m ? __ldg(sa + a0 + 32 * j) : 0x7f7f7f7fu;
 #pragma unroll
-                for (int j = 0; j < 4 * S::kPartsW; ++j)
-                    word[4 + j] = w0 + 32 * j < p.n ? __ldg(reinterpret_cast<const uint32_t*>(sw) + w0 + 32 * j) : 0x7f7f7f7fu;
-                ok = warp_wait(&sm.scales_empty[stage], phase ^ 1);
-                if (!ok) break;
-                uint4* to = reinterpret_cast<uint4*>(sm.scales[stage]) + lane;
+            for (int j = 0; j < 4 * S::kPartsW; ++j) word[4 + j] = w0 + 32 * j < p.n ? __ldg(sw + w0 + 32 * j) : 0x7f7f7f7fu;
+        };
+        bool ok = true;
+        if (tile < n_tiles) {
+            at = place<CG, NT>(part, sm, masked, m_tiles, tile);
+            fetch();
+        }
+        while (tile < n_tiles) {
+            ok = warp_wait(&sm.scales_empty[to.stage], to.phase ^ 1);
+            if (!ok) break;
+            uint4* dst = reinterpret_cast<uint4*>(sm.scales[to.stage]) + lane;
 #pragma unroll
-                for (int q = 0; q < 1 + S::kPartsW; ++q) to[32 * q] = make_uint4(word[4 * q], word[4 * q + 1], word[4 * q + 2], word[4 * q + 3]);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) arrive_at_leader<CG>(&sm.scales_full[stage]);
-                if (++stage == 2) stage = 0, phase ^= 1;
+            for (int q = 0; q < kParts; ++q) dst[32 * q] = make_uint4(word[4 * q], word[4 * q + 1], word[4 * q + 2], word[4 * q + 3]);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) arrive_at_leader<CG>(&sm.scales_full[to.stage]);
+            to.next();
+            k += 4;
+            if (k >= k_blocks) {
+                k = 0;
+                tile += step;
+                if (tile < n_tiles) at = place<CG, NT>(part, sm, masked, m_tiles, tile);
             }
+            if (tile < n_tiles) fetch();
         }
         if (!ok) sm.abort = 1;
     } else if (warp < kLoadWarp) {
@@ -487,83 +546,133 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         int b = 0;
         uint32_t phase = 0;
         bool ok = true;
+        const bool eight = p.out == nullptr;
+        uint8_t* const box = sm.out[warp];
+        int turn = 0;  // half of it that is next
         for (int i = first_tile; i < n_tiles; i += step) {
             const Place at = place<CG, NT>(part, sm, masked, m_tiles, i);
-            ok = warp_wait(&sm.sums_full[b], phase);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t from = tmem + lanes + b * S::kSecond + half * S::kCols;
-            uint32_t bits[S::kCols];
-            if constexpr (S::kOverlap) {
-                // first the columns that the next tile's sums will take: the last 32 of the first place, the first 32 of the second
-                static_assert(NT - S::kSecond == 32 && S::kCols == 128, "one load");
-                if (half != b) {
-                    const int c = b == 0 ? 96 : 0;
-                    uint32_t head[32];
-                    tmem_load32(from + c, head);
-                    tmem_wait_load<32>(head);
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive_at_leader<CG>(&sm.overlap_free[b]);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        if (b == 0) bits[96 + e] = head[e]; else bits[e] = head[e];
-                    }
-                    if (b == 0) {
-#pragma unroll
-                        for (int k = 0; k < 96; k += 32) tmem_load32(from + k, bits + k);
-                    } else {
-#pragma unroll
-                        for (int k = 32; k < 128; k += 32) tmem_load32(from + k, bits + k);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 128; k += 32) tmem_load32(from + k, bits + k);
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < S::kCols; k += 32) tmem_load32(from + k, bits + k);
-            }
-            tmem_wait_load<S::kCols>(bits);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at_leader<CG>(&sm.sums_free[b]);
-
-            const int row = at.m + rank * kRows + r, n0 = at.n + half * S::kCols;
+            const int row = at.m + rank * kRows + r, row0 = row - lane, n0 = at.n + half * S::kCols;
             bool live = row < p.m;
             int seq = 0;
             if (live) {
                 seq = p.row_seq[row];
                 live = !masked || p.dev_mask[seq] != 0;
             }
-            float v[S::kCols];
+            // the copy engine takes the warp's rows together; it leaves out what lies behind the last row and column
+            const bool boxed = p.boxes && __all_sync(0xffffffffu, live || row >= p.m) && row0 < p.m;
+            ok = warp_wait(&sm.sums_full[b], phase);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t from = tmem + lanes + b * S::kSecond + half * S::kCols;
+            // 32 columns at a time, in a loop whose code stays in the instruction cache (unrolled over all columns it was two to three times as
+            // slow). First the columns that the next tile's sums will take: the last of the first place, the first of the second.
+            constexpr int kChunks = S::kCols / 32;
+            const bool backwards = S::kOverlap && half == 1 && b == 0;
+            auto chunk = [&](int j) { return 32 * (backwards ? kChunks - 1 - j : j); };
+            auto load_chunk = [&](int j, float (&v)[32]) {
+                uint32_t bits[32];
+                tmem_load32(from + chunk(j), bits);
+                tmem_wait_load<32>(bits);
 #pragma unroll
-            for (int e = 0; e < S::kCols; ++e) v[e] = __uint_as_float(bits[e]);
-            finish_sums<DT, S::kCols>(p, n0, v);
-            if (p.out != nullptr) {
-                if (live) write_row<DT, S::kCols>(p, row, seq, n0, v);
-            } else {
-                float top = row_top<S::kCols>(v);
-                if constexpr (S::kCols == 64) {  // a block of 128 columns lies in two threads
-                    sm.top[b][half][r] = top;
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(&sm.tops[b]);
-                    ok = warp_wait(&sm.tops[b], phase);
-                    if (!ok) break;
-                    top = fmaxf(top, sm.top[b][half ^ 1][r]);
+                for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(bits[e]);
+            };
+            auto give_back = [&](uint64_t* bar) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_at_leader<CG>(bar);
+            };
+            float held[32], top = 0.f;
+#pragma unroll 1
+            for (int j = 0; j < kChunks; ++j) {
+                const int c = n0 + chunk(j);
+                Cols<T> bias, gate, residual;  // asked for before the sums
+                if (p.bias != nullptr) bias.load(p.bias, 0, 0, c, p.n, p.vectors);
+                if (p.gate != nullptr && live) gate.load(p.gate, seq, p.gate_stride, c, p.n, p.vectors);
+                if (p.residual != nullptr && live) residual.load(p.residual, row, p.residual_stride, c, p.n, p.vectors);
+                float v[32];
+                load_chunk(j, v);
+                if (S::kOverlap && j == 0 && half != b) give_back(&sm.overlap_free[b]);
+                if (!eight && j == kChunks - 1) give_back(&sm.sums_free[b]);
+                if (p.bias != nullptr) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] += bias.at(e);
                 }
-                const uint32_t byte = scale_byte(top);
-                if (live) {
-                    write_codes<S::kCols>(p, row, n0, inverse_of(byte), v);
-                    if (n0 % kBlock8 == 0 && n0 < p.n)
+                finish_sums(p, c, v);
+                if (!eight) {
+                    if (p.gate != nullptr && live) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] *= gate.at(e);
+                    }
+                    if (p.residual != nullptr && live) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] += residual.at(e);
+                    }
+                    uint32_t w[8 * sizeof(T)];
+                    pack_row<T>(v, w);
+                    if (boxed) {
+                        if (c < p.n) {
+                            constexpr int kPitch = 32 * sizeof(T), kBoxes = kStageOut / (32 * kPitch);
+                            static_assert(kBoxes <= 2, "two halves");
+                            uint8_t* to = box + (kBoxes > 1 ? turn : 0) * (32 * kPitch);
+                            turn ^= 1;
+                            boxes_read<kBoxes - 1>(lane);
+                            stage_row<kPitch>(to, lane, 0, w);
+                            send_box(&map_out, to, c, row0, lane);
+                        }
+                    } else if (live) {
+                        write_row(reinterpret_cast<T*>(p.out) + row * p.out_stride, c, p.n, p.vectors, w);
+                    }
+                    continue;
+                }
+                top = fmaxf(top, row_top(v));
+                // the first stay here, the others wait for the scale where their sums were
+                if (j == 0) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) held[e] = v[e];
+                } else {
+                    uint32_t bits[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) bits[e] = __float_as_uint(v[e]);
+                    tmem_store32(from + chunk(j), bits);
+                }
+            }
+            if constexpr (S::kCols >= 64) {
+                if (eight) {
+                    tmem_wait_store();
+                    if constexpr (S::kCols == 64) {  // a block of 128 columns lies in two threads
+                        sm.top[b][half][r] = top;
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&sm.tops[b]);
+                        ok = warp_wait(&sm.tops[b], phase);
+                        if (!ok) break;
+                        top = fmaxf(top, sm.top[b][half ^ 1][r]);
+                    }
+                    const uint32_t byte = scale_byte(top);
+                    const float inv = inverse_of(byte);
+                    if (live && n0 % kBlock8 == 0 && n0 < p.n)
                         p.out8.scales[n0 / (4 * kBlock8) * p.out8.scale_stride + 4 * static_cast<int64_t>(row) + n0 / kBlock8 % 4] =
                             static_cast<uint8_t>(byte);
+                    constexpr int kPitch = S::kCols <= 64 ? 64 : 128;
+                    if (boxed) boxes_read<0>(lane);
+#pragma unroll 1
+                    for (int j = 0; j < kChunks; ++j) {
+                        if (j > 0) load_chunk(j, held);
+                        if (j == kChunks - 1) give_back(&sm.sums_free[b]);
+                        uint32_t w[8];
+                        pack_codes(held, inv, w);
+                        if (boxed)
+                            stage_row<kPitch>(box, lane, chunk(j) / 16, w);
+                        else if (live)
+                            write_row(p.out8.codes + row * p.out8.code_stride, n0 + chunk(j), p.n, p.vectors, w);
+                    }
+                    if (boxed && n0 < p.n) send_box(&map_out, box, n0, row0, lane);
                 }
             }
             if (b == 1) phase ^= 1;
             b ^= 1;
         }
         if (!ok) sm.abort = 1;
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     tc_fence_before();
@@ -590,12 +699,28 @@ bool encode8(CUtensorMap* map, const uint8_t* base, int k, int rows, int64_t str
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The output as boxes of 32 rows: of 32 columns in the layer's type, of what an epilogue thread has in 8 bits.
+bool encode_out(CUtensorMap* map, const Matmul8Params& p, int elem, int code_cols) {
+    const bool eight = p.out == nullptr;
+    void* base = eight ? p.out8.codes : reinterpret_cast<uint8_t*>(p.out);
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.n), static_cast<cuuint64_t>(p.m)};
+    const int64_t stride = eight ? p.out8.code_stride : p.out_stride * elem;
+    const cuuint64_t strides[1] = {p.m > 1 ? static_cast<cuuint64_t>(stride) : 128};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(eight ? code_cols : 32), 32}, ones[2] = {1, 1};
+    const int width = eight ? code_cols : 32 * elem;
+    return encoder()(map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+                     2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int DT, int CG, int NT>
-cudaError_t run(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
+cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
     using S = Shape<CG, NT>;
     if (encoder() == nullptr) return cudaErrorNotSupported;
-    CUtensorMap a, w;
+    CUtensorMap a, w, out = {};
     if (!encode8(&a, p.a, p.k, p.m, p.a_stride, kRows) || !encode8(&w, p.w, p.k, p.n, p.w_stride, S::kRowsW)) return cudaErrorNotSupported;
+    p.boxes = p.vectors && encode_out(&out, p, Type<DT>::kBytes, S::kCols);
     constexpr uint32_t smem = sizeof(Smem<CG, NT>);
     static_assert(smem <= 232448 && smem > 116224, "fits one SM, and no two blocks share one (tensor memory)");
     const auto kernel = matmul8_tc_kernel<DT, CG, NT>;
@@ -612,7 +737,7 @@ cudaError_t run(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
             part.n_tiles = static_cast<int>((min(p.n - n0, kMaxN * NT) + NT - 1) / NT);
             const int64_t tiles = static_cast<int64_t>(part.m_tiles) * part.n_tiles;
             const int blocks = static_cast<int>(min(tiles, static_cast<int64_t>(sm_count / CG))) * CG;
-            kernel<<<blocks, kThreads, smem, stream>>>(p, part, a, w);
+            kernel<<<blocks, kThreads, smem, stream>>>(p, part, a, w, out);
             e = cudaGetLastError();
             if (e != cudaSuccess) return e;
         }
