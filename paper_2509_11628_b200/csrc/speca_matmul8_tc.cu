@@ -3,10 +3,11 @@
 // The scales go with the operands into the tensor cores (block-scaled tcgen05.mma), so sums over all of k stay in tensor memory in
 // fp32. A tile is 128 rows times CG by NT features; with CG = 2 the two SMs of a cluster share it: each holds its 128 rows of A, half of
 // the rows of W and its half of the sums, which halves what every SM reads of W. Blocks are persistent over tiles:
-//   warps 0-3, 4-7   epilogue of the left and the right half of the columns: one thread per row, its sums in registers
+//   warps 0-3, 4-7   epilogue of the left and the right half of the columns: one thread per row
 //   warp 8           TMA loads of A and W, 128 elements of k a stage
 //   warp 9           issues the products (of both SMs, in the first of them)
-//   warp 10          scales: of 512 elements of k at once, from memory through registers into the order that the tensor memory takes
+//   warps 12-15      scales: of 512 elements of k at once, through registers into every quarter of the lanes of tensor memory. (Copied there
+//                    from shared memory by the tensor cores themselves they cost 270 cycles of every 2048: 8192 x 8192 x 4096 206 us, 188 without.)
 // Sums alternate between two places in tensor memory, so that the epilogue of a tile runs beside the products of the next.
 // Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
 #include "speca_matmul8_common.cuh"
@@ -15,14 +16,12 @@
 namespace speca {
 namespace {
 
-// Three warpgroups of 168 registers a thread at launch; the epilogue's two take 216 (half a row of sums stays in registers), the third
-// gives up what they take: 2 x 216 + 72 = 3 x 168.
-constexpr int kThreads = 384;
-constexpr int kLoadWarp = 8, kIssueWarp = 9, kScaleWarp = 10;
+// Four warpgroups of 128 registers a thread at launch; the epilogue's two take 176, the others give up what they take: 2 x 176 + 2 x 80 = 4 x 128.
+constexpr int kThreads = 512;
+constexpr int kLoadWarp = 8, kIssueWarp = 9, kScaleWarp = 12;
 constexpr int kRows = 128;                       // rows of a tile in one SM
 constexpr uint32_t kTmemCols = 512;
 constexpr int kScaleCol = 480;                   // two stages of 16 columns: 4 for A's scales, up to 8 for W's
-constexpr int kScaleStages = 3;                  // in shared memory
 constexpr uint32_t kStageOut = 32 * 128;
 constexpr int kMaxTilesM = 2048;                 // tiles of rows of one launch, listed in shared memory where there is a mask
 constexpr int kGroupM = 8;                       // tiles of rows that run beside each other share their features in L2
@@ -33,7 +32,6 @@ struct Shape {
     static constexpr int kRowsW = NT / CG;       // rows of W that one SM holds
     static constexpr uint32_t kBytesA = kRows * 128, kBytesW = kRowsW * 128, kStage = kBytesA + kBytesW;
     static constexpr int kPartsW = (NT + 127) / 128;
-    static constexpr uint32_t kScaleBytes = 512 * (1 + kPartsW);
     static constexpr int kStages = kStage <= 24576 ? 8 : kStage <= 28672 ? 6 : kStage <= 32768 ? 5 : 3;
     static constexpr int kCols = NT / 2;         // columns of one epilogue thread
     // place of the second sums: behind the first, or as far behind as the scales leave room
@@ -45,11 +43,9 @@ template <int CG, int NT>
 struct Smem {
     using S = Shape<CG, NT>;
     uint8_t tiles[S::kStages][S::kStage];
-    uint8_t out[kThreads / 32 - 4][kStageOut];   // of each epilogue warp: 32 rows on their way to memory
-    uint8_t scales[kScaleStages][S::kScaleBytes];
+    uint8_t out[8][kStageOut];   // of each epilogue warp: 32 rows on their way to memory
     uint64_t full[S::kStages], empty[S::kStages];
-    uint64_t scales_full[kScaleStages], scales_empty[kScaleStages];
-    uint64_t scales_used[2];
+    uint64_t scales_full[2], scales_used[2];
     uint64_t sums_full[2], sums_free[2], overlap_free[2];
     uint64_t tops[2], drain;
     float top[2][2][kRows];
@@ -74,14 +70,22 @@ __device__ __forceinline__ uint32_t leaders(uint64_t* bar) {
     if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
     return a;
 }
+// Tells the first SM that this warp's accesses to tensor memory are done. They are (the warp waited for them) and no other memory is
+// handed over, so nothing has to be released: a release to the cluster waits 1200 cycles for the thread's stores.
 template <int CG>
-__device__ __forceinline__ void arrive_at_leader(uint64_t* bar) {
-    if constexpr (CG == 1)
-        bar_arrive(bar);
-    else
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders<CG>(bar)) : "memory");
+__device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+        if constexpr (CG == 1)
+            bar_arrive(bar);
+        else
+            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders<CG>(bar)) : "memory");
+    }
 }
-// One thread looks, or waits, for arrivals from both SMs.
+// Looks, or waits, for arrivals from both SMs. The wait polls: a suspended thread wakes up some hundred cycles late, and between two tiles
+// three of them wait for one another.
+constexpr uint32_t kPollLimit = 1u << 24;  // some tenths of a second
 __device__ __forceinline__ bool pair_test(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
@@ -92,15 +96,13 @@ __device__ __forceinline__ bool pair_test(uint64_t* bar, uint32_t parity) {
     return ok != 0;
 }
 __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
-        uint32_t ok;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (ok != 0) return true;
-    }
+    for (uint32_t poll = 0; poll < kPollLimit; ++poll)
+        if (pair_test(bar, parity)) return true;
+    return false;
+}
+__device__ __forceinline__ bool pair_warp_wait(uint64_t* bar, uint32_t parity) {
+    for (uint32_t poll = 0; poll < kPollLimit; ++poll)
+        if (__all_sync(0xffffffffu, pair_test(bar, parity))) return true;
     return false;
 }
 // A place in a ring.
@@ -128,14 +130,7 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, 
             "l"(map), "r"(x), "r"(y), "r"(bar)
             : "memory");
 }
-// Arrives, when all products so far are done, at this SM's barrier, or at the barrier of this name in every SM of the tile.
-template <int CG>
-__device__ __forceinline__ void commit_here(uint64_t* bar) {
-    if constexpr (CG == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
+// Arrives, when all products so far are done, at the barrier of this name in every SM of the tile.
 template <int CG>
 __device__ __forceinline__ void commit(uint64_t* bar) {
     if constexpr (CG == 1)
@@ -144,16 +139,6 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
         asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
                      "h"(static_cast<uint16_t>(3))
                      : "memory");
-}
-// 32 rows of 16 bytes into 4 columns of every quarter of the lanes: the scales of 128 rows.
-template <int CG>
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t smem) {
-    // no swizzle, groups of 8 rows (128 bytes) one after another
-    const uint64_t desc = static_cast<uint64_t>((smem >> 4) & 0x3fff) | uint64_t(8) << 16 | uint64_t(8) << 32 | uint64_t(1) << 46;
-    if constexpr (CG == 1)
-        asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-    else
-        asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
 }
 // 128 bytes of k a row, with the 128-byte swizzle: 1024 bytes between groups of 8 rows.
 __device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
@@ -358,11 +343,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             bar_init(&sm.full[i], 1);
             bar_init(&sm.empty[i], 1);
         }
-        for (int i = 0; i < kScaleStages; ++i) {
-            bar_init(&sm.scales_full[i], CG);
-            bar_init(&sm.scales_empty[i], 1);
-        }
         for (int b = 0; b < 2; ++b) {
+            bar_init(&sm.scales_full[b], 4 * CG);   // one arrival per warp
             bar_init(&sm.scales_used[b], 1);
             bar_init(&sm.sums_full[b], 1);
             bar_init(&sm.sums_free[b], 8 * CG);     // one arrival per warp
@@ -411,7 +393,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     const int n_tiles = m_tiles * part.n_tiles, first_tile = blockIdx.x / CG, step = gridDim.x / CG;
     const int k_blocks = (p.k + kBlock8 - 1) / kBlock8;
 
-    if (warp >= kLoadWarp) fewer_registers<72>();
+    if (warp >= kLoadWarp) fewer_registers<80>();
     if (warp == kLoadWarp) {
         // ---- loads: one thread ----
         if (lane == 0) {
@@ -444,10 +426,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         // already satisfied takes some 200 cycles to say so, and a stage's products take 512. ----
         if (rank == 0 && elect_one()) {
             Turn<S::kStages> at;
-            Turn<kScaleStages> in;
-            Turn<2> held, sums_at;
+            Turn<2> held, sums_at;  // scales, sums
             uint32_t overlap_phase[2] = {0, 0};
-            bool ok = true, ready = false, scales_ready = false;
+            bool ok = true, ready = false;
             for (int i = first_tile; i < n_tiles && ok; i += step) {
                 const int b = sums_at.stage;
                 ok = pair_wait(&sm.sums_free[b], sums_at.phase ^ 1);
@@ -457,33 +438,21 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 }
                 const uint32_t sums = tmem + b * S::kSecond;
                 for (int k = 0; k < k_blocks && ok; ++k) {
-                    const uint32_t scales = tmem + kScaleCol + held.stage * 16;
-                    if (k % 4 == 0) {
-                        ok = (scales_ready || pair_wait(&sm.scales_full[in.stage], in.phase)) && pair_wait(&sm.scales_used[held.stage], held.phase ^ 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                        const uint32_t from = smem_u32(sm.scales[in.stage]);
-                        copy_scales<CG>(scales, from);
-#pragma unroll
-                        for (int q = 0; q < S::kPartsW; ++q) copy_scales<CG>(scales + 4 + 4 * q, from + 512 + 512 * q);
-                        commit<CG>(&sm.scales_empty[in.stage]);
-                        in.next();
-                    }
-                    ok = ready || pair_wait(&sm.full[at.stage], at.phase);
+                    if (k % 4 == 0) ok = pair_wait(&sm.scales_full[held.stage], held.phase);
+                    ok = ok && (ready || pair_wait(&sm.full[at.stage], at.phase));
                     if (!ok) break;
                     const int stage = at.stage;
                     at.next();
                     ready = pair_test(&sm.full[at.stage], at.phase);
-                    scales_ready = pair_test(&sm.scales_full[in.stage], in.phase);
                     tc_fence_after();
-                    const uint32_t from = smem_u32(sm.tiles[stage]);
+                    const uint32_t from = smem_u32(sm.tiles[stage]), scales = tmem + kScaleCol + held.stage * 16;
                     const uint64_t a = tile_desc(from), w = tile_desc(from + S::kBytesA);
                     const uint32_t desc = mma_desc8<CG, NT>(0) | static_cast<uint32_t>(k % 4) << 4 | static_cast<uint32_t>(k % 4) << 29;
 #pragma unroll
                     for (int s = 0; s < 4; ++s) mma8<CG>(sums, a + 2 * s, w + 2 * s, desc, scales, scales + 4, k > 0 || s > 0);
                     commit<CG>(&sm.empty[stage]);
                     if (k % 4 == 3 || k + 1 == k_blocks) {
-                        commit_here<CG>(&sm.scales_used[held.stage]);
+                        commit<CG>(&sm.scales_used[held.stage]);
                         held.next();
                     }
                     if (k + 1 == k_blocks) commit<CG>(&sm.sums_full[b]);
@@ -497,12 +466,11 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             }
         }
         __syncwarp();
-    } else if (warp == kScaleWarp) {
-        // ---- scales: lane i takes rows i, 32 + i, ... of a part of 128 rows. Those of the next group are on their way from memory while
-        // this one waits for room ----
-        constexpr int kParts = 1 + S::kPartsW;
-        Turn<kScaleStages> to;
-        uint32_t word[4 * kParts];
+    } else if (warp >= kScaleWarp) {
+        // ---- scales: lane i takes rows i, 32 + i, ... of a part of 128 rows, each warp for its quarter of the lanes. Those of the next group
+        // are on their way from memory while this one waits for room ----
+        Turn<2> to;
+        uint32_t word[4 * (1 + S::kPartsW)];
         int tile = first_tile, k = 0;
         Place at{0, 0};
         auto fetch = [&] {
@@ -519,15 +487,15 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             at = place<CG, NT>(part, sm, masked, m_tiles, tile);
             fetch();
         }
+        const uint32_t first = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16) + kScaleCol;
         while (tile < n_tiles) {
-            ok = warp_wait(&sm.scales_empty[to.stage], to.phase ^ 1);
+            ok = pair_warp_wait(&sm.scales_used[to.stage], to.phase ^ 1);
             if (!ok) break;
-            uint4* dst = reinterpret_cast<uint4*>(sm.scales[to.stage]) + lane;
+            tc_fence_after();
 #pragma unroll
-            for (int q = 0; q < kParts; ++q) dst[32 * q] = make_uint4(word[4 * q], word[4 * q + 1], word[4 * q + 2], word[4 * q + 3]);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) arrive_at_leader<CG>(&sm.scales_full[to.stage]);
+            for (int q = 0; q < 1 + S::kPartsW; ++q) tmem_store4(first + to.stage * 16 + 4 * q, word + 4 * q);
+            tmem_wait_store();
+            hand_over<CG>(&sm.scales_full[to.stage], lane);
             to.next();
             k += 4;
             if (k >= k_blocks) {
@@ -540,7 +508,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) sm.abort = 1;
     } else if (warp < kLoadWarp) {
         // ---- epilogue ----
-        more_registers<216>();
+        more_registers<176>();
         const int half = warp / 4, r = threadIdx.x % 128;
         const uint32_t lanes = static_cast<uint32_t>(warp % 4 * 32) << 16;
         int b = 0;
@@ -560,7 +528,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             }
             // the copy engine takes the warp's rows together; it leaves out what lies behind the last row and column
             const bool boxed = p.boxes && __all_sync(0xffffffffu, live || row >= p.m) && row0 < p.m;
-            ok = warp_wait(&sm.sums_full[b], phase);
+            ok = pair_warp_wait(&sm.sums_full[b], phase);
             if (!ok) break;
             tc_fence_after();
             const uint32_t from = tmem + lanes + b * S::kSecond + half * S::kCols;
@@ -576,11 +544,6 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(bits[e]);
             };
-            auto give_back = [&](uint64_t* bar) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_at_leader<CG>(bar);
-            };
             float held[32], top = 0.f;
 #pragma unroll 1
             for (int j = 0; j < kChunks; ++j) {
@@ -591,8 +554,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 if (p.residual != nullptr && live) residual.load(p.residual, row, p.residual_stride, c, p.n, p.vectors);
                 float v[32];
                 load_chunk(j, v);
-                if (S::kOverlap && j == 0 && half != b) give_back(&sm.overlap_free[b]);
-                if (!eight && j == kChunks - 1) give_back(&sm.sums_free[b]);
+                if (S::kOverlap && j == 0 && half != b) hand_over<CG>(&sm.overlap_free[b], lane);
+                if (!eight && j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
                 if (p.bias != nullptr) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] += bias.at(e);
@@ -657,7 +620,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll 1
                     for (int j = 0; j < kChunks; ++j) {
                         if (j > 0) load_chunk(j, held);
-                        if (j == kChunks - 1) give_back(&sm.sums_free[b]);
+                        if (j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
                         uint32_t w[8];
                         pack_codes(held, inv, w);
                         if (boxed)
