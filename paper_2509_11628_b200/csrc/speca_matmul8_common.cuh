@@ -7,18 +7,18 @@ namespace speca {
 namespace {
 
 // GELU and SILU are both t * sigmoid(s) = t / (1 + 2^x), x = -s log2(e); so negative t keep their digits, which 1 + tanh would cost.
+// GELU: x = t (kGelu1 + kGelu3 t^2), with 2 sqrt(2 / pi) log2(e) and 0.044715 of it; SILU: x = kSilu1 t.
+constexpr float kGelu1 = static_cast<float>(-1.5957691216057308 * 1.4426950408889634), kGelu3 = static_cast<float>(-0.044715 * 1.5957691216057308 * 1.4426950408889634);
+constexpr float kSilu1 = -1.4426950408889634f;
 __device__ __forceinline__ float times_sigmoid(float t, float x) {
     float e, r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
     return t * r;
 }
-__device__ __forceinline__ float gelu(float t) {
-    constexpr double k = 1.5957691216057308 * 1.4426950408889634;  // 2 sqrt(2 / pi) log2(e)
-    return times_sigmoid(t, t * fmaf(t * t, static_cast<float>(-0.044715 * k), static_cast<float>(-k)));
+__device__ __forceinline__ float activate(float t, int act) {
+    return act == SPECA_ACT_GELU ? times_sigmoid(t, t * fmaf(t * t, kGelu3, kGelu1)) : act == SPECA_ACT_SILU ? times_sigmoid(t, t * kSilu1) : t;
 }
-__device__ __forceinline__ float silu(float t) { return times_sigmoid(t, t * -1.4426950408889634f); }
-__device__ __forceinline__ float activate(float t, int act) { return act == SPECA_ACT_GELU ? gelu(t) : act == SPECA_ACT_SILU ? silu(t) : t; }
 
 // Four consecutive elements of a row of `n`, from c on, where they exist; zeros elsewhere.
 template <typename T>

@@ -34,6 +34,7 @@ struct Shape {
     static constexpr int kPartsW = (NT + 127) / 128;
     static constexpr int kStages = kStage <= 24576 ? 8 : kStage <= 28672 ? 6 : kStage <= 32768 ? 5 : 3;
     static constexpr int kCols = NT / 2;         // columns of one epilogue thread
+    static_assert(kCols == 64 || kCols == 128, "boxes of 64 or 128 codes");
     // place of the second sums: behind the first, or as far behind as the scales leave room
     static constexpr int kSecond = NT <= kScaleCol - NT ? NT : kScaleCol - NT;
     static constexpr bool kOverlap = kSecond < NT;
@@ -189,8 +190,41 @@ __device__ __forceinline__ bool tile_live(const Matmul8Params& p, int first, int
     return false;
 }
 
-// ---- epilogue of one thread: 32 columns of a row at a time ----
-// 32 elements of a row from column c on, as they lie in memory; zeros behind the last column.
+// ---- epilogue: a warp has 32 rows, one a lane, and takes 32 columns at a time ----
+// What the output is: the sums after bias and activation in the layer's type; the same with gate and residual; 8 bits. Each has a kernel of its
+// own: the epilogue's code has to stay in the instruction cache (one for all, unrolled over all columns, was three times as slow).
+enum Epilogue { kPlain, kResidual, kEight };
+
+// v[e] of every lane plus what lane e holds.
+__device__ __forceinline__ void add_columns(float (&v)[32], float x) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] += __shfl_sync(0xffffffffu, x, e);
+}
+// t / (1 + 2^x), two at a time.
+__device__ __forceinline__ uint64_t times_sigmoid2(uint64_t t, uint64_t x) {
+    float x0, x1, d0, d1;
+    unpair(x, x0, x1);
+    unpair(add2(pair(ex2(x0), ex2(x1)), pair(1.f, 1.f)), d0, d1);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d0));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d1));
+    return mul2(t, pair(d0, d1));
+}
+__device__ __forceinline__ void activate32(float (&v)[32], int act) {
+    if (act == SPECA_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const uint64_t t = pair(v[e], v[e + 1]);
+            unpair(times_sigmoid2(t, mul2(t, fma2(mul2(t, t), pair(kGelu3, kGelu3), pair(kGelu1, kGelu1)))), v[e], v[e + 1]);
+        }
+    } else if (act == SPECA_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const uint64_t t = pair(v[e], v[e + 1]);
+            unpair(times_sigmoid2(t, mul2(t, pair(kSilu1, kSilu1))), v[e], v[e + 1]);
+        }
+    }
+}
+// 32 elements of a lane's own row from column c on, as they lie in memory; zeros behind the last column.
 template <typename T>
 struct Cols {
     static constexpr int kWords = 8 * sizeof(T);
@@ -221,99 +255,82 @@ struct Cols {
         return __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
     }
 };
-
-// Activation of 32 columns, in place; zeros behind the last column.
-__device__ __forceinline__ void finish_sums(const Matmul8Params& p, int c, float (&v)[32]) {
-    if (p.act == SPECA_ACT_GELU) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = gelu(v[i]);
-    } else if (p.act == SPECA_ACT_SILU) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = silu(v[i]);
-    }
-    if (c + 32 > p.n) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = c + i < p.n ? v[i] : 0.f;
-    }
-}
-
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 // 32 columns of a row in the output's type, as they lie in memory.
 template <typename T>
 __device__ __forceinline__ void pack_row(const float (&v)[32], uint32_t (&w)[8 * sizeof(T)]) {
 #pragma unroll
     for (int e = 0; e < static_cast<int>(8 * sizeof(T)); ++e) {
         if constexpr (sizeof(T) == 2)
-            w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
+            w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
         else
             w[e] = __float_as_uint(v[e]);
     }
 }
-// N words of a row straight to memory: where the copy engine cannot take the 32 rows of a warp together.
-template <typename T, int N>
-__device__ __forceinline__ void write_row(T* to, int c, int n, bool vectors, const uint32_t (&w)[N]) {
-    constexpr int kCols = 4 * N / sizeof(T);
-    if (vectors && c + kCols <= n) {
-#pragma unroll
-        for (int i = 0; i < N; i += 4) reinterpret_cast<uint4*>(to + c)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < kCols; ++e) {
-        if (c + e >= n) continue;
-        if constexpr (sizeof(T) == 4)
-            to[c + e] = T(__uint_as_float(w[e]));
-        else if constexpr (sizeof(T) == 2)
-            reinterpret_cast<uint16_t*>(to)[c + e] = static_cast<uint16_t>(w[e / 2] >> 16 * (e % 2));
-        else
-            to[c + e] = static_cast<T>(w[e / 4] >> 8 * (e % 4));
-    }
+
+// Boxes: 32 rows of PITCH bytes in shared memory, with the swizzle of that width.
+template <int PITCH>
+__device__ __forceinline__ uint32_t box_piece(int row, int piece) {
+    static_assert(PITCH == 64 || PITCH == 128, "a swizzle of this width");
+    return row * PITCH + (piece ^ (PITCH == 128 ? row % 8 : row / 2 % 4)) * 16;
 }
-// N words of this lane's row, from 16-byte piece `first` on, into a box of 32 rows of PITCH bytes with the swizzle of that width.
+
+// N words of this lane's row, from 16-byte piece `first` on.
 template <int PITCH, int N>
 __device__ __forceinline__ void stage_row(uint8_t* box, int lane, int first, const uint32_t (&w)[N]) {
-    static_assert(PITCH == 64 || PITCH == 128, "a swizzle of this width");
-    const int turn = PITCH == 128 ? lane % 8 : lane / 2 % 4;
 #pragma unroll
     for (int i = 0; i < N; i += 4)
-        *reinterpret_cast<uint4*>(box + lane * PITCH + ((first + i / 4) ^ turn) * 16) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+        *reinterpret_cast<uint4*>(box + box_piece<PITCH>(lane, first + i / 4)) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
 }
-// What the warp staged goes out, by one lane; x, y: column and row of the box.
-__device__ __forceinline__ void send_box(const CUtensorMap* map, const uint8_t* box, int x, int y, int lane) {
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0) {
-        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(smem_u32(box))
-                     : "memory");
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+// What the warp staged goes out. By the copy engine, all rows together, which leaves out what lies behind the last row and column; or, where
+// it cannot address the output or a row is not to be written, row by row.
+template <typename T, int PITCH>
+__device__ __forceinline__ void send_box(const CUtensorMap* map, bool boxed, const uint8_t* box, T* out, int64_t stride, int c, int n, int row0,
+                                         uint32_t live, int lane) {
+    if (c >= n) return;
+    if (boxed) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c), "r"(row0), "r"(smem_u32(box))
+                         : "memory");
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
+        return;
     }
+    __syncwarp();
+    for (uint32_t rest = live; rest != 0; rest &= rest - 1) {
+        const int r = __ffs(rest) - 1;
+        T* to = out + (row0 + r) * stride + c;
+#pragma unroll 1
+        for (int e = lane; e < PITCH / static_cast<int>(sizeof(T)); e += 32) {
+            const int byte = e * sizeof(T);
+            if (c + e < n) to[e] = *reinterpret_cast<const T*>(box + box_piece<PITCH>(r, byte / 16) + byte % 16);
+        }
+    }
+    __syncwarp();
 }
-// All but the last N boxes have been read out of shared memory.
-template <int N>
-__device__ __forceinline__ void boxes_read(int lane) {
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+// The box has been read out of shared memory.
+__device__ __forceinline__ void box_read(int lane) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
 }
 
-// Largest finite magnitude; infinities become NaN.
+// Largest finite magnitude of a lane's 32 values; infinities become NaN.
 __device__ __forceinline__ float row_top(float (&v)[32]) {
     const float inf = __uint_as_float(0x7f800000u);
-    float top = 0.f;
+    float top[4] = {};
 #pragma unroll
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf(v[i]));
-    if (top == inf) {
-        top = 0.f;
+    for (int i = 0; i < 32; ++i) top[i % 4] = fmaxf(top[i % 4], fabsf(v[i]));
+    float all = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+    if (__any_sync(0xffffffffu, all == inf)) {
+        all = 0.f;
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             if (fabsf(v[i]) == inf) v[i] = __uint_as_float(0x7fffffffu);
-            top = fmaxf(top, fabsf(v[i]));
+            all = fmaxf(all, fabsf(v[i]));
         }
     }
-    return top;
+    return all;
 }
 
 __device__ __forceinline__ void pack_codes(const float (&v)[32], float inv, uint32_t (&w)[8]) {
@@ -322,7 +339,7 @@ __device__ __forceinline__ void pack_codes(const float (&v)[32], float inv, uint
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------
-template <int DT, int CG, int NT>
+template <int DT, int CG, int NT, Epilogue E>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     matmul8_tc_kernel(const __grid_constant__ Matmul8Params p, const __grid_constant__ Part part, const __grid_constant__ CUtensorMap map_a,
                       const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_out) {
@@ -514,9 +531,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         int b = 0;
         uint32_t phase = 0;
         bool ok = true;
-        const bool eight = p.out == nullptr;
         uint8_t* const box = sm.out[warp];
-        int turn = 0;  // half of it that is next
         for (int i = first_tile; i < n_tiles; i += step) {
             const Place at = place<CG, NT>(part, sm, masked, m_tiles, i);
             const int row = at.m + rank * kRows + r, row0 = row - lane, n0 = at.n + half * S::kCols;
@@ -526,16 +541,12 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 seq = p.row_seq[row];
                 live = !masked || p.dev_mask[seq] != 0;
             }
-            // the copy engine takes the warp's rows together; it leaves out what lies behind the last row and column
-            const bool boxed = p.boxes && __all_sync(0xffffffffu, live || row >= p.m) && row0 < p.m;
-            ok = pair_warp_wait(&sm.sums_full[b], phase);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t from = tmem + lanes + b * S::kSecond + half * S::kCols;
-            // 32 columns at a time, in a loop whose code stays in the instruction cache (unrolled over all columns it was two to three times as
-            // slow). First the columns that the next tile's sums will take: the last of the first place, the first of the second.
+            const uint32_t lives = __ballot_sync(0xffffffffu, live);
+            const bool boxed = p.boxes && lives == __ballot_sync(0xffffffffu, row < p.m) && lives != 0;
+            // First the columns that the next tile's sums will take: the last of the first place, the first of the second.
             constexpr int kChunks = S::kCols / 32;
             const bool backwards = S::kOverlap && half == 1 && b == 0;
+            const uint32_t from = tmem + lanes + b * S::kSecond + half * S::kCols;
             auto chunk = [&](int j) { return 32 * (backwards ? kChunks - 1 - j : j); };
             auto load_chunk = [&](int j, float (&v)[32]) {
                 uint32_t bits[32];
@@ -544,92 +555,99 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(bits[e]);
             };
-            float held[32], top = 0.f;
+            // bias, lane by lane, and residual of a chunk are asked for before its sums are
+            float bias = 0.f;
+            Cols<T> residual;
+            auto ask = [&](int j) {
+                const int c = n0 + chunk(j);
+                if (p.bias != nullptr) bias = c + lane < p.n ? to_float(reinterpret_cast<const T*>(p.bias)[c + lane]) : 0.f;
+                if constexpr (E == kResidual)
+                    if (p.residual != nullptr && live) residual.load(p.residual, row, p.residual_stride, c, p.n, p.vectors);
+            };
+            ask(0);
+            ok = pair_warp_wait(&sm.sums_full[b], phase);
+            if (!ok) break;
+            tc_fence_after();
+            [[maybe_unused]] float held[32], top = 0.f;
 #pragma unroll 1
             for (int j = 0; j < kChunks; ++j) {
                 const int c = n0 + chunk(j);
-                Cols<T> bias, gate, residual;  // asked for before the sums
-                if (p.bias != nullptr) bias.load(p.bias, 0, 0, c, p.n, p.vectors);
-                if (p.gate != nullptr && live) gate.load(p.gate, seq, p.gate_stride, c, p.n, p.vectors);
-                if (p.residual != nullptr && live) residual.load(p.residual, row, p.residual_stride, c, p.n, p.vectors);
                 float v[32];
                 load_chunk(j, v);
                 if (S::kOverlap && j == 0 && half != b) hand_over<CG>(&sm.overlap_free[b], lane);
-                if (!eight && j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
-                if (p.bias != nullptr) {
+                if (E != kEight && j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
+                if (p.bias != nullptr) add_columns(v, bias);
+                activate32(v, p.act);
+                if constexpr (E == kEight) {
+                    if (j + 1 < kChunks) ask(j + 1);
+                    top = fmaxf(top, row_top(v));
+                    // the first stay here, the others wait for the scale where their sums were
+                    if (j == 0) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] += bias.at(e);
-                }
-                finish_sums(p, c, v);
-                if (!eight) {
-                    if (p.gate != nullptr && live) {
+                        for (int e = 0; e < 32; ++e) held[e] = v[e];
+                    } else {
+                        uint32_t bits[32];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] *= gate.at(e);
+                        for (int e = 0; e < 32; ++e) bits[e] = __float_as_uint(v[e]);
+                        tmem_store32(from + chunk(j), bits);
                     }
-                    if (p.residual != nullptr && live) {
+                } else {
+                    if constexpr (E == kResidual) {
+                        if (p.gate != nullptr) {  // one sequence after another, of those that the warp's rows belong to
+                            for (uint32_t rest = lives; rest != 0;) {
+                                const int s = __shfl_sync(0xffffffffu, seq, __ffs(rest) - 1);
+                                const bool mine = live && seq == s;
+                                rest &= ~__ballot_sync(0xffffffffu, mine);
+                                const float g = c + lane < p.n ? to_float(reinterpret_cast<const T*>(p.gate)[s * p.gate_stride + c + lane]) : 0.f;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] += residual.at(e);
+                                for (int e = 0; e < 32; ++e) {
+                                    const float f = __shfl_sync(0xffffffffu, g, e);
+                                    v[e] = mine ? v[e] * f : v[e];
+                                }
+                            }
+                        }
+                        if (p.residual != nullptr && live) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] += residual.at(e);
+                        }
                     }
+                    if (j + 1 < kChunks) ask(j + 1);
+                    // a box holds 128 bytes a row: one or two chunks
+                    constexpr int kPer = 4 / sizeof(T);
                     uint32_t w[8 * sizeof(T)];
                     pack_row<T>(v, w);
-                    if (boxed) {
-                        if (c < p.n) {
-                            constexpr int kPitch = 32 * sizeof(T), kBoxes = kStageOut / (32 * kPitch);
-                            static_assert(kBoxes <= 2, "two halves");
-                            uint8_t* to = box + (kBoxes > 1 ? turn : 0) * (32 * kPitch);
-                            turn ^= 1;
-                            boxes_read<kBoxes - 1>(lane);
-                            stage_row<kPitch>(to, lane, 0, w);
-                            send_box(&map_out, to, c, row0, lane);
-                        }
-                    } else if (live) {
-                        write_row(reinterpret_cast<T*>(p.out) + row * p.out_stride, c, p.n, p.vectors, w);
-                    }
-                    continue;
-                }
-                top = fmaxf(top, row_top(v));
-                // the first stay here, the others wait for the scale where their sums were
-                if (j == 0) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) held[e] = v[e];
-                } else {
-                    uint32_t bits[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) bits[e] = __float_as_uint(v[e]);
-                    tmem_store32(from + chunk(j), bits);
+                    if (j % kPer == 0) box_read(lane);
+                    stage_row<128>(box, lane, chunk(j) / 32 % kPer * 4, w);
+                    if (j % kPer == kPer - 1)
+                        send_box<T, 128>(&map_out, boxed, box, reinterpret_cast<T*>(p.out), p.out_stride, n0 + chunk(j) / (32 * kPer) * (32 * kPer), p.n,
+                                         row0, lives, lane);
                 }
             }
-            if constexpr (S::kCols >= 64) {
-                if (eight) {
-                    tmem_wait_store();
-                    if constexpr (S::kCols == 64) {  // a block of 128 columns lies in two threads
-                        sm.top[b][half][r] = top;
-                        __syncwarp();
-                        if (lane == 0) bar_arrive(&sm.tops[b]);
-                        ok = warp_wait(&sm.tops[b], phase);
-                        if (!ok) break;
-                        top = fmaxf(top, sm.top[b][half ^ 1][r]);
-                    }
-                    const uint32_t byte = scale_byte(top);
-                    const float inv = inverse_of(byte);
-                    if (live && n0 % kBlock8 == 0 && n0 < p.n)
-                        p.out8.scales[n0 / (4 * kBlock8) * p.out8.scale_stride + 4 * static_cast<int64_t>(row) + n0 / kBlock8 % 4] =
-                            static_cast<uint8_t>(byte);
-                    constexpr int kPitch = S::kCols <= 64 ? 64 : 128;
-                    if (boxed) boxes_read<0>(lane);
-#pragma unroll 1
-                    for (int j = 0; j < kChunks; ++j) {
-                        if (j > 0) load_chunk(j, held);
-                        if (j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
-                        uint32_t w[8];
-                        pack_codes(held, inv, w);
-                        if (boxed)
-                            stage_row<kPitch>(box, lane, chunk(j) / 16, w);
-                        else if (live)
-                            write_row(p.out8.codes + row * p.out8.code_stride, n0 + chunk(j), p.n, p.vectors, w);
-                    }
-                    if (boxed && n0 < p.n) send_box(&map_out, box, n0, row0, lane);
+            if constexpr (E == kEight) {
+                tmem_wait_store();
+                if constexpr (S::kCols == 64) {  // a block of 128 columns lies in two threads
+                    sm.top[b][half][r] = top;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(&sm.tops[b]);
+                    ok = warp_wait(&sm.tops[b], phase);
+                    if (!ok) break;
+                    top = fmaxf(top, sm.top[b][half ^ 1][r]);
                 }
+                const uint32_t byte = scale_byte(top);
+                const float inv = inverse_of(byte);
+                if (live && n0 % kBlock8 == 0 && n0 < p.n)
+                    p.out8.scales[n0 / (4 * kBlock8) * p.out8.scale_stride + 4 * static_cast<int64_t>(row) + n0 / kBlock8 % 4] =
+                        static_cast<uint8_t>(byte);
+                box_read(lane);
+#pragma unroll 1
+                for (int j = 0; j < kChunks; ++j) {
+                    if (j > 0) load_chunk(j, held);
+                    if (j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
+                    uint32_t w[8];
+                    pack_codes(held, inv, w);
+                    stage_row<S::kCols>(box, lane, chunk(j) / 16, w);
+                }
+                send_box<uint8_t, S::kCols>(&map_out, boxed, box, p.out8.codes, p.out8.code_stride, n0, p.n, row0, lives, lane);
             }
             if (b == 1) phase ^= 1;
             b ^= 1;
@@ -662,15 +680,15 @@ bool encode8(CUtensorMap* map, const uint8_t* base, int k, int rows, int64_t str
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// The output as boxes of 32 rows: of 32 columns in the layer's type, of what an epilogue thread has in 8 bits.
+// The output as boxes of 32 rows: of 128 bytes in the layer's type, of what an epilogue thread has in 8 bits.
 bool encode_out(CUtensorMap* map, const Matmul8Params& p, int elem, int code_cols) {
     const bool eight = p.out == nullptr;
     void* base = eight ? p.out8.codes : reinterpret_cast<uint8_t*>(p.out);
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.n), static_cast<cuuint64_t>(p.m)};
     const int64_t stride = eight ? p.out8.code_stride : p.out_stride * elem;
     const cuuint64_t strides[1] = {p.m > 1 ? static_cast<cuuint64_t>(stride) : 128};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(eight ? code_cols : 32), 32}, ones[2] = {1, 1};
-    const int width = eight ? code_cols : 32 * elem;
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(eight ? code_cols : 128 / elem), 32}, ones[2] = {1, 1};
+    const int width = eight ? code_cols : 128;
     return encoder()(map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
                      2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                      width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
@@ -686,7 +704,9 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
     p.boxes = p.vectors && encode_out(&out, p, Type<DT>::kBytes, S::kCols);
     constexpr uint32_t smem = sizeof(Smem<CG, NT>);
     static_assert(smem <= 232448 && smem > 116224, "fits one SM, and no two blocks share one (tensor memory)");
-    const auto kernel = matmul8_tc_kernel<DT, CG, NT>;
+    const auto kernel = p.out == nullptr                                  ? matmul8_tc_kernel<DT, CG, NT, kEight>
+                        : p.residual != nullptr || p.gate != nullptr ? matmul8_tc_kernel<DT, CG, NT, kResidual>
+                                                                     : matmul8_tc_kernel<DT, CG, NT, kPlain>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     // parts: what the list of tiles holds, and what counts in 32 bits
