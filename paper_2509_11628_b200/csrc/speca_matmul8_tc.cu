@@ -45,6 +45,7 @@ struct Smem {
     using S = Shape<CG, NT>;
     uint8_t tiles[S::kStages][S::kStage];
     uint8_t out[8][kStageOut];   // of each epilogue warp: 32 rows on their way to memory
+    float columns[8][2][S::kCols];  // of each epilogue warp: bias and gate of its columns
     uint64_t full[S::kStages], empty[S::kStages];
     uint64_t scales_full[2], scales_used[2];
     uint64_t sums_full[2], sums_free[2], overlap_free[2];
@@ -195,19 +196,14 @@ __device__ __forceinline__ bool tile_live(const Matmul8Params& p, int first, int
 // own: the epilogue's code has to stay in the instruction cache (one for all, unrolled over all columns, was three times as slow).
 enum Epilogue { kPlain, kResidual, kEight };
 
-// v[e] of every lane plus what lane e holds.
-__device__ __forceinline__ void add_columns(float (&v)[32], float x) {
-#pragma unroll
-    for (int e = 0; e < 32; ++e) v[e] += __shfl_sync(0xffffffffu, x, e);
-}
-// t / (1 + 2^x), two at a time.
+// t / (1 + 2^x), two at a time with one reciprocal, 1 / a = b / (a b): the special function unit, which forms 16 a cycle, bounds an epilogue
+// with an activation. So that a b stays finite x is held at 63: below 2^-63 t the result is that.
 __device__ __forceinline__ uint64_t times_sigmoid2(uint64_t t, uint64_t x) {
-    float x0, x1, d0, d1;
+    float x0, x1, d0, d1, r;
     unpair(x, x0, x1);
-    unpair(add2(pair(ex2(x0), ex2(x1)), pair(1.f, 1.f)), d0, d1);
-    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d0));
-    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(d1));
-    return mul2(t, pair(d0, d1));
+    unpair(add2(pair(ex2(fminf(x0, 63.f)), ex2(fminf(x1, 63.f))), pair(1.f, 1.f)), d0, d1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
+    return mul2(t, mul2(pair(d1, d0), pair(r, r)));
 }
 __device__ __forceinline__ void activate32(float (&v)[32], int act) {
     if (act == SPECA_ACT_GELU) {
@@ -224,6 +220,21 @@ __device__ __forceinline__ void activate32(float (&v)[32], int act) {
         }
     }
 }
+// A warp's columns of a row of `n` elements (bias, gate) into its part of shared memory, zeros behind the last; every lane then reads them all.
+template <typename T, int N>
+__device__ __forceinline__ void stage_columns(float* to, const T* from, int c, int n, int lane) {
+#pragma unroll
+    for (int i = lane; i < N; i += 32) to[i] = c + i < n ? to_float(from[c + i]) : 0.f;
+    __syncwarp();
+}
+__device__ __forceinline__ void add_columns(float (&v)[32], const float* x) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(x + e);
+        v[e] += f.x, v[e + 1] += f.y, v[e + 2] += f.z, v[e + 3] += f.w;
+    }
+}
+
 // 32 elements of a lane's own row from column c on, as they lie in memory; zeros behind the last column.
 template <typename T>
 struct Cols {
@@ -555,16 +566,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(bits[e]);
             };
-            // bias, lane by lane, and residual of a chunk are asked for before its sums are
-            float bias = 0.f;
+            // before the sums are there: bias, gate (of a warp whose rows belong to one sequence), the residual of the first chunk
+            __syncwarp();
+            if (p.bias != nullptr) stage_columns<T, S::kCols>(sm.columns[warp][0], reinterpret_cast<const T*>(p.bias), n0, p.n, lane);
+            bool one_gate = false;
             Cols<T> residual;
             auto ask = [&](int j) {
-                const int c = n0 + chunk(j);
-                if (p.bias != nullptr) bias = c + lane < p.n ? to_float(reinterpret_cast<const T*>(p.bias)[c + lane]) : 0.f;
-                if constexpr (E == kResidual)
-                    if (p.residual != nullptr && live) residual.load(p.residual, row, p.residual_stride, c, p.n, p.vectors);
+                if (p.residual != nullptr && live) residual.load(p.residual, row, p.residual_stride, n0 + chunk(j), p.n, p.vectors);
             };
-            ask(0);
+            if constexpr (E == kResidual) {
+                const int s = __shfl_sync(0xffffffffu, seq, lives == 0 ? 0 : __ffs(lives) - 1);
+                one_gate = p.gate != nullptr && __all_sync(0xffffffffu, !live || seq == s);
+                if (one_gate) stage_columns<T, S::kCols>(sm.columns[warp][1], reinterpret_cast<const T*>(p.gate) + s * p.gate_stride, n0, p.n, lane);
+                ask(0);
+            }
             ok = pair_warp_wait(&sm.sums_full[b], phase);
             if (!ok) break;
             tc_fence_after();
@@ -576,10 +591,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 load_chunk(j, v);
                 if (S::kOverlap && j == 0 && half != b) hand_over<CG>(&sm.overlap_free[b], lane);
                 if (E != kEight && j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
-                if (p.bias != nullptr) add_columns(v, bias);
+                if (p.bias != nullptr) add_columns(v, sm.columns[warp][0] + chunk(j));
                 activate32(v, p.act);
                 if constexpr (E == kEight) {
-                    if (j + 1 < kChunks) ask(j + 1);
                     top = fmaxf(top, row_top(v));
                     // the first stay here, the others wait for the scale where their sums were
                     if (j == 0) {
@@ -593,25 +607,25 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                     }
                 } else {
                     if constexpr (E == kResidual) {
-                        if (p.gate != nullptr) {  // one sequence after another, of those that the warp's rows belong to
-                            for (uint32_t rest = lives; rest != 0;) {
-                                const int s = __shfl_sync(0xffffffffu, seq, __ffs(rest) - 1);
-                                const bool mine = live && seq == s;
-                                rest &= ~__ballot_sync(0xffffffffu, mine);
-                                const float g = c + lane < p.n ? to_float(reinterpret_cast<const T*>(p.gate)[s * p.gate_stride + c + lane]) : 0.f;
+                        if (one_gate) {
+                            const float* g = sm.columns[warp][1] + chunk(j);
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const float f = __shfl_sync(0xffffffffu, g, e);
-                                    v[e] = mine ? v[e] * f : v[e];
-                                }
+                            for (int e = 0; e < 32; e += 4) {
+                                const float4 f = *reinterpret_cast<const float4*>(g + e);
+                                v[e] *= f.x, v[e + 1] *= f.y, v[e + 2] *= f.z, v[e + 3] *= f.w;
                             }
+                        } else if (p.gate != nullptr && live) {
+                            Cols<T> gate;
+                            gate.load(p.gate, seq, p.gate_stride, c, p.n, p.vectors);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] *= gate.at(e);
                         }
                         if (p.residual != nullptr && live) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) v[e] += residual.at(e);
                         }
+                        if (j + 1 < kChunks) ask(j + 1);
                     }
-                    if (j + 1 < kChunks) ask(j + 1);
                     // a box holds 128 bytes a row: one or two chunks
                     constexpr int kPer = 4 / sizeof(T);
                     uint32_t w[8 * sizeof(T)];
