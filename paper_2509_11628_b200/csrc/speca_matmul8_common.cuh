@@ -1,7 +1,8 @@
-// What the 8-bit products share: their epilogue.
+// What the 8-bit products share: operands' tensor maps, activations, the epilogue of a warp.
 #pragma once
 #include "speca_eight_common.cuh"
 #include "speca_rows_common.cuh"
+#include "speca_tc.cuh"
 
 namespace speca {
 namespace {
@@ -88,6 +89,17 @@ __device__ __forceinline__ void finish_block(const Matmul8Params& p, int row, in
         for (int e = 0; e < 4; ++e)
             if (c + e < p.n) to[e] = from_float<T>(v[e]);
     }
+}
+
+// [rows, k] bytes as boxes of 128 bytes x box_rows; what lies behind either end reads as zero.
+bool encode8(CUtensorMap* map, const uint8_t* base, int k, int rows, int64_t stride, int box_rows) {
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
+    // a dimension of one element is never stepped through: any multiple of 16 will do
+    const cuuint64_t strides[1] = {rows > 1 ? static_cast<cuuint64_t>(stride) : 128};
+    const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace

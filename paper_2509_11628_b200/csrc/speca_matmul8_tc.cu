@@ -11,7 +11,6 @@
 // Sums alternate between two places in tensor memory, so that the epilogue of a tile runs beside the products of the next.
 // Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
 #include "speca_matmul8_common.cuh"
-#include "speca_tc.cuh"
 
 namespace speca {
 namespace {
@@ -683,17 +682,6 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     }
 }
 
-// [rows, k] bytes as boxes of 128 bytes x box_rows; what lies behind either end reads as zero.
-bool encode8(CUtensorMap* map, const uint8_t* base, int k, int rows, int64_t stride, int box_rows) {
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
-    // a dimension of one element is never stepped through: any multiple of 16 will do
-    const cuuint64_t strides[1] = {rows > 1 ? static_cast<cuuint64_t>(stride) : 128};
-    const cuuint32_t box[2] = {128, static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
-    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, box, ones,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 // The output as boxes of 32 rows: of 128 bytes in the layer's type, of what an epilogue thread has in 8 bits.
 bool encode_out(CUtensorMap* map, const Matmul8Params& p, int elem, int code_cols) {
     const bool eight = p.out == nullptr;
@@ -750,6 +738,7 @@ cudaError_t dispatch(const Matmul8Params& p, int sm_count, cudaStream_t stream) 
 
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream) {
     if (p.m == 0) return cudaSuccess;
+    if (p.m <= kFewRows) return launch_matmul8_few(p, dtype, sm_count, stream);
     return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, sm_count, stream) : dispatch<SPECA_F32>(p, sm_count, stream);
 }
 
