@@ -136,7 +136,7 @@ struct Matmul8Params {
     uint32_t* gave_up;
 };
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
-constexpr int kFewRows = 64;  // up to here the weights' bytes bound a product, and a kernel of its own reads them
+constexpr int kFewRows = 256;  // up to here the weights' bytes bound a product, and a kernel of its own reads them
 cudaError_t launch_matmul8_few(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
 
 }  // namespace speca

@@ -10,7 +10,7 @@
 //                    from shared memory by the tensor cores themselves they cost 270 cycles of every 2048: 8192 x 8192 x 4096 206 us, 188 without.)
 // Sums alternate between two places in tensor memory, so that the epilogue of a tile runs beside the products of the next.
 // Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
-#include "speca_matmul8_common.cuh"
+#include "speca_matmul8_tensor.cuh"
 
 namespace speca {
 namespace {
@@ -18,7 +18,6 @@ namespace {
 // Four warpgroups of 128 registers a thread at launch; the epilogue's two take 176, the others give up what they take: 2 x 176 + 2 x 80 = 4 x 128.
 constexpr int kThreads = 512;
 constexpr int kLoadWarp = 8, kIssueWarp = 9, kScaleWarp = 12;
-constexpr int kRows = 128;                       // rows of a tile in one SM
 constexpr uint32_t kTmemCols = 512;
 constexpr int kScaleCol = 480;                   // two stages of 16 columns: 4 for A's scales, up to 8 for W's
 constexpr uint32_t kStageOut = 32 * 128;
@@ -54,117 +53,6 @@ struct Smem {
     uint32_t warp_count[kThreads / 32];
     uint16_t live[kMaxTilesM];
 };
-
-// ---- the pair of SMs ----------------------------------------------------------------------------
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The first SM's barrier of this name.
-template <int CG>
-__device__ __forceinline__ uint32_t leaders(uint64_t* bar) {
-    uint32_t a = smem_u32(bar);
-    if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
-    return a;
-}
-// Tells the first SM that this warp's accesses to tensor memory are done. They are (the warp waited for them) and no other memory is
-// handed over, so nothing has to be released: a release to the cluster waits 1200 cycles for the thread's stores.
-template <int CG>
-__device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) {
-        if constexpr (CG == 1)
-            bar_arrive(bar);
-        else
-            asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders<CG>(bar)) : "memory");
-    }
-}
-// Looks, or waits, for arrivals from both SMs. The wait polls: a suspended thread wakes up some hundred cycles late, and between two tiles
-// three of them wait for one another.
-constexpr uint32_t kPollLimit = 1u << 24;  // some tenths of a second
-__device__ __forceinline__ bool pair_test(uint64_t* bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity) {
-    for (uint32_t poll = 0; poll < kPollLimit; ++poll)
-        if (pair_test(bar, parity)) return true;
-    return false;
-}
-__device__ __forceinline__ bool pair_warp_wait(uint64_t* bar, uint32_t parity) {
-    for (uint32_t poll = 0; poll < kPollLimit; ++poll)
-        if (__all_sync(0xffffffffu, pair_test(bar, parity))) return true;
-    return false;
-}
-// A place in a ring.
-template <int N>
-struct Turn {
-    int stage = 0;
-    uint32_t phase = 0;
-    __device__ __forceinline__ void next() {
-        if (++stage == N) stage = 0, phase ^= 1;
-    }
-};
-
-// ---- tensor cores -------------------------------------------------------------------------------
-template <int CG>
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    if constexpr (CG == 1)
-        asm volatile(
-            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-    else
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-                dst),
-            "l"(map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-}
-// Arrives, when all products so far are done, at the barrier of this name in every SM of the tile.
-template <int CG>
-__device__ __forceinline__ void commit(uint64_t* bar) {
-    if constexpr (CG == 1)
-        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
-                     "h"(static_cast<uint16_t>(3))
-                     : "memory");
-}
-// 128 bytes of k a row, with the 128-byte swizzle: 1024 bytes between groups of 8 rows.
-__device__ __forceinline__ uint64_t tile_desc(uint32_t addr) {
-    return static_cast<uint64_t>((addr >> 4) & 0x3fff) | uint64_t(1) << 16 | uint64_t(64) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
-}
-// e4m3 x e4m3 -> fp32, scales of 8-bit exponents. The scale of block i (0 .. 3) is byte i of a column.
-template <int CG, int NT>
-__host__ __device__ constexpr uint32_t mma_desc8(uint32_t i) {
-    return i << 4 | static_cast<uint32_t>(NT >> 3) << 17 | 1u << 23 | static_cast<uint32_t>(kRows * CG >> 4) << 24 | i << 29;
-}
-template <int CG>
-__device__ __forceinline__ void mma8(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, uint32_t scale_a, uint32_t scale_b, uint32_t accumulate) {
-    if constexpr (CG == 1)
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-            " tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-            "l"(a), "l"(b), "r"(desc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
-            : "memory");
-    else
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-            " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-            "l"(a), "l"(b), "r"(desc), "r"(scale_a), "r"(scale_b), "r"(accumulate)
-            : "memory");
-}
 
 // ---- tiles --------------------------------------------------------------------------------------
 struct Part {  // what one launch covers
@@ -502,12 +390,10 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         Place at{0, 0};
         auto fetch = [&] {
             const int a0 = at.m + rank * kRows + lane, w0 = at.n + lane;
-            const uint32_t* sa = reinterpret_cast<const uint32_t*>(p.a_scales + k / 4 * p.a_scale_stride);
-            const uint32_t* sw = reinterpret_cast<const uint32_t*>(p.w_scales + k / 4 * p.w_scale_stride);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) word[j] = a0 + 32 * j < p.m ? __ldg(sa + a0 + 32 * j) : 0x7f7f7f7fu;
+            for (int j = 0; j < 4; ++j) word[j] = scale_word(p.a_scales, p.a_scale_stride, k / 4, a0 + 32 * j, p.m);
 #pragma unroll
-            for (int j = 0; j < 4 * S::kPartsW; ++j) word[4 + j] = w0 + 32 * j < p.n ? __ldg(sw + w0 + 32 * j) : 0x7f7f7f7fu;
+            for (int j = 0; j < 4 * S::kPartsW; ++j) word[4 + j] = scale_word(p.w_scales, p.w_scale_stride, k / 4, w0 + 32 * j, p.n);
         };
         bool ok = true;
         if (tile < n_tiles) {
