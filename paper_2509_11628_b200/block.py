@@ -3,12 +3,14 @@
 The scheduler takes its model from the caller. ``TransformerBlock`` is the block such models are made of -- adaptive
 layer norm, projections, rotary positions with the heads' RMS norm, attention over packed samples, gated
 residuals, MLP -- built from ``speca_layer_modulate``, ``speca_layer_rope`` and ``speca_layer_attention`` with plain
-matrix products in between. ``BlockStack`` runs L of them with random weights as the sampler's model: a full step computes and
+matrix products in between, or, with ``eight=True``, from ``speca_layer_norm8``, ``speca_layer_quantize8`` and
+``speca_layer_matmul8``: weights and the products' inputs in 8 bits, bias, GELU and gated residual in their epilogues. ``BlockStack`` runs L of them with random weights as the sampler's model: a full step computes and
 caches every block's output; a speculative step computes the last block alone, on the forecast of its input, which
 is the fresh feature that verification compares with the forecast of its output. The layer calls skip samples that are not
-active; the products in between run over all rows.
+active, the products in 8 bits among them; plain ones run over all rows.
 
     python -m paper_2509_11628_b200.block        # a sampler run over a small stack, per-step decisions and counts
+    python -m paper_2509_11628_b200.block --eight-bit
 """
 from __future__ import annotations
 
@@ -31,7 +33,7 @@ class TransformerBlock:
     """One block over ``batch`` samples of ``tokens`` tokens. Weights are random; the arithmetic is the block's."""
 
     def __init__(self, batch: int, tokens: int, heads: int, head_dim: int, axis_dims: Sequence[int], dtype: int = S.SPECA_BF16,
-                 device: str = "cuda:0", seed: int = 0, mlp_ratio: int = 4):
+                 device: str = "cuda:0", seed: int = 0, mlp_ratio: int = 4, eight: bool = False):
         self.batch, self.tokens, self.heads, self.head_dim = batch, tokens, heads, head_dim
         self.dim = dim = heads * head_dim
         self.device, tdt = torch.device(device), S._TORCH_DTYPES[dtype]
@@ -53,8 +55,16 @@ class TransformerBlock:
         def rows_of(*shape):
             return torch.zeros(rows, *shape, device=self.device, dtype=tdt)
 
-        self.norm, self.mid, self.attn, self.unit = rows_of(dim), rows_of(dim), rows_of(heads, head_dim), rows_of(dim)
+        self.mid, self.attn = rows_of(dim), rows_of(heads, head_dim)
         self.q, self.k = rows_of(heads, head_dim), rows_of(heads, head_dim)
+        self.eight = eight
+        if eight:  # the products take weights as [outputs, inputs]
+            for name in ("w_qkv", "w_out", "w_up", "w_down"):
+                setattr(self, name, S.quantize8(getattr(self, name).T.contiguous()))
+            self.norm8, self.attn8, self.up8 = (S.Matrix8.empty(rows, n, self.device) for n in (dim, dim, mlp_ratio * dim))
+            self.qkv, self.branch = rows_of(3 * dim), rows_of(dim)
+        else:
+            self.norm, self.unit = rows_of(dim), rows_of(dim)
 
     def __call__(self, x: torch.Tensor, cond: torch.Tensor, positions: torch.Tensor, out: torch.Tensor, active=None) -> torch.Tensor:
         """``out`` [rows, dim] = the block's output for ``x`` [rows, dim] and the conditioning ``cond`` [batch, dim]. Rows of
@@ -62,6 +72,20 @@ class TransformerBlock:
         h, hd, dim = self.heads, self.head_dim, self.dim
         mod = torch.nn.functional.silu(cond) @ self.w_mod                      # [batch, 6 dim]
         shift_a, scale_a, gate_a, shift_m, scale_m, gate_m = mod.split(dim, 1)
+        if self.eight:
+            layer = self.layer
+            layer.norm8(x, self.norm8, S.SPECA_NORM_LAYER, scale=scale_a, shift=shift_a, active=active)
+            layer.matmul8(self.norm8, self.w_qkv, self.qkv, active=active)
+            qkv = self.qkv.view(-1, 3 * h, hd)
+            layer.rope(qkv[:, :h], self.q, qkv[:, h:2 * h], self.k, positions, self.q_norm, self.k_norm, active=active)
+            layer.attention(self.q, self.k, qkv[:, 2 * h:], self.attn, active=active)
+            layer.quantize8(self.attn.view(-1, dim), self.attn8, active=active)
+            layer.matmul8(self.attn8, self.w_out, self.branch, active=active)
+            layer.norm8(x, self.norm8, S.SPECA_NORM_LAYER, branch=self.branch, gate=gate_a, scale=scale_m, shift=shift_m, x_out=self.mid,
+                        active=active)
+            layer.matmul8(self.norm8, self.w_up, self.up8, activation=S.SPECA_ACT_GELU, active=active)
+            layer.matmul8(self.up8, self.w_down, out, residual=self.mid, gate=gate_m, active=active)
+            return out
         self.layer.modulate(x, self.norm, scale=scale_a, shift=shift_a, active=active)
         qkv = (self.norm @ self.w_qkv).view(-1, 3 * h, hd)
         self.layer.rope(qkv[:, :h], self.q, qkv[:, h:2 * h], self.k, positions, self.q_norm, self.k_norm, active=active)
@@ -78,10 +102,10 @@ class BlockStack:
     """L blocks as the model of ``scheduler.run_sampler``; the cached entries are their outputs, verified on the last."""
 
     def __init__(self, blocks: int, batch: int, tokens: int, heads: int, head_dim: int, axis_dims: Sequence[int],
-                 positions: torch.Tensor, dtype: int = S.SPECA_BF16, device: str = "cuda:0", seed: int = 0):
+                 positions: torch.Tensor, dtype: int = S.SPECA_BF16, device: str = "cuda:0", seed: int = 0, eight: bool = False):
         if blocks < 2:
             raise ValueError("a stack needs two blocks: the last one is verified on the forecast of the one before")
-        self.blocks = [TransformerBlock(batch, tokens, heads, head_dim, axis_dims, dtype, device, seed + i) for i in range(blocks)]
+        self.blocks = [TransformerBlock(batch, tokens, heads, head_dim, axis_dims, dtype, device, seed + i, eight=eight) for i in range(blocks)]
         self.batch, self.tokens, self.dim = batch, tokens, heads * head_dim
         self.device, tdt = torch.device(device), S._TORCH_DTYPES[dtype]
         self.positions = positions.repeat(batch, 1).contiguous()
@@ -122,11 +146,16 @@ class BlockStack:
 
 
 def main() -> None:
+    import argparse
+
     from .scheduler import SpecaCacheBackend, run_sampler
+    parser = argparse.ArgumentParser(description="A sampler run over a small stack of transformer blocks with random weights.")
+    parser.add_argument("--eight-bit", action="store_true", help="weights and the products' inputs in 8 bits")
+    args = parser.parse_args()
     device = "cuda:0"
     positions = grid_positions(16, 1, 16, 16, device)
     stack = BlockStack(blocks=6, batch=2, tokens=positions.shape[0], heads=6, head_dim=64, axis_dims=(16, 24, 24),
-                       positions=positions, device=device)
+                       positions=positions, device=device, eight=args.eight_bit)
     cache = S.SpecaCache(stack.entries, stack.batch, 2, S.SPECA_BF16, device)
     stack.backend = backend = SpecaCacheBackend(cache)
     trace = run_sampler(backend, stack, [1.0 - 0.02 * i for i in range(50)], tau0=0.1, beta=0.5, period=5, warm_refs=3,

@@ -164,7 +164,8 @@ speca_status_t speca_layer_matmul8(speca_layer_t* c, int32_t n, int32_t k, const
     if (r.status == SPECA_OK) r = take(w, n, k, &mw);
     if (r.status == SPECA_OK && out_8bit != nullptr) r = take(out_8bit, m, n, &mo);
     if (r.status != SPECA_OK) return fail(c, r.status, "matmul8: %s", r.why);
-    if ((out != nullptr) == (out_8bit != nullptr)) return fail(c, SPECA_ERR_INVALID_ARG, "matmul8: one output is expected, in the layer's type or in 8 bits");
+    if (m > 0 ? (out != nullptr) == (out_8bit != nullptr) : out != nullptr && out_8bit != nullptr)
+        return fail(c, SPECA_ERR_INVALID_ARG, "matmul8: one output is expected, in the layer's type or in 8 bits");
     if (out_8bit != nullptr && (residual != nullptr || gate != nullptr))
         return fail(c, SPECA_ERR_INVALID_ARG, "matmul8: an output in 8 bits takes no residual and no gate");
     for (const speca_matrix8_t* q : {&ma, &mw})

@@ -136,7 +136,15 @@ struct Matmul8Params {
     uint32_t* gave_up;
 };
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
-constexpr int kFewRows = 256;  // up to here the weights' bytes bound a product, and a kernel of its own reads them
+// The kernel for few rows: rows of a tile, and how many blocks share the k of a tile of 128 features (a cluster): as many as let all blocks run
+// at once, two to an SM, each with four stages of 128 at least.
+constexpr int kFewRanks = 8;
+inline int few_rows(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128; }
+inline int few_ranks(int64_t tiles, int k_blocks, int sm_count) {
+    int ranks = 1;
+    while (2 * ranks <= kFewRanks && ranks * tiles <= sm_count && k_blocks >= 8 * ranks) ranks *= 2;
+    return ranks;
+}
 cudaError_t launch_matmul8_few(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
 
 }  // namespace speca

@@ -14,6 +14,7 @@ namespace {
 
 constexpr int kFewThreads = 256;
 constexpr int kLoader = 4, kIssuer = 5;
+constexpr uint32_t kMaxRanks = kFewRanks;
 
 template <int NR>
 struct FewShape {
@@ -58,6 +59,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     }
     const int k_blocks = (p.k + kBlock8 - 1) / kBlock8, share = (k_blocks + ranks - 1) / ranks;
     const int begin = min(static_cast<int>(rank) * share, k_blocks), end = min(begin + share, k_blocks);
+
+    const int first_row = rank + ranks * warp;  // of this warp's epilogue
+    int seq = first_row < rows ? p.row_seq[m0 + first_row] : 0;
 
     int stage = 0;
     uint32_t phase = 0;
@@ -176,26 +180,32 @@ __global__ void __launch_bounds__(kFewThreads, 2)
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t*>(&sm.abort) != 0) atomicExch(p.gave_up, 1u);
-    cluster_sync();
-    // a row for each warp of the cluster in turn: the shares in the order of their ranks
+    if (ranks > 1) cluster_sync();
+    // a row for each warp of the cluster in turn: the shares in the order of their ranks, all asked for at once
     for (int r = rank + ranks * warp; r < rows; r += ranks * 8) {
-        const int row = m0 + r, seq = p.row_seq[row];
-        if (p.dev_mask != nullptr && p.dev_mask[seq] == 0) continue;
+        const int row = m0 + r;
         const uint32_t at = smem_u32(raw) + (r * kRows + 4 * lane) * 4;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (uint32_t q = 0; q < ranks; ++q) {
-            uint32_t there;
-            float x[4];
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(q));
-            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(there) : "memory");
+        float x[kMaxRanks][4], v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += x[e];
+        for (uint32_t q = 0; q < kMaxRanks; ++q) {
+            if (q >= ranks) break;
+            uint32_t there;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(q));
+            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(x[q][0]), "=f"(x[q][1]), "=f"(x[q][2]), "=f"(x[q][3]) : "r"(there) : "memory");
+        }
+        if (r != first_row) seq = p.row_seq[row];
+        if (p.dev_mask != nullptr && p.dev_mask[seq] == 0) continue;
+#pragma unroll
+        for (uint32_t q = 0; q < kMaxRanks; ++q) {
+            if (q >= ranks) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += x[q][e];
         }
         finish_block<DT>(p, row, seq, n0, lane, v);
     }
     __syncwarp();
     __syncthreads();
-    cluster_sync();  // the others may still read this block's sums
+    if (ranks > 1) cluster_sync();  // the others may still read this block's sums
     if (warp == kLoader) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols));
@@ -214,9 +224,7 @@ cudaError_t run_few(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     const int64_t tiles = (static_cast<int64_t>(p.n) + kRows - 1) / kRows * ((p.m + NR - 1) / NR);
     const int k_blocks = (p.k + kBlock8 - 1) / kBlock8;
-    // shares of k: as many as let all blocks run at once, two to an SM, each with two stages at least
-    int ranks = 1;
-    while (ranks < 8 && 2 * ranks * tiles <= 2 * sm_count && k_blocks >= 4 * ranks) ranks *= 2;
+    const int ranks = few_ranks(tiles, k_blocks, sm_count);
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(static_cast<unsigned>(tiles * ranks));
     config.blockDim = dim3(kFewThreads);
@@ -234,10 +242,12 @@ cudaError_t run_few(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
 
 template <int DT>
 cudaError_t dispatch_few(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
-    if (p.m <= 16) return run_few<DT, 16>(p, sm_count, stream);
-    if (p.m <= 32) return run_few<DT, 32>(p, sm_count, stream);
-    if (p.m <= 64) return run_few<DT, 64>(p, sm_count, stream);
-    return run_few<DT, 128>(p, sm_count, stream);
+    switch (few_rows(p.m)) {
+        case 16: return run_few<DT, 16>(p, sm_count, stream);
+        case 32: return run_few<DT, 32>(p, sm_count, stream);
+        case 64: return run_few<DT, 64>(p, sm_count, stream);
+        default: return run_few<DT, 128>(p, sm_count, stream);
+    }
 }
 
 }  // namespace

@@ -10,6 +10,8 @@
 //                    from shared memory by the tensor cores themselves they cost 270 cycles of every 2048: 8192 x 8192 x 4096 206 us, 188 without.)
 // Sums alternate between two places in tensor memory, so that the epilogue of a tile runs beside the products of the next.
 // Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
+#include <algorithm>
+
 #include "speca_matmul8_tensor.cuh"
 
 namespace speca {
@@ -30,7 +32,8 @@ struct Shape {
     static constexpr int kRowsW = NT / CG;       // rows of W that one SM holds
     static constexpr uint32_t kBytesA = kRows * 128, kBytesW = kRowsW * 128, kStage = kBytesA + kBytesW;
     static constexpr int kPartsW = (NT + 127) / 128;
-    static constexpr int kStages = kStage <= 24576 ? 8 : kStage <= 28672 ? 6 : kStage <= 32768 ? 5 : 3;
+    static constexpr int kStages = 5;            // of 32 KB
+    static_assert(kStage == 32768, "128 + 128 rows");
     static constexpr int kCols = NT / 2;         // columns of one epilogue thread
     static_assert(kCols == 64 || kCols == 128, "boxes of 64 or 128 codes");
     // place of the second sums: behind the first, or as far behind as the scales leave room
@@ -179,13 +182,15 @@ __device__ __forceinline__ void stage_row(uint8_t* box, int lane, int first, con
     for (int i = 0; i < N; i += 4)
         *reinterpret_cast<uint4*>(box + box_piece<PITCH>(lane, first + i / 4)) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
 }
-// What the warp staged goes out. By the copy engine, all rows together, which leaves out what lies behind the last row and column; or, where
-// it cannot address the output or a row is not to be written, row by row.
+// What the warp staged goes out. By the copy engine, all rows together, which leaves out what lies behind the last row, and behind the last column
+// in pieces of 16 bytes (what follows a last piece that is cut was overwritten with zeros); or, where it cannot address the output, where
+// a row is not to be written or the last piece is cut, row by row.
 template <typename T, int PITCH>
 __device__ __forceinline__ void send_box(const CUtensorMap* map, bool boxed, const uint8_t* box, T* out, int64_t stride, int c, int n, int row0,
                                          uint32_t live, int lane) {
     if (c >= n) return;
-    if (boxed) {
+    constexpr int kBoxCols = PITCH / static_cast<int>(sizeof(T)), kPiece = 16 / static_cast<int>(sizeof(T));
+    if (boxed && (c + kBoxCols <= n || n % kPiece == 0)) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
@@ -200,7 +205,7 @@ __device__ __forceinline__ void send_box(const CUtensorMap* map, bool boxed, con
         const int r = __ffs(rest) - 1;
         T* to = out + (row0 + r) * stride + c;
 #pragma unroll 1
-        for (int e = lane; e < PITCH / static_cast<int>(sizeof(T)); e += 32) {
+        for (int e = lane; e < kBoxCols; e += 32) {
             const int byte = e * sizeof(T);
             if (c + e < n) to[e] = *reinterpret_cast<const T*>(box + box_piece<PITCH>(r, byte / 16) + byte % 16);
         }
@@ -615,17 +620,37 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
     return cudaSuccess;
 }
 
+// The three kernels' times in us, as fits to what they measured over 1 to 4096 rows, 1152 to 14336 features and elements of k
+// (largest error 25 %; what matters is where they cross). A start, then rounds of tiles over the SMs, each with a step for 128 elements of
+// k and an end. Few rows: bound by the weights' bytes at 6.5 TB/s, or by their steps. In us, rows x features x k, few / one SM / a pair:
+// 1 x 4096 x 4096 8.5 / 13.7 / 15.6;  512 x 4096 x 4096 17.7 / 14.7 / 16.5;  384 x 4096 x 14336 34 / 41 / 45;  768 x 4096 x 14336 56 / 77 / 43;
+// 64 x 4608 x 1152 8.1 / 6.9 / 10.4;  4096 x 14336 x 4096 307 / 265 / 176.
+enum Kind { kFew, kOne, kPair };
+Kind choose(const Matmul8Params& p, int sm_count) {
+    const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
+    auto tiles = [&](int64_t rows, int64_t features) { return (p.m + rows - 1) / rows * ((p.n + features - 1) / features); };
+    auto rounds = [](int64_t n, int64_t places) { return static_cast<double>((n + places - 1) / places); };
+    const int rows = few_rows(p.m);
+    const int64_t few = tiles(rows, kRows), ranks = few_ranks(few, static_cast<int>(kb), sm_count);
+    const double start = rows == 16 ? 6.0 : rows == 32 ? 6.8 : rows == 64 ? 8.0 : 10.5;
+    const double t_few = start + std::max(static_cast<double>(p.n) * p.k / 6.5e6, rounds(few * ranks, 2 * sm_count) * rounds(kb, ranks) * 0.5);
+    const double t_one = 4.2 + rounds(tiles(kRows, 128), sm_count) * (0.7 + 0.29 * kb);
+    const double t_pair = 4.5 + rounds(tiles(2 * kRows, 256), sm_count / 2) * (1.0 + 0.33 * kb);
+    return t_few <= t_one && t_few <= t_pair ? kFew : t_one <= t_pair ? kOne : kPair;
+}
+
 template <int DT>
-cudaError_t dispatch(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
-    return run<DT, 2, 256>(p, sm_count, stream);
+cudaError_t dispatch(const Matmul8Params& p, Kind kind, int sm_count, cudaStream_t stream) {
+    return kind == kOne ? run<DT, 1, 128>(p, sm_count, stream) : run<DT, 2, 256>(p, sm_count, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream) {
     if (p.m == 0) return cudaSuccess;
-    if (p.m <= kFewRows) return launch_matmul8_few(p, dtype, sm_count, stream);
-    return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, sm_count, stream) : dispatch<SPECA_F32>(p, sm_count, stream);
+    const Kind kind = choose(p, sm_count);
+    if (kind == kFew) return launch_matmul8_few(p, dtype, sm_count, stream);
+    return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, kind, sm_count, stream) : dispatch<SPECA_F32>(p, kind, sm_count, stream);
 }
 
 }  // namespace speca
