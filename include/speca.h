@@ -698,7 +698,7 @@ typedef enum { SPECA_ACT_NONE = 0, SPECA_ACT_GELU = 1, SPECA_ACT_SILU = 2 } spec
 /*
  * [rows, dim] of F32 or BF16 into 8 bits: weights, when a model is loaded. Needs no handle, so no mask: all rows are written.
  *   x       device, row stride in elements;  out: host struct, read before the call returns. Codes and scales may not overlap x.
- * Rows of a multiple of 8 elements that start on 16 bytes, with codes on 8, take the vector path.
+ * Rows of a multiple of 16 elements that start on 16 bytes, codes among them, take the vector path.
  * Errors: INVALID_ARG (null, dtype, device), SHAPE, ALIGNMENT, UNSUPPORTED (not an sm_100 device), CUDA.
  */
 speca_status_t speca_quantize8(int64_t rows, int32_t dim, const void* x, int64_t x_stride, int32_t dtype, const speca_matrix8_t* out,

@@ -697,6 +697,7 @@ class Matrix8:
         self.codes, self.scales, self.shape, self.device = codes, scales, codes.shape, codes.device
         self.index = codes.get_device()
         self.desc = Matrix8Desc(codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0))
+        self.ref = ctypes.byref(self.desc)
 
     @classmethod
     def empty(cls, rows: int, dim: int, device="cuda:0") -> "Matrix8":
@@ -725,6 +726,9 @@ def quantize8(x: torch.Tensor, out: Optional[Matrix8] = None, stream=None) -> Ma
     return out
 
 
+_NO_STRIDE, _NO_MODULATIONS = (0,), (None, None, None)
+
+
 class SpecaLayer:
     """The parts of a verification layer that are not plain matrix products, over packed sequences: sequence s of a
     ``[rows, ...]`` tensor is rows ``q_start[s]`` to ``q_start[s + 1] - 1``. Owns the workspace and the handle. Tensors
@@ -748,6 +752,7 @@ class SpecaLayer:
         nbytes = speca_layer_workspace_bytes(q_start, dtype, **kw)
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.handle = speca_layer_create(q_start, dtype, self.workspace, device=self.index, **kw)
+        self.lib = _lib()
 
     def close(self):
         if self.handle:
@@ -838,49 +843,67 @@ class SpecaLayer:
             self._heads(out, "out", self.q_shape), self._vector(kv_len, "kv_len", self.n_seqs, torch.int32),
             self._vector(active, "active", self.n_seqs, torch.uint8), p_lse, self._stream(stream))
 
+    # The 8-bit calls go straight to the library: for a few rows the call costs more than the kernel, so it is kept short.
+
     def _matrix8(self, m, name, shape):
+        """What the library takes for a Matrix8 of this shape."""
         if not isinstance(m, Matrix8):
             raise TypeError("%s: a Matrix8 is expected" % name)
         if m.index != self.index:
             raise TypeError("%s: a matrix on %s is expected" % (name, self.device))
         if m.shape != shape:
             raise ValueError("%s: shape %s is expected, not %s" % (name, tuple(shape), tuple(m.shape)))
-        return m.desc
+        return m.ref
+
+    def _active(self, active):
+        return None if active is None else self._tensor(active, "active", (self.n_seqs,), torch.uint8)[0]
 
     def quantize8(self, x, out, active=None, stream=None):
         """The rows of x in 8 bits."""
-        shape = (self.rows, x.shape[-1])
+        dim = x.shape[-1]
+        shape = (self.rows, dim)
         px, sx = self._tensor(x, "x", shape, self.torch_dtype)
-        speca_layer_quantize8(self.handle, shape[1], px, sx[0], self._vector(active, "active", self.n_seqs, torch.uint8),
-                              self._matrix8(out, "out", shape), self._stream(stream))
+        status = self.lib.speca_layer_quantize8(self.handle, dim, px, sx[0], self._active(active), self._matrix8(out, "out", shape), self._stream(stream))
+        if status:
+            _check_layer(status, self.handle)
 
     def norm8(self, x, out, kind=SPECA_NORM_RMS, branch=None, gate=None, scale=None, shift=None, weight=None, x_out=None, active=None,
               stream=None):
         """x' = x + gate * branch; out = 8 bits of norm(x') * weight * (1 + scale) + shift, the modulations by sequence."""
-        dim, dt = x.shape[-1], self.torch_dtype
+        dim, dt, tensor = x.shape[-1], self.torch_dtype, self._tensor
         shape = (self.rows, dim)
-        px, sx = self._tensor(x, "x", shape, dt)
-        pb, sb = (None, (0,)) if branch is None else self._tensor(branch, "branch", shape, dt)
-        po, so = (None, (0,)) if x_out is None else self._tensor(x_out, "x_out", shape, dt)
-        mods, mod_stride = self._modulations((gate, scale, shift), dim)
-        speca_layer_norm8(self.handle, kind, dim, px, sx[0], pb, sb[0], *mods, mod_stride, self._vector(weight, "weight", dim, dt),
-                          self._vector(active, "active", self.n_seqs, torch.uint8), po, so[0], self._matrix8(out, "out", shape),
-                          self._stream(stream))
+        px, sx = tensor(x, "x", shape, dt)
+        pb, sb = (None, _NO_STRIDE) if branch is None else tensor(branch, "branch", shape, dt)
+        po, so = (None, _NO_STRIDE) if x_out is None else tensor(x_out, "x_out", shape, dt)
+        pw = None if weight is None else tensor(weight, "weight", (dim,), dt)[0]
+        if gate is None and scale is None and shift is None:
+            (pg, ps, pt), mod_stride = _NO_MODULATIONS, 0
+        else:
+            (pg, ps, pt), mod_stride = self._modulations((gate, scale, shift), dim)
+        status = self.lib.speca_layer_norm8(self.handle, kind, dim, px, sx[0], pb, sb[0], pg, ps, pt, mod_stride, pw, self._active(active), po, so[0],
+                                            self._matrix8(out, "out", shape), self._stream(stream))
+        if status:
+            _check_layer(status, self.handle)
 
     def matmul8(self, a, w, out, bias=None, activation=SPECA_ACT_NONE, residual=None, gate=None, active=None, stream=None):
         """out = residual + gate * act(a w^T + bias), the gate by sequence; ``out``: a tensor of the layer's type, or a Matrix8 (which
         takes no residual and no gate)."""
         if not isinstance(w, Matrix8):
             raise TypeError("w: a Matrix8 is expected")
-        (n, k), dt = w.shape, self.torch_dtype
+        (n, k), dt, tensor = w.shape, self.torch_dtype, self._tensor
         shape = (self.rows, n)
-        da, dw = self._matrix8(a, "a", (self.rows, k)), self._matrix8(w, "w", w.shape)
-        eight = self._matrix8(out, "out", shape) if isinstance(out, Matrix8) else None
-        po, so = (None, (0,)) if eight is not None else self._tensor(out, "out", shape, dt)
-        pr, sr = (None, (0,)) if residual is None else self._tensor(residual, "residual", shape, dt)
-        pg, sg = (None, (0,)) if gate is None else self._tensor(gate, "gate", (self.n_seqs, n), dt)
-        speca_layer_matmul8(self.handle, n, k, da, dw, self._vector(bias, "bias", n, dt), activation, pr, sr[0], pg, sg[0],
-                            self._vector(active, "active", self.n_seqs, torch.uint8), po, so[0], eight, self._stream(stream))
+        ra, rw = self._matrix8(a, "a", (self.rows, k)), self._matrix8(w, "w", w.shape)
+        if isinstance(out, Matrix8):
+            eight, po, so = self._matrix8(out, "out", shape), None, _NO_STRIDE
+        else:
+            eight, (po, so) = None, tensor(out, "out", shape, dt)
+        pb = None if bias is None else tensor(bias, "bias", (n,), dt)[0]
+        pr, sr = (None, _NO_STRIDE) if residual is None else tensor(residual, "residual", shape, dt)
+        pg, sg = (None, _NO_STRIDE) if gate is None else tensor(gate, "gate", (self.n_seqs, n), dt)
+        status = self.lib.speca_layer_matmul8(self.handle, n, k, ra, rw, pb, activation, pr, sr[0], pg, sg[0], self._active(active), po, so[0], eight,
+                                              self._stream(stream))
+        if status:
+            _check_layer(status, self.handle)
 
     def check(self, stream=None):
         """Waits for `stream` and raises if a kernel of this layer gave up on a bounded wait."""

@@ -34,9 +34,9 @@ bool vectors8(const Norm8Params& p, size_t e) {
     auto on = [&](const void* q, int64_t stride) {
         return q == nullptr || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && stride * static_cast<int64_t>(e) % 16 == 0);
     };
-    return p.dim % 8 == 0 && on(p.x, p.x_stride) && on(p.branch, p.branch_stride) && on(p.gate, p.mod_stride) &&
+    return p.dim % 16 == 0 && on(p.x, p.x_stride) && on(p.branch, p.branch_stride) && on(p.gate, p.mod_stride) &&
            on(p.scale, p.mod_stride) && on(p.shift, p.mod_stride) && on(p.weight, 0) && on(p.x_out, p.x_out_stride) &&
-           reinterpret_cast<uintptr_t>(p.out.codes) % 8 == 0 && p.out.code_stride % 8 == 0;
+           reinterpret_cast<uintptr_t>(p.out.codes) % 16 == 0 && p.out.code_stride % 16 == 0;
 }
 
 Out8 out8(const speca_matrix8_t& m) {

@@ -117,7 +117,7 @@ struct Norm8Params {
     int32_t centre;  // the mean is taken off
     float eps;
 };
-// `vectors`: rows of a multiple of 8 elements that start on 16 bytes everywhere, and codes on 8
+// `vectors`: rows of a multiple of 16 elements that start on 16 bytes everywhere, codes among them
 cudaError_t launch_norm8(const Norm8Params& p, int dtype, bool vectors, cudaStream_t stream);
 
 struct Matmul8Params {

@@ -2,68 +2,100 @@
 //
 //   z = x + gate * branch;  u = (z - mean) * rsqrt(mean((z - mean)^2) + eps), mean = 0 for the RMS norm
 //   y = u * weight * (1 + scale) + shift;  per 128 elements of y: the scale byte, the codes
-// One pass over memory: the G threads of a row keep it in registers (NV accesses of 8 elements each), 16 lanes share a block of 128,
-// so its largest magnitude takes four shuffles. y is rounded once, to its code. Bound by memory.
+// One pass over memory: the G threads of a row keep it in registers (NV accesses of 16 elements each). Eight lanes share a block of 128,
+// so its largest magnitude takes three shuffles. y is rounded once, to its code. Bound by memory in the end, by instructions and by the blocks that
+// registers leave room for on the way there: 20926 rows x 4096 bf16 with branch, gate and weight 113 us (5.3 TB/s), as they are 49 us (5.2 TB/s); with 8 elements a
+// lane (four shuffles, one scale and one set of addresses for half as much) 210 and 84. Tried and not kept, 20926 x 4096: weight, scale and shift loaded in
+// front of the sums 155 us (registers), bounds on the registers 114 to 146.
 #include "speca_eight_common.cuh"
 #include "speca_rows_common.cuh"
 
 namespace speca {
 namespace {
 
-// Eight elements of a block of 128 that lane l of 16 holds: consecutive ones, as accesses of 16 bytes, or every 16th from l on, one
-// access each, where rows do not start on 16 bytes or hold no multiple of 8.
+constexpr int kPer = 16, kLanes = kBlock8 / kPer;  // elements of an access, lanes of a block
+
+// Sixteen elements of a block of 128 that lane l of 8 holds: consecutive ones, as accesses of 16 bytes; or every 8th from l on, one access
+// each, where rows do not start on 16 bytes or hold no multiple of 16. `at`: the block's first element of the row.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const char* base, int first, int l, int dim, T (&out)[8]) {
+__device__ __forceinline__ void load16(const T* row, int at, int l, int dim, float (&out)[kPer]) {
     if constexpr (VEC) {
         constexpr int E = 16 / sizeof(T);
+        Pack<T, E> v[kPer / E];
 #pragma unroll
-        for (int i = 0; i < 8; i += E) {
-            const Pack<T, E> v = load<T, E>(base, first + 8 * l + i);
+        for (int i = 0; i < kPer / E; ++i) v[i] = *reinterpret_cast<const Pack<T, E>*>(row + at + kPer * l + i * E);
 #pragma unroll
-            for (int e = 0; e < E; ++e) out[i + e] = v.e[e];
-        }
+        for (int i = 0; i < kPer; ++i) out[i] = to_float(v[i / E].e[i % E]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (first + l + 16 * e < dim) out[e] = reinterpret_cast<const T*>(base)[first + l + 16 * e];
+        for (int e = 0; e < kPer; ++e) out[e] = at + l + kLanes * e < dim ? to_float(row[at + l + kLanes * e]) : 0.f;
     }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store8(char* base, int first, int l, int dim, const float (&v)[8]) {
+__device__ __forceinline__ void store16(T* row, int at, int l, int dim, const float (&v)[kPer]) {
     if constexpr (VEC) {
         constexpr int E = 16 / sizeof(T);
 #pragma unroll
-        for (int i = 0; i < 8; i += E) {
+        for (int i = 0; i < kPer; i += E) {
             Pack<T, E> out;
 #pragma unroll
             for (int e = 0; e < E; ++e) out.e[e] = from_float<T>(v[i + e]);
-            store<T, E>(base, first + 8 * l + i, out);
+            *reinterpret_cast<Pack<T, E>*>(row + at + kPer * l + i) = out;
         }
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (first + l + 16 * e < dim) reinterpret_cast<T*>(base)[first + l + 16 * e] = from_float<T>(v[e]);
+        for (int e = 0; e < kPer; ++e)
+            if (at + l + kLanes * e < dim) row[at + l + kLanes * e] = from_float<T>(v[e]);
     }
 }
 
-// One block of 128 of row `row`, 8 values in each of 16 lanes (zeros behind the end), to codes and scale. The whole warp calls.
+// One block of 128 of row `row`, 16 values in each of 8 lanes (zeros behind the end), to codes and scale. The whole warp calls.
 template <bool VEC>
-__device__ __forceinline__ void put8(const Out8& o, int row, int first, int l, int dim, bool write, float (&v)[8]) {
-    const uint32_t byte = scale_byte(block_top<8, 8>(v));
+__device__ __forceinline__ void put16(const Out8& o, int64_t row, int at, int l, int dim, bool write, float (&v)[kPer]) {
+    const uint32_t byte = scale_byte(block_top<kPer, kLanes / 2>(v));
     const float inv = inverse_of(byte);
+    uint32_t w[kPer / 4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= inv;
-    if (!write || first >= dim) return;
-    const uint32_t lo = pack_e4m3(v[0], v[1], v[2], v[3]), hi = pack_e4m3(v[4], v[5], v[6], v[7]);
-    uint8_t* codes = o.codes + row * o.code_stride + first;
+    for (int i = 0; i < kPer / 4; ++i) w[i] = pack_e4m3(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
+    if (!write || at >= dim) return;
+    uint8_t* codes = o.codes + row * o.code_stride + at;
     if constexpr (VEC) {
-        if (first + 8 * l < dim) *reinterpret_cast<uint2*>(codes + 8 * l) = make_uint2(lo, hi);
+        if (at + kPer * l < dim) *reinterpret_cast<uint4*>(codes + kPer * l) = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (first + l + 16 * e < dim) codes[l + 16 * e] = static_cast<uint8_t>((e < 4 ? lo : hi) >> 8 * (e % 4));
+        for (int e = 0; e < kPer; ++e)
+            if (at + l + kLanes * e < dim) codes[l + kLanes * e] = static_cast<uint8_t>(w[e / 4] >> 8 * (e % 4));
     }
-    if (l == 0) o.scales[first / (4 * kBlock8) * o.scale_stride + 4 * static_cast<int64_t>(row) + first / kBlock8 % 4] = static_cast<uint8_t>(byte);
+    if (l == 0) o.scales[at / (4 * kBlock8) * o.scale_stride + 4 * row + at / kBlock8 % 4] = static_cast<uint8_t>(byte);
+}
+
+// Rows as they are: nothing ties a row's blocks of 128 together, so 8 lanes take one after another of all rows' blocks, kBlocks of them at once.
+constexpr int kQuantThreads = 256, kBlocks = 2;
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(kQuantThreads) quantize8_kernel(const __grid_constant__ Norm8Params p, const int64_t total, const int per_row) {
+    using T = typename Type<DT>::T;
+    constexpr int kGroups = kQuantThreads / kLanes;
+    const int l = threadIdx.x % kLanes;
+    const int64_t index = static_cast<int64_t>(blockIdx.x) * (kGroups * kBlocks) + threadIdx.x / kLanes;
+    int64_t row = total <= 0xffffffff ? static_cast<uint32_t>(index) / static_cast<uint32_t>(per_row) : index / per_row;
+    int64_t block = index - row * per_row;
+    float v[kBlocks][kPer];
+    int64_t rows[kBlocks];
+    int at[kBlocks];
+    bool live[kBlocks];
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) {
+        rows[i] = row;
+        at[i] = static_cast<int>(block) * kBlock8;
+        live[i] = row < p.rows && (p.dev_mask == nullptr || p.dev_mask[p.row_seq[row]] != 0);
+        for (block += kGroups; block >= per_row; block -= per_row) ++row;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) v[i][e] = 0.f;
+        if (live[i] && (!VEC || at[i] + kPer * l < p.dim))
+            load16<T, VEC>(reinterpret_cast<const T*>(p.x) + rows[i] * p.x_stride, at[i], l, p.dim, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kBlocks; ++i) put16<VEC>(p.out, rows[i], at[i], l, p.dim, live[i], v[i]);
 }
 
 template <int DT, bool VEC, int NV, int G, int NT>
@@ -71,96 +103,97 @@ __global__ void __launch_bounds__(NT) norm8_kernel(const __grid_constant__ Norm8
     using T = typename Type<DT>::T;
     __shared__ float red[2][NT / 32];
     const int row = blockIdx.x * (NT / G) + threadIdx.x / G;
-    const int t = threadIdx.x % G, l = t % 16;
-    // where the 8 elements of access i begin, and which of them there are
-    auto first = [&](int i) { return (t / 16 + i * (G / 16)) * kBlock8; };
-    auto there = [&](int i, int e) { return first(i) + (VEC ? 8 * l : l + 16 * e) < p.dim; };
+    const int t = threadIdx.x % G, l = t % kLanes;
+    auto at = [&](int i) { return (t / kLanes + i * (G / kLanes)) * kBlock8; };                // block of access i
+    auto some = [&](int i) { return VEC ? at(i) + kPer * l < p.dim : at(i) < p.dim; };         // whether any of it exists
+    auto there = [&](int i, int e) { return VEC ? some(i) : at(i) + l + kLanes * e < p.dim; };
+    auto row_of = [&](const char* base, int64_t i, int64_t stride) { return reinterpret_cast<const T*>(base) + i * stride; };
     bool live = row < p.rows;
     int seq = 0;
-    if (live && p.row_seq != nullptr) {
+    if (live) {
         seq = p.row_seq[row];
         live = p.dev_mask == nullptr || p.dev_mask[seq] != 0;
     }
-    float z[NV][8];
-    float sum = 0.f;
+    float z[NV][kPer];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) z[i][e] = 0.f;
-    auto at = [&](const char* base, int64_t index, int64_t stride) { return base + index * stride * static_cast<int64_t>(sizeof(T)); };
+        for (int e = 0; e < kPer; ++e) z[i][e] = 0.f;
     if (live) {
-        const char* px = at(p.x, row, p.x_stride);
-        T in[NV][8];
+        const T* px = row_of(p.x, row, p.x_stride);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (there(i, 0)) load8<T, VEC>(px, first(i), l, p.dim, in[i]);
+            if (some(i)) load16<T, VEC>(px, at(i), l, p.dim, z[i]);
         if (p.branch != nullptr) {
-            const char* pb = at(p.branch, row, p.branch_stride);
-            T br[NV][8];
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (there(i, 0)) load8<T, VEC>(pb, first(i), l, p.dim, br[i]);
+            const T* pb = row_of(p.branch, row, p.branch_stride);
+            const T* pg = row_of(p.gate, seq, p.mod_stride);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                if (!there(i, 0)) continue;
-                T g[8];
-                if (p.gate != nullptr) load8<T, VEC>(at(p.gate, seq, p.mod_stride), first(i), l, p.dim, g);
+                if (!some(i)) continue;
+                float b[kPer];
+                load16<T, VEC>(pb, at(i), l, p.dim, b);
+                if (p.gate != nullptr) {
+                    float g[kPer];
+                    load16<T, VEC>(pg, at(i), l, p.dim, g);
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (there(i, e)) z[i][e] = fmaf(p.gate != nullptr ? to_float(g[e]) : 1.f, to_float(br[i][e]), to_float(in[i][e]));
+                    for (int e = 0; e < kPer; ++e) z[i][e] = fmaf(g[e], b[e], z[i][e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e) z[i][e] += b[e];
+                }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (there(i, e)) z[i][e] = to_float(in[i][e]);
         }
         if (p.x_out != nullptr) {
-            char* po = p.x_out + row * p.x_out_stride * static_cast<int64_t>(sizeof(T));
+            T* po = reinterpret_cast<T*>(p.x_out) + row * p.x_out_stride;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (there(i, 0)) store8<T, VEC>(po, first(i), l, p.dim, z[i]);
+                if (some(i)) store16<T, VEC>(po, at(i), l, p.dim, z[i]);
         }
     }
-    if (p.norm) {
-        // every thread takes part in the sums: a row's threads may share a barrier with a dead row's
-        if (p.centre) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum += z[i][e];
-            const float mean = sum_row<G>(sum, red[0]) / p.dim;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (there(i, e)) z[i][e] -= mean;
-        }
-        float sq = 0.f;
+    // every thread takes part in the sums: a row's threads may share a barrier with a dead row's
+    if (p.centre) {
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(z[i][e], z[i][e], sq);
-        const float rstd = 1.f / sqrtf(sum_row<G>(sq, red[1]) / p.dim + p.eps);
+            for (int e = 0; e < kPer; ++e) sum += z[i][e];
+        const float mean = sum_row<G>(sum, red[0]) / p.dim;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            T w[8], s[8], b[8];
-            const bool some = live && there(i, 0);
-            if (some && p.weight != nullptr) load8<T, VEC>(p.weight, first(i), l, p.dim, w);
-            if (some && p.scale != nullptr) load8<T, VEC>(at(p.scale, seq, p.mod_stride), first(i), l, p.dim, s);
-            if (some && p.shift != nullptr) load8<T, VEC>(at(p.shift, seq, p.mod_stride), first(i), l, p.dim, b);
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (!live || !there(i, e)) continue;
-                float y = z[i][e] * rstd;
-                if (p.weight != nullptr) y *= to_float(w[e]);
-                z[i][e] = fmaf(y, p.scale != nullptr ? 1.f + to_float(s[e]) : 1.f, p.shift != nullptr ? to_float(b[e]) : 0.f);
+            for (int e = 0; e < kPer; ++e)
+                if (there(i, e)) z[i][e] -= mean;
+    }
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) sq = fmaf(z[i][e], z[i][e], sq);
+    const float rstd = 1.f / sqrtf(sum_row<G>(sq, red[1]) / p.dim + p.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (live && some(i)) {
+            float f[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) z[i][e] *= rstd;
+            if (p.weight != nullptr) {
+                load16<T, VEC>(row_of(p.weight, 0, 0), at(i), l, p.dim, f);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) z[i][e] *= f[e];
+            }
+            if (p.scale != nullptr) {
+                load16<T, VEC>(row_of(p.scale, seq, p.mod_stride), at(i), l, p.dim, f);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) z[i][e] = fmaf(z[i][e], f[e], z[i][e]);
+            }
+            if (p.shift != nullptr) {
+                load16<T, VEC>(row_of(p.shift, seq, p.mod_stride), at(i), l, p.dim, f);
+#pragma unroll
+                for (int e = 0; e < kPer; ++e) z[i][e] += f[e];
             }
         }
+        put16<VEC>(p.out, row, at(i), l, p.dim, live, z[i]);
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) put8<VEC>(p.out, row, first(i), l, p.dim, live, z[i]);
 }
 
 // Rows too long for the registers of one block: passes over memory, the later ones out of L2. A thread meets the same elements in each.
@@ -169,49 +202,47 @@ __global__ void __launch_bounds__(1024) norm8_long_kernel(const __grid_constant_
     using T = typename Type<DT>::T;
     __shared__ float red[2][32];
     const int row = blockIdx.x;
-    const int seq = p.row_seq == nullptr ? 0 : p.row_seq[row];
-    if (p.row_seq != nullptr && p.dev_mask != nullptr && p.dev_mask[seq] == 0) return;
+    const int seq = p.row_seq[row];
+    if (p.dev_mask != nullptr && p.dev_mask[seq] == 0) return;
     auto row_of = [&](const char* base, int64_t i, int64_t stride) { return base == nullptr ? nullptr : reinterpret_cast<const T*>(base) + i * stride; };
     const T *px = row_of(p.x, row, p.x_stride), *pb = row_of(p.branch, row, p.branch_stride), *pw = row_of(p.weight, 0, 0);
     const T *pg = row_of(p.gate, seq, p.mod_stride), *ps = row_of(p.scale, seq, p.mod_stride), *pt = row_of(p.shift, seq, p.mod_stride);
     T* po = p.x_out == nullptr ? nullptr : reinterpret_cast<T*>(p.x_out) + row * p.x_out_stride;
-    const int l = threadIdx.x % 16, start = threadIdx.x / 16 * kBlock8;
+    constexpr int kStep = 1024 / kLanes * kBlock8;
+    const int l = threadIdx.x % kLanes, start = threadIdx.x / kLanes * kBlock8;
     auto value = [&](int c) {
         const float v = to_float(px[c]);
         return pb == nullptr ? v : fmaf(pg == nullptr ? 1.f : to_float(pg[c]), to_float(pb[c]), v);
     };
-    float mean = 0.f, rstd = 1.f;
-    if (p.norm) {
-        if (p.centre) {
-            float sum = 0.f;
-            for (int f = start; f < p.dim; f += 64 * kBlock8)
-                for (int c = f + l; c < min(f + kBlock8, p.dim); c += 16) sum += value(c);
-            mean = sum_row<1024>(sum, red[0]) / p.dim;
-        }
-        float sq = 0.f;
-        for (int f = start; f < p.dim; f += 64 * kBlock8)
-            for (int c = f + l; c < min(f + kBlock8, p.dim); c += 16) {
-                const float d = value(c) - mean;
-                sq = fmaf(d, d, sq);
-            }
-        rstd = 1.f / sqrtf(sum_row<1024>(sq, red[1]) / p.dim + p.eps);
+    float mean = 0.f;
+    if (p.centre) {
+        float sum = 0.f;
+        for (int f = start; f < p.dim; f += kStep)
+            for (int c = f + l; c < min(f + kBlock8, p.dim); c += kLanes) sum += value(c);
+        mean = sum_row<1024>(sum, red[0]) / p.dim;
     }
-    const int last = threadIdx.x / 32 * 2 * kBlock8;  // both blocks of a warp go through the loop together
-    for (int f = start, g = last; g < p.dim; f += 64 * kBlock8, g += 64 * kBlock8) {
-        float v[8];
+    float sq = 0.f;
+    for (int f = start; f < p.dim; f += kStep)
+        for (int c = f + l; c < min(f + kBlock8, p.dim); c += kLanes) {
+            const float d = value(c) - mean;
+            sq = fmaf(d, d, sq);
+        }
+    const float rstd = 1.f / sqrtf(sum_row<1024>(sq, red[1]) / p.dim + p.eps);
+    // the blocks of a warp go through the loop together
+    for (int f = start, first = threadIdx.x / 32 * (32 / kLanes) * kBlock8; first < p.dim; f += kStep, first += kStep) {
+        float v[kPer];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int c = f + l + 16 * e;
+        for (int e = 0; e < kPer; ++e) {
+            const int c = f + l + kLanes * e;
             v[e] = 0.f;
             if (c >= p.dim) continue;
             v[e] = value(c);
             if (po != nullptr) po[c] = from_float<T>(v[e]);
-            if (!p.norm) continue;
             float y = (v[e] - mean) * rstd;
             if (pw != nullptr) y *= to_float(pw[c]);
             v[e] = fmaf(y, ps == nullptr ? 1.f : 1.f + to_float(ps[c]), pt == nullptr ? 0.f : to_float(pt[c]));
         }
-        put8<false>(p.out, row, f, l, p.dim, true, v);
+        put16<false>(p.out, row, f, l, p.dim, true, v);
     }
 }
 
@@ -223,14 +254,26 @@ void run_norm8(const Norm8Params& p, cudaStream_t stream) {
 
 template <int DT, bool VEC>
 void dispatch_norm8(const Norm8Params& p, cudaStream_t stream) {
-    const int n = (p.dim + kBlock8 - 1) / kBlock8 * 16;  // accesses per row: 16 lanes a block
-    if (n <= 32 * 2) return run_norm8<DT, VEC, 2, 32, 128>(p, stream);
-    if (n <= 64 * 2) return run_norm8<DT, VEC, 2, 64, 128>(p, stream);
-    if (n <= 128 * 2) return run_norm8<DT, VEC, 2, 128, 128>(p, stream);
-    if (n <= 128 * 3) return run_norm8<DT, VEC, 3, 128, 128>(p, stream);
-    if (n <= 128 * 5) return run_norm8<DT, VEC, 5, 128, 128>(p, stream);
-    if (n <= 256 * 4) return run_norm8<DT, VEC, 4, 256, 256>(p, stream);
-    if (n <= 512 * 4) return run_norm8<DT, VEC, 4, 512, 512>(p, stream);
+    const int per_row = (p.dim + kBlock8 - 1) / kBlock8;
+    if (!p.norm) {
+        constexpr int per = kQuantThreads / kLanes * kBlocks;
+        const int64_t total = static_cast<int64_t>(p.rows) * per_row;
+        quantize8_kernel<DT, VEC><<<static_cast<unsigned>((total + per - 1) / per), kQuantThreads, 0, stream>>>(p, total, per_row);
+        return;
+    }
+    // One access a thread as long as a block has threads for the row: of 4096 elements 256 threads x 1 took 113 us with branch and gate (20926 rows),
+    // 128 x 2 took 125; of 1152, 96 x 1 39 us with the branch, 32 x 3 47. Behind 6144 two: 8192 as 256 x 2 94 us (8345 rows), 512 x 1 111.
+    const int n = per_row * kLanes;  // accesses of a row
+    if (n <= 32) return run_norm8<DT, VEC, 1, 32, 128>(p, stream);
+    if (n <= 64) return run_norm8<DT, VEC, 1, 64, 128>(p, stream);
+    if (n <= 96) return run_norm8<DT, VEC, 1, 96, 96>(p, stream);
+    if (n <= 128) return run_norm8<DT, VEC, 1, 128, 128>(p, stream);
+    if (n <= 192) return run_norm8<DT, VEC, 1, 192, 192>(p, stream);
+    if (n <= 256) return run_norm8<DT, VEC, 1, 256, 256>(p, stream);
+    if (n <= 320) return run_norm8<DT, VEC, 1, 320, 320>(p, stream);
+    if (n <= 384) return run_norm8<DT, VEC, 1, 384, 384>(p, stream);
+    if (n <= 512) return run_norm8<DT, VEC, 2, 256, 256>(p, stream);
+    if (n <= 512 * 2) return run_norm8<DT, VEC, 2, 512, 512>(p, stream);
     norm8_long_kernel<DT><<<p.rows, 1024, 0, stream>>>(p);
 }
 

@@ -104,7 +104,7 @@ def test_quantize_and_norm_refuse(S, lib, dtype):
     assert lib.host_norms() == before
     # and what is fine: which rows take 16 bytes at once
     for kw, vectors in [({}, 1), (dict(x=A + size), 0), (dict(out=(B + 4, DIM, C, 4 * ROWS)), 0), (dict(out=(B, DIM + 4, C, 4 * ROWS)), 0),
-                        (dict(dim=DIM - 4, out=(B, DIM, C, 4 * ROWS)), 0), (dict(x_stride=0), 1), (dict(out=(B, DIM, C, 4 * ROWS + 64)), 1)]:
+                        (dict(dim=DIM - 8, out=(B, DIM, C, 4 * ROWS)), 0), (dict(x_stride=0), 1), (dict(out=(B, DIM, C, 4 * ROWS + 64)), 1)]:
         assert quantize(S, lib, layer, **kw) == S.SPECA_OK and lib.host_vectors() == vectors, kw
         assert norm(S, lib, layer, **kw) == S.SPECA_OK and lib.host_vectors() == vectors, kw
     assert norm(S, lib, layer, weight=D + size) == S.SPECA_OK and lib.host_vectors() == 0
