@@ -211,8 +211,13 @@ speca_status_t speca_layer_matmul8(speca_layer_t* c, int32_t n, int32_t k, const
     p.gate_stride = gate_stride;
     p.out_stride = out_stride;
     p.act = activation;
-    const bool out_on = out != nullptr ? on_16(c, out, out_stride, 0) : reinterpret_cast<uintptr_t>(mo.codes) % 16 == 0 && mo.code_stride % 16 == 0;
-    p.vectors = out_on && on_16(c, bias, 0, 0) && on_16(c, residual, residual_stride, 0) && on_16(c, gate, gate_stride, 0);
+    auto out_on = [&](int64_t bytes) {
+        const void* rows = out != nullptr ? out : mo.codes;
+        const int64_t stride = out != nullptr ? out_stride * static_cast<int64_t>(elem_size(c)) : mo.code_stride;
+        return reinterpret_cast<uintptr_t>(rows) % bytes == 0 && stride % bytes == 0;
+    };
+    p.vectors = out_on(16) && on_16(c, bias, 0, 0) && on_16(c, residual, residual_stride, 0) && on_16(c, gate, gate_stride, 0);
+    p.wide = out_on(32);
     p.gave_up = reinterpret_cast<uint32_t*>(c->ws + c->gave_up_off);
     DeviceGuard guard(c->device);
     if (!guard.ok) return fail(c, SPECA_ERR_CUDA, "cudaSetDevice failed");

@@ -132,6 +132,7 @@ struct Matmul8Params {
     int64_t residual_stride, gate_stride, out_stride;  // elements
     int32_t act;
     int32_t vectors;  // rows of bias, residual, gate and out (or the codes) start on 16 bytes
+    int32_t wide;     // those of the codes on 32
     int32_t boxes;    // the copy engine can address the output (set by the launch)
     uint32_t* gave_up;
 };

@@ -182,26 +182,12 @@ __device__ __forceinline__ void stage_row(uint8_t* box, int lane, int first, con
     for (int i = 0; i < N; i += 4)
         *reinterpret_cast<uint4*>(box + box_piece<PITCH>(lane, first + i / 4)) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
 }
-// What the warp staged goes out. By the copy engine, all rows together, which leaves out what lies behind the last row, and behind the last column
-// in pieces of 16 bytes (what follows a last piece that is cut was overwritten with zeros); or, where it cannot address the output, where
-// a row is not to be written or the last piece is cut, row by row.
+// What the warp staged goes out, row by row.
 template <typename T, int PITCH>
-__device__ __forceinline__ void send_box(const CUtensorMap* map, bool boxed, const uint8_t* box, T* out, int64_t stride, int c, int n, int row0,
-                                         uint32_t live, int lane) {
-    if (c >= n) return;
-    constexpr int kBoxCols = PITCH / static_cast<int>(sizeof(T)), kPiece = 16 / static_cast<int>(sizeof(T));
-    if (boxed && (c + kBoxCols <= n || n % kPiece == 0)) {
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-            asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c), "r"(row0), "r"(smem_u32(box))
-                         : "memory");
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        }
-        return;
-    }
+__device__ __forceinline__ void write_box(const uint8_t* box, T* out, int64_t stride, int c, int n, int row0, uint32_t live, int lane) {
+    constexpr int kBoxCols = PITCH / static_cast<int>(sizeof(T));
     __syncwarp();
-    for (uint32_t rest = live; rest != 0; rest &= rest - 1) {
+    for (uint32_t rest = c < n ? live : 0; rest != 0; rest &= rest - 1) {
         const int r = __ffs(rest) - 1;
         T* to = out + (row0 + r) * stride + c;
 #pragma unroll 1
@@ -212,10 +198,39 @@ __device__ __forceinline__ void send_box(const CUtensorMap* map, bool boxed, con
     }
     __syncwarp();
 }
+// The same by the copy engine, all rows together. It leaves out what lies behind the last row, and behind the last column in pieces of 16 bytes
+// (what follows a last piece that is cut was overwritten with zeros): so not where it cannot address the output, where a row is not to be written or
+// the last piece is cut.
+template <typename T>
+__device__ __forceinline__ void send_box(const CUtensorMap* map, bool boxed, const uint8_t* box, T* out, int64_t stride, int c, int n, int row0,
+                                         uint32_t live, int lane) {
+    constexpr int kBoxCols = 128 / static_cast<int>(sizeof(T)), kPiece = 16 / static_cast<int>(sizeof(T));
+    if (!boxed || (c + kBoxCols > n && n % kPiece != 0)) return write_box<T, 128>(box, out, stride, c, n, row0, live, lane);
+    if (c >= n) return;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(c), "r"(row0), "r"(smem_u32(box))
+                     : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+}
 // The box has been read out of shared memory.
 __device__ __forceinline__ void box_read(int lane) {
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     __syncwarp();
+}
+
+// 32 bytes at once (a whole sector) where rows start on 32.
+__device__ __forceinline__ void store32(uint8_t* to, const uint32_t (&w)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                     "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
 }
 
 // Largest finite magnitude of a lane's 32 values; infinities become NaN.
@@ -438,7 +453,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             const int row = at.m + rank * kRows + r, row0 = row - lane, n0 = at.n + half * S::kCols;
             bool live = row < p.m;
             int seq = 0;
-            if (live) {
+            if (live && (masked || E == kResidual)) {
                 seq = p.row_seq[row];
                 live = !masked || p.dev_mask[seq] != 0;
             }
@@ -523,7 +538,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                     if (j % kPer == 0) box_read(lane);
                     stage_row<128>(box, lane, chunk(j) / 32 % kPer * 4, w);
                     if (j % kPer == kPer - 1)
-                        send_box<T, 128>(&map_out, boxed, box, reinterpret_cast<T*>(p.out), p.out_stride, n0 + chunk(j) / (32 * kPer) * (32 * kPer), p.n,
+                        send_box<T>(&map_out, boxed, box, reinterpret_cast<T*>(p.out), p.out_stride, n0 + chunk(j) / (32 * kPer) * (32 * kPer), p.n,
                                          row0, lives, lane);
                 }
             }
@@ -542,16 +557,21 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 if (live && n0 % kBlock8 == 0 && n0 < p.n)
                     p.out8.scales[n0 / (4 * kBlock8) * p.out8.scale_stride + 4 * static_cast<int64_t>(row) + n0 / kBlock8 % 4] =
                         static_cast<uint8_t>(byte);
-                box_read(lane);
+                // each lane writes its row's codes, 32 bytes at once; where it cannot, through the box, row by row. (Through the copy engine, whose fence
+                // waits some hundred cycles, 8192 x 8192 x 1152 with GELU took 107 us, 101 so.)
+                const bool direct = p.vectors && n0 + S::kCols <= p.n;
 #pragma unroll 1
                 for (int j = 0; j < kChunks; ++j) {
                     if (j > 0) load_chunk(j, held);
                     if (j == kChunks - 1) hand_over<CG>(&sm.sums_free[b], lane);
                     uint32_t w[8];
                     pack_codes(held, inv, w);
-                    stage_row<S::kCols>(box, lane, chunk(j) / 16, w);
+                    if (!direct)
+                        stage_row<S::kCols>(box, lane, chunk(j) / 16, w);
+                    else if (live)
+                        store32(p.out8.codes + row * p.out8.code_stride + n0 + chunk(j), w, p.wide);
                 }
-                send_box<uint8_t, S::kCols>(&map_out, boxed, box, p.out8.codes, p.out8.code_stride, n0, p.n, row0, lives, lane);
+                if (!direct) write_box<uint8_t, S::kCols>(box, p.out8.codes, p.out8.code_stride, n0, p.n, row0, lives, lane);
             }
             if (b == 1) phase ^= 1;
             b ^= 1;
@@ -573,18 +593,13 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     }
 }
 
-// The output as boxes of 32 rows: of 128 bytes in the layer's type, of what an epilogue thread has in 8 bits.
-bool encode_out(CUtensorMap* map, const Matmul8Params& p, int elem, int code_cols) {
-    const bool eight = p.out == nullptr;
-    void* base = eight ? p.out8.codes : reinterpret_cast<uint8_t*>(p.out);
+// An output in the layer's type as boxes of 32 rows of 128 bytes.
+bool encode_out(CUtensorMap* map, const Matmul8Params& p, int elem) {
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.n), static_cast<cuuint64_t>(p.m)};
-    const int64_t stride = eight ? p.out8.code_stride : p.out_stride * elem;
-    const cuuint64_t strides[1] = {p.m > 1 ? static_cast<cuuint64_t>(stride) : 128};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(eight ? code_cols : 128 / elem), 32}, ones[2] = {1, 1};
-    const int width = eight ? code_cols : 128;
-    return encoder()(map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
-                     2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                     width == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+    const cuuint64_t strides[1] = {p.m > 1 ? static_cast<cuuint64_t>(p.out_stride) * elem : 128};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / elem), 32}, ones[2] = {1, 1};
+    return encoder()(map, elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p.out, dims, strides, box, ones,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -594,7 +609,7 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
     if (encoder() == nullptr) return cudaErrorNotSupported;
     CUtensorMap a, w, out = {};
     if (!encode8(&a, p.a, p.k, p.m, p.a_stride, kRows) || !encode8(&w, p.w, p.k, p.n, p.w_stride, S::kRowsW)) return cudaErrorNotSupported;
-    p.boxes = p.vectors && encode_out(&out, p, Type<DT>::kBytes, S::kCols);
+    p.boxes = p.vectors && p.out != nullptr && encode_out(&out, p, Type<DT>::kBytes);
     constexpr uint32_t smem = sizeof(Smem<CG, NT>);
     static_assert(smem <= 232448 && smem > 116224, "fits one SM, and no two blocks share one (tensor memory)");
     const auto kernel = p.out == nullptr                                  ? matmul8_tc_kernel<DT, CG, NT, kEight>
