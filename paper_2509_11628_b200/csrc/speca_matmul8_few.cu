@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         if (elect_one()) {
             Turn<2> held;
             for (int kb = begin; kb < end; ++kb) {
-                if (kb == begin || kb % 4 == 0) ok = pair_wait(&sm.scales_full[held.stage], held.phase);
-                ok = ok && pair_wait(&sm.full[stage], phase);
+                if (kb == begin || kb % 4 == 0) ok = pair_wait<1>(&sm.scales_full[held.stage], held.phase);
+                ok = ok && pair_wait<1>(&sm.full[stage], phase);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t from = smem_u32(sm.tiles[stage]), scales = tmem + S::kScales + held.stage * 8;
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         const uint32_t first = tmem + (static_cast<uint32_t>(warp * 32) << 16);
         if (begin < end) fetch(begin / 4);
         for (int kb = begin; kb < end; kb = kb / 4 * 4 + 4) {
-            ok = pair_warp_wait(&sm.scales_used[to.stage], to.phase ^ 1);
+            ok = pair_warp_wait<1>(&sm.scales_used[to.stage], to.phase ^ 1);
             if (!ok) break;
             tc_fence_after();
             tmem_store4(first + S::kScales + to.stage * 8, word);
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         // ---- the sums, one feature a lane: [row][feature] where the tiles were ----
         float* const sums = reinterpret_cast<float*>(raw);
         static_assert(NR * kRows * 4 <= sizeof(sm.tiles), "room");
-        ok = pair_warp_wait(&sm.sums_full, 0) && ok;
+        ok = pair_warp_wait<1>(&sm.sums_full, 0) && ok;
         if (ok) {
             tc_fence_after();
 #pragma unroll 1

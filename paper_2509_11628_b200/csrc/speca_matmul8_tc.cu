@@ -9,6 +9,13 @@
 //   warps 12-15      scales: of 512 elements of k at once, through registers into every quarter of the lanes of tensor memory. (Copied there
 //                    from shared memory by the tensor cores themselves they cost 270 cycles of every 2048: 8192 x 8192 x 4096 206 us, 188 without.)
 // Sums alternate between two places in tensor memory, so that the epilogue of a tile runs beside the products of the next.
+//
+// What bounds it: a step of 128 elements of k is 512 cycles of the tensor pipe in a pair (256 x 256) and brings 32 KB into each SM, which takes as
+// long (an SM got 90 to 110 GB/s from L2 in every shape tried, 50 to 58 bytes a cycle); tiles of one SM (128 x 128) read as much for half the
+// products. Between tiles some 1300 cycles pass while the last sums are read. In a loop the card runs into its power limit (1000 W, 1.4 GHz).
+// Measured, e4m3 with bf16 out: 4096 x 4608 x 1152 22.7 us (1.92 PFLOP/s), 8352 x 14336 x 4096 357 us in a short run (2.74), 408 in a loop (2.41; a library's
+// block-scaled product 385), 8192^3 434 in a loop (2.53; 459), 20928 x 16384 x 4096 1130 in a loop (2.49; 1260). Short k with an activation is bound by the
+// epilogue: 4096 x 4608 x 1152 with bias and GELU into 8 bits 30 us, three quarters of it the special function unit's 1.5 results an element.
 // Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
 #include <algorithm>
 
@@ -366,19 +373,19 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
             bool ok = true, ready = false;
             for (int i = first_tile; i < n_tiles && ok; i += step) {
                 const int b = sums_at.stage;
-                ok = pair_wait(&sm.sums_free[b], sums_at.phase ^ 1);
+                ok = pair_wait<CG>(&sm.sums_free[b], sums_at.phase ^ 1);
                 if (S::kOverlap && i != first_tile && ok) {
-                    ok = pair_wait(&sm.overlap_free[b ^ 1], overlap_phase[b ^ 1]);
+                    ok = pair_wait<CG>(&sm.overlap_free[b ^ 1], overlap_phase[b ^ 1]);
                     overlap_phase[b ^ 1] ^= 1;
                 }
                 const uint32_t sums = tmem + b * S::kSecond;
                 for (int k = 0; k < k_blocks && ok; ++k) {
-                    if (k % 4 == 0) ok = pair_wait(&sm.scales_full[held.stage], held.phase);
-                    ok = ok && (ready || pair_wait(&sm.full[at.stage], at.phase));
+                    if (k % 4 == 0) ok = pair_wait<CG>(&sm.scales_full[held.stage], held.phase);
+                    ok = ok && (ready || pair_wait<CG>(&sm.full[at.stage], at.phase));
                     if (!ok) break;
                     const int stage = at.stage;
                     at.next();
-                    ready = pair_test(&sm.full[at.stage], at.phase);
+                    ready = pair_test<CG>(&sm.full[at.stage], at.phase);
                     tc_fence_after();
                     const uint32_t from = smem_u32(sm.tiles[stage]), scales = tmem + kScaleCol + held.stage * 16;
                     const uint64_t a = tile_desc(from), w = tile_desc(from + S::kBytesA);
@@ -422,7 +429,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         }
         const uint32_t first = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16) + kScaleCol;
         while (tile < n_tiles) {
-            ok = pair_warp_wait(&sm.scales_used[to.stage], to.phase ^ 1);
+            ok = pair_warp_wait<CG>(&sm.scales_used[to.stage], to.phase ^ 1);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -485,7 +492,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                 if (one_gate) stage_columns<T, S::kCols>(sm.columns[warp][1], reinterpret_cast<const T*>(p.gate) + s * p.gate_stride, n0, p.n, lane);
                 ask(0);
             }
-            ok = pair_warp_wait(&sm.sums_full[b], phase);
+            ok = pair_warp_wait<CG>(&sm.sums_full[b], phase);
             if (!ok) break;
             tc_fence_after();
             [[maybe_unused]] float held[32], top = 0.f;
@@ -638,19 +645,21 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
 // The three kernels' times in us, as fits to what they measured over 1 to 4096 rows, 1152 to 14336 features and elements of k
 // (largest error 25 %; what matters is where they cross). A start, then rounds of tiles over the SMs, each with a step for 128 elements of
 // k and an end. Few rows: bound by the weights' bytes at 6.5 TB/s, or by their steps. In us, rows x features x k, few / one SM / a pair:
-// 1 x 4096 x 4096 8.5 / 13.7 / 15.6;  512 x 4096 x 4096 17.7 / 14.7 / 16.5;  384 x 4096 x 14336 34 / 41 / 45;  768 x 4096 x 14336 56 / 77 / 43;
-// 64 x 4608 x 1152 8.1 / 6.9 / 10.4;  4096 x 14336 x 4096 307 / 265 / 176.
+// 1 x 4096 x 4096 8.5 / 12.6 / 15.6;  512 x 4096 x 4096 17.7 / 13.3 / 16.6;  384 x 4096 x 14336 34 / 40 / 41;  1024 x 4096 x 14336 63 / 73 / 48;
+// 64 x 4608 x 1152 8.1 / 6.9 / 8.8;  4096 x 1152 x 4608 30 / 27 / 30;  4096 x 14336 x 4096 307 / 252 / 180.
+// A mask, which only the device knows, is taken to leave three rows of four: of 16 samples of 256 rows, 11 of them active, x 1152 x 4608 a pair's
+// tiles fill one round in place of two.
 enum Kind { kFew, kOne, kPair };
 Kind choose(const Matmul8Params& p, int sm_count) {
-    const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
-    auto tiles = [&](int64_t rows, int64_t features) { return (p.m + rows - 1) / rows * ((p.n + features - 1) / features); };
+    const int64_t kb = (p.k + kBlock8 - 1) / kBlock8, m = p.dev_mask != nullptr ? p.m - p.m / 4 : p.m;
+    auto tiles = [&](int64_t rows, int64_t features) { return (m + rows - 1) / rows * ((p.n + features - 1) / features); };
     auto rounds = [](int64_t n, int64_t places) { return static_cast<double>((n + places - 1) / places); };
     const int rows = few_rows(p.m);
     const int64_t few = tiles(rows, kRows), ranks = few_ranks(few, static_cast<int>(kb), sm_count);
     const double start = rows == 16 ? 6.0 : rows == 32 ? 6.8 : rows == 64 ? 8.0 : 10.5;
     const double t_few = start + std::max(static_cast<double>(p.n) * p.k / 6.5e6, rounds(few * ranks, 2 * sm_count) * rounds(kb, ranks) * 0.5);
-    const double t_one = 4.2 + rounds(tiles(kRows, 128), sm_count) * (0.7 + 0.29 * kb);
-    const double t_pair = 4.5 + rounds(tiles(2 * kRows, 256), sm_count / 2) * (1.0 + 0.33 * kb);
+    const double t_one = 4.2 + rounds(tiles(kRows, 128), sm_count) * (0.7 + 0.27 * kb);
+    const double t_pair = 4.5 + rounds(tiles(2 * kRows, 256), sm_count / 2) * (1.0 + 0.34 * kb);
     return t_few <= t_one && t_few <= t_pair ? kFew : t_one <= t_pair ? kOne : kPair;
 }
 

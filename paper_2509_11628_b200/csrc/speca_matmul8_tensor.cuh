@@ -36,34 +36,46 @@ __device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
             asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(leaders<CG>(bar)) : "memory");
     }
 }
-// Looks, or waits, for arrivals from both SMs. One thread's wait polls: a suspended one wakes up some hundred cycles late.
+// Looks, or waits, for arrivals: from both SMs where there are two. One thread's wait polls: a suspended one wakes up some hundred cycles late.
 constexpr uint32_t kPollLimit = 1u << 24;  // some tenths of a second
+template <int CG>
 __device__ __forceinline__ bool pair_test(uint64_t* bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile(
-        "{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
+    if constexpr (CG == 1)
+        asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok)
+                     : "r"(smem_u32(bar)), "r"(parity)
+                     : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok)
+                     : "r"(smem_u32(bar)), "r"(parity)
+                     : "memory");
     return ok != 0;
 }
+template <int CG>
 __device__ __forceinline__ bool pair_wait(uint64_t* bar, uint32_t parity) {
     for (uint32_t poll = 0; poll < kPollLimit; ++poll)
-        if (pair_test(bar, parity)) return true;
+        if (pair_test<CG>(bar, parity)) return true;
     return false;
 }
 // A whole warp suspends: where eight or twelve of them polled beside the products, large ones ran 1.3 % slower (power).
+template <int CG>
 __device__ __forceinline__ bool pair_warp_wait(uint64_t* bar, uint32_t parity) {
-    for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
-        uint32_t ok;
-        asm volatile(
-            "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (__all_sync(0xffffffffu, ok != 0)) return true;
+    if constexpr (CG == 1) {
+        return warp_wait(bar, parity);
+    } else {
+        for (uint32_t spin = 0; spin < kSpinLimit; ++spin) {
+            uint32_t ok;
+            asm volatile(
+                "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                : "=r"(ok)
+                : "r"(smem_u32(bar)), "r"(parity)
+                : "memory");
+            if (__all_sync(0xffffffffu, ok != 0)) return true;
+        }
+        return false;
     }
-    return false;
 }
 // A place in a ring.
 template <int N>
