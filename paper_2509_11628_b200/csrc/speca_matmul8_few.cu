@@ -5,7 +5,10 @@
 // some 100 KB each on its way from memory (a ring of stages of 128 elements of k, filled by the copy engine).
 //   warps 0-3  scales into tensor memory, a quarter of the lanes each; then the sums into shared memory
 //   warp 4     loads;  warp 5: issues the products;  all eight: the epilogue, a row at a time
-// Every wait is bounded, as in the kernel for many rows. (With mma.sync in place of the tensor memory's products, 8 rows by 14336 x 4096 took
+// Every wait is bounded, as in the kernel for many rows.
+// Measured: weights stream at 6.7 TB/s behind a start and an end of 6 us together (of which an empty launch is 2.5): 1 row x 4096 x 4096 8.2 us, 14336 x 4096
+// 14.7, 64 rows 10.0 and 17.1. Tried and not kept: shares sent to the row's block instead of fetched by it (equal or slower), one block an SM with
+// twice the stages (17 us for 4096 x 4096 of two shares, 8 us as it is). (With mma.sync in place of the tensor memory's products, 8 rows by 14336 x 4096 took
 // 17 us and 32 rows 37.)
 #include "speca_matmul8_tensor.cuh"
 

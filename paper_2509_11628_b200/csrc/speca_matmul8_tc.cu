@@ -658,7 +658,8 @@ Kind choose(const Matmul8Params& p, int sm_count) {
     const int64_t few = tiles(rows, kRows), ranks = few_ranks(few, static_cast<int>(kb), sm_count);
     const double start = rows == 16 ? 6.0 : rows == 32 ? 6.8 : rows == 64 ? 8.0 : 10.5;
     const double t_few = start + std::max(static_cast<double>(p.n) * p.k / 6.5e6, rounds(few * ranks, 2 * sm_count) * rounds(kb, ranks) * 0.5);
-    const double t_one = 4.2 + rounds(tiles(kRows, 128), sm_count) * (0.7 + 0.27 * kb);
+    // (tiles of one SM with 16 rows or fewer took half as long again: 22 us for 14336 x 4096, 15.4 from 32 rows on)
+    const double t_one = 4.2 + rounds(tiles(kRows, 128), sm_count) * (0.7 + (rows == 16 ? 0.45 : 0.27) * kb);
     const double t_pair = 4.5 + rounds(tiles(2 * kRows, 256), sm_count / 2) * (1.0 + 0.34 * kb);
     return t_few <= t_one && t_few <= t_pair ? kFew : t_one <= t_pair ? kOne : kPair;
 }
