@@ -692,7 +692,8 @@ typedef struct {
 } speca_matrix8_t;
 
 typedef enum { SPECA_NORM_LAYER = 0, SPECA_NORM_RMS = 1 } speca_norm_t;
-/* GELU is the tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))); SILU is x / (1 + exp(-x)). */
+/* GELU is the tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))); SILU is x / (1 + exp(-x)). A factor of x below 2^-63 may be taken
+ * as 2^-63. */
 typedef enum { SPECA_ACT_NONE = 0, SPECA_ACT_GELU = 1, SPECA_ACT_SILU = 2 } speca_activation_t;
 
 /*
@@ -734,8 +735,8 @@ speca_status_t speca_layer_norm8(speca_layer_t* layer, int32_t kind, int32_t dim
  *                 same stride.  gate: [n_seqs, n], row stride gate_stride, or NULL (1).
  *   out, out_8bit exactly one of them; nothing else may overlap the output. residual and gate go with out alone.
  * Rows of inactive sequences are not written, and tiles of rows that hold no others are not computed. A NaN (code 0x7f or 0xff, or a scale byte
- * of 255) makes its row or column of the product NaN. Results do not depend on the mask or on the launch: no atomics on values, a fixed
- * order of sums.
+ * of 255) makes its row or column of the product NaN. A row's result does not depend on the mask: no atomics on values, an order of sums that the
+ * sizes fix (the number of rows among them: k is shared out where there are few).
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, UNSUPPORTED (a stride of 2^40 bytes or more), CUDA.
  */
 speca_status_t speca_layer_matmul8(speca_layer_t* layer, int32_t n, int32_t k, const speca_matrix8_t* a, const speca_matrix8_t* w,

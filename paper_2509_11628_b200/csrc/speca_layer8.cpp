@@ -124,6 +124,8 @@ speca_status_t speca_layer_norm8(speca_layer_t* c, int32_t kind, int32_t dim, co
         for (const void* q : {static_cast<const void*>(x_out), branch, gate, scale, shift, weight})
             if (q != nullptr && (q == p.out.codes || q == p.out.scales))
                 return fail(c, SPECA_ERR_INVALID_ARG, "norm8: the 8-bit output overlaps another tensor");
+    if (c->total_q > 0 && x_out != nullptr && (x_out == gate || x_out == scale || x_out == shift || x_out == weight))
+        return fail(c, SPECA_ERR_INVALID_ARG, "norm8: x_out overlaps a modulation or the weight");
     if (!on_elements(c, branch) || !on_elements(c, gate) || !on_elements(c, scale) || !on_elements(c, shift) || !on_elements(c, weight) ||
         !on_elements(c, x_out))
         return fail(c, SPECA_ERR_ALIGNMENT, "norm8: a tensor is not aligned to the element size");

@@ -97,6 +97,9 @@ def test_quantize_and_norm_refuse(S, lib, dtype):
         (dict(x_out=D, x_out_stride=DIM - 1), "SHAPE"), (dict(x_out=A, x_out_stride=DIM + 8), "INVALID_ARG"),
         (dict(branch=D, branch_stride=DIM, x_out=D, x_out_stride=DIM + 8), "INVALID_ARG"), (dict(x_out=B, x_out_stride=DIM), "INVALID_ARG"),
         (dict(x_out=C, x_out_stride=DIM), "INVALID_ARG"), (dict(branch=B, branch_stride=DIM), "INVALID_ARG"), (dict(weight=C), "INVALID_ARG"),
+        (dict(weight=D, x_out=D, x_out_stride=DIM), "INVALID_ARG"), (dict(scale=D, x_out=D, x_out_stride=DIM), "INVALID_ARG"),
+        (dict(shift=D, x_out=D, x_out_stride=DIM), "INVALID_ARG"),
+        (dict(branch=E, branch_stride=DIM, gate=D, x_out=D, x_out_stride=DIM), "INVALID_ARG"),
         (dict(weight=D + 1), "ALIGNMENT"), (dict(shift=D + 1), "ALIGNMENT"), (dict(x_out=D + 1, x_out_stride=DIM), "ALIGNMENT"),
     ]:
         assert norm(S, lib, layer, **kw) == getattr(S, "SPECA_ERR_" + status), kw

@@ -119,7 +119,8 @@ def test_epilogues(S, dt, kind, m, n, k):
     E.check8(m8, t, bt, "8 bits")
 
 
-@pytest.mark.parametrize("m,n,k", [(12, 200, 300), (500, 300, 256), (4608, 2304, 256)])
+# the third goes to tiles of one SM without a mask and to a pair's with one
+@pytest.mark.parametrize("m,n,k", [(12, 200, 300), (500, 300, 256), (4096, 1152, 4608), (4608, 2304, 256), (100, 300, 8200)])
 def test_masked_samples_are_left_alone_and_others_do_not_see_it(S, m, n, k):
     g = gen(1)
     lens = [m // 4, 0, 1, m // 2, m - m // 4 - 1 - m // 2]
