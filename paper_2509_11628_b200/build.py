@@ -18,7 +18,7 @@ SOURCES = ["speca_kernels.cu", "speca_static.cu", "speca_layer_rows.cu", "speca_
            "speca_norm8.cu", "speca_matmul8_tc.cu", "speca_matmul8_few.cu", "speca_api.cpp", "speca_layer.cpp", "speca_layer8.cpp"]
 HEADERS = [os.path.join(CSRC, "speca_internal.h"), os.path.join(CSRC, "speca_layer_internal.h"),
            os.path.join(CSRC, "speca_layer_handle.h"), os.path.join(CSRC, "speca_rows_common.cuh"),
-           os.path.join(CSRC, "speca_eight_common.cuh"), os.path.join(CSRC, "speca_tc.cuh"), os.path.join(CSRC, "speca_matmul8_common.cuh"), os.path.join(CSRC, "speca_matmul8_tensor.cuh"),
+           os.path.join(CSRC, "speca_eight_common.cuh"), os.path.join(CSRC, "speca_tc.cuh"), os.path.join(CSRC, "speca_early.cuh"), os.path.join(CSRC, "speca_matmul8_common.cuh"), os.path.join(CSRC, "speca_matmul8_tensor.cuh"),
            os.path.join(CSRC, "speca_attention_common.cuh"), os.path.join(ROOT, "include", "speca.h")]
 
 

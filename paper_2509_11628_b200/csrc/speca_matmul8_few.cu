@@ -55,6 +55,22 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         if (threadIdx.x == 0) atomicExch(p.gave_up, 1u);
         return;
     }
+    if (threadIdx.x == kLoader * 32) {
+        for (int i = 0; i < S::kStages; ++i) {
+            bar_init(&sm.full[i], 1);
+            bar_init(&sm.empty[i], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            bar_init(&sm.scales_full[b], 4);  // one arrival per warp
+            bar_init(&sm.scales_used[b], 1);
+        }
+        bar_init(&sm.sums_full, 1);
+        sm.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fetch_map(&map_w);
+        fetch_map(&map_a);
+    }
+    wait_for_stream();
     if (p.dev_mask != nullptr) {  // the same in every block of the cluster
         bool live = false;
         for (int r = lane; r < rows; r += 32) live = live || p.dev_mask[p.row_seq[m0 + r]] != 0;
@@ -77,20 +93,8 @@ __global__ void __launch_bounds__(kFewThreads, 2)
         if (++stage == S::kStages) stage = 0, phase ^= 1;
     };
     if (warp == kLoader) {
-        if (lane == 0) {
-            for (int i = 0; i < S::kStages; ++i) {
-                bar_init(&sm.full[i], 1);
-                bar_init(&sm.empty[i], 1);
-            }
-            for (int b = 0; b < 2; ++b) {
-                bar_init(&sm.scales_full[b], 4);  // one arrival per warp
-                bar_init(&sm.scales_used[b], 1);
-            }
-            bar_init(&sm.sums_full, 1);
-            sm.abort = 0;
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        if (lane == 0)
             for (int kb = begin; kb < min(begin + S::kStages, end); ++kb) load(kb);  // the first stages have room
-        }
         __syncwarp();
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(S::kCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
@@ -228,19 +232,7 @@ cudaError_t run_few(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
     const int64_t tiles = (static_cast<int64_t>(p.n) + kRows - 1) / kRows * ((p.m + NR - 1) / NR);
     const int k_blocks = (p.k + kBlock8 - 1) / kBlock8;
     const int ranks = few_ranks(tiles, k_blocks, sm_count);
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(static_cast<unsigned>(tiles * ranks));
-    config.blockDim = dim3(kFewThreads);
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(ranks);
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    config.attrs = attr;
-    config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, kernel, p, a, w);
+    return launch_early(kernel, static_cast<unsigned>(tiles * ranks), static_cast<unsigned>(ranks), kFewThreads, smem, stream, p, a, w);
 }
 
 template <int DT>

@@ -1,11 +1,14 @@
 // What the 8-bit products on the tensor cores share: waits, loads, block-scaled products, scales in tensor memory.
 #pragma once
+#include "speca_early.cuh"
 #include "speca_matmul8_common.cuh"
 
 namespace speca {
 namespace {
 
 constexpr int kRows = 128;  // rows of an operand of one SM, and lanes of tensor memory
+
+__device__ __forceinline__ void fetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 // ---- the pair of SMs ----------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t cluster_rank() {

@@ -7,6 +7,7 @@
 // registers leave room for on the way there: 20926 rows x 4096 bf16 with branch, gate and weight 113 us (5.3 TB/s), as they are 49 us (5.2 TB/s); with 8 elements a
 // lane (four shuffles, one scale and one set of addresses for half as much) 210 and 84. Tried and not kept, 20926 x 4096: weight, scale and shift loaded in
 // front of the sums 155 us (registers), bounds on the registers 114 to 146.
+#include "speca_early.cuh"
 #include "speca_eight_common.cuh"
 #include "speca_rows_common.cuh"
 
@@ -75,6 +76,7 @@ template <int DT, bool VEC>
 __global__ void __launch_bounds__(kQuantThreads) quantize8_kernel(const __grid_constant__ Norm8Params p, const int64_t total, const int per_row) {
     using T = typename Type<DT>::T;
     constexpr int kGroups = kQuantThreads / kLanes;
+    wait_for_stream();
     const int l = threadIdx.x % kLanes;
     const int64_t index = static_cast<int64_t>(blockIdx.x) * (kGroups * kBlocks) + threadIdx.x / kLanes;
     int64_t row = total <= 0xffffffff ? static_cast<uint32_t>(index) / static_cast<uint32_t>(per_row) : index / per_row;
@@ -108,6 +110,7 @@ __global__ void __launch_bounds__(NT) norm8_kernel(const __grid_constant__ Norm8
     auto some = [&](int i) { return VEC ? at(i) + kPer * l < p.dim : at(i) < p.dim; };         // whether any of it exists
     auto there = [&](int i, int e) { return VEC ? some(i) : at(i) + l + kLanes * e < p.dim; };
     auto row_of = [&](const char* base, int64_t i, int64_t stride) { return reinterpret_cast<const T*>(base) + i * stride; };
+    wait_for_stream();
     bool live = row < p.rows;
     int seq = 0;
     if (live) {
@@ -202,6 +205,7 @@ __global__ void __launch_bounds__(1024) norm8_long_kernel(const __grid_constant_
     using T = typename Type<DT>::T;
     __shared__ float red[2][32];
     const int row = blockIdx.x;
+    wait_for_stream();
     const int seq = p.row_seq[row];
     if (p.dev_mask != nullptr && p.dev_mask[seq] == 0) return;
     auto row_of = [&](const char* base, int64_t i, int64_t stride) { return base == nullptr ? nullptr : reinterpret_cast<const T*>(base) + i * stride; };
@@ -247,19 +251,18 @@ __global__ void __launch_bounds__(1024) norm8_long_kernel(const __grid_constant_
 }
 
 template <int DT, bool VEC, int NV, int G, int NT>
-void run_norm8(const Norm8Params& p, cudaStream_t stream) {
+cudaError_t run_norm8(const Norm8Params& p, cudaStream_t stream) {
     const int per = NT / G;
-    norm8_kernel<DT, VEC, NV, G, NT><<<(p.rows + per - 1) / per, NT, 0, stream>>>(p);
+    return launch_early(norm8_kernel<DT, VEC, NV, G, NT>, (p.rows + per - 1) / per, 1, NT, 0, stream, p);
 }
 
 template <int DT, bool VEC>
-void dispatch_norm8(const Norm8Params& p, cudaStream_t stream) {
+cudaError_t dispatch_norm8(const Norm8Params& p, cudaStream_t stream) {
     const int per_row = (p.dim + kBlock8 - 1) / kBlock8;
     if (!p.norm) {
         constexpr int per = kQuantThreads / kLanes * kBlocks;
         const int64_t total = static_cast<int64_t>(p.rows) * per_row;
-        quantize8_kernel<DT, VEC><<<static_cast<unsigned>((total + per - 1) / per), kQuantThreads, 0, stream>>>(p, total, per_row);
-        return;
+        return launch_early(quantize8_kernel<DT, VEC>, static_cast<unsigned>((total + per - 1) / per), 1, kQuantThreads, 0, stream, p, total, per_row);
     }
     // One access a thread as long as a block has threads for the row: of 4096 elements 256 threads x 1 took 113 us with branch and gate (20926 rows),
     // 128 x 2 took 125; of 1152, 96 x 1 39 us with the branch, 32 x 3 47. Behind 6144 two: 8192 as 256 x 2 94 us (8345 rows), 512 x 1 111.
@@ -274,18 +277,15 @@ void dispatch_norm8(const Norm8Params& p, cudaStream_t stream) {
     if (n <= 384) return run_norm8<DT, VEC, 1, 384, 384>(p, stream);
     if (n <= 512) return run_norm8<DT, VEC, 2, 256, 256>(p, stream);
     if (n <= 512 * 2) return run_norm8<DT, VEC, 2, 512, 512>(p, stream);
-    norm8_long_kernel<DT><<<p.rows, 1024, 0, stream>>>(p);
+    return launch_early(norm8_long_kernel<DT>, p.rows, 1, 1024, 0, stream, p);
 }
 
 }  // namespace
 
 cudaError_t launch_norm8(const Norm8Params& p, int dtype, bool vectors, cudaStream_t stream) {
     if (p.rows == 0) return cudaSuccess;
-    if (dtype == SPECA_BF16)
-        vectors ? dispatch_norm8<SPECA_BF16, true>(p, stream) : dispatch_norm8<SPECA_BF16, false>(p, stream);
-    else
-        vectors ? dispatch_norm8<SPECA_F32, true>(p, stream) : dispatch_norm8<SPECA_F32, false>(p, stream);
-    return cudaGetLastError();
+    if (dtype == SPECA_BF16) return vectors ? dispatch_norm8<SPECA_BF16, true>(p, stream) : dispatch_norm8<SPECA_BF16, false>(p, stream);
+    return vectors ? dispatch_norm8<SPECA_F32, true>(p, stream) : dispatch_norm8<SPECA_F32, false>(p, stream);
 }
 
 }  // namespace speca
