@@ -13,10 +13,11 @@
 // What bounds it: a step of 128 elements of k is 512 cycles of the tensor pipe in a pair (256 x 256) and brings 32 KB into each SM, which takes as
 // long (an SM got 90 to 110 GB/s from L2 in every shape tried, 50 to 58 bytes a cycle); tiles of one SM (128 x 128) read as much for half the
 // products. Between tiles some 1300 cycles pass while the last sums are read. In a loop the card runs into its power limit (1000 W, 1.4 GHz).
-// Measured, e4m3 with bf16 out: 4096 x 4608 x 1152 22.7 us (1.92 PFLOP/s), 8352 x 14336 x 4096 357 us in a short run (2.74), 408 in a loop (2.41; a library's
-// block-scaled product 385), 8192^3 434 in a loop (2.53; 459), 20928 x 16384 x 4096 1130 in a loop (2.49; 1260). Short k with an activation is bound by the
-// epilogue: 4096 x 4608 x 1152 with bias and GELU into 8 bits 30 us, three quarters of it the special function unit's 1.5 results an element.
-// Every wait is bounded. A wait that runs out sets the layer's gave-up flag and ends the block's work.
+// Measured, e4m3 with bf16 out, in a loop: 4096 x 4608 x 1152 22.9 us (1.90 PFLOP/s; a library's block-scaled product 23.3), 4096 x 1152 x 4608 26.8 (1.62;
+// 28.0), 8352 x 14336 x 4096 399 (2.46; 390), 8192^3 422 (2.61; 470), 20928 x 16384 x 4096 1100 (2.55; 1277); 8352 x 14336 x 4096 in a short run 357 (2.74).
+// Short k with an activation is bound by the epilogue: 4096 x 4608 x 1152 with bias and GELU into 8 bits 28 us, 20 without them. Tried there and
+// not kept: 16 epilogue warps in place of 8 (28.1 us), exponentials of one pair in 4, 3 or 2 by polynomial (28.3 to 28.9), what the next tile needs asked
+// for a tile ahead (30.8 then, 30.1).
 #include <algorithm>
 
 #include "speca_matmul8_tensor.cuh"
@@ -25,7 +26,7 @@ namespace speca {
 namespace {
 
 // Four warpgroups of 128 registers a thread at launch; the epilogue's two take 176, the others give up what they take: 2 x 176 + 2 x 80 = 4 x 128.
-constexpr int kThreads = 512;
+constexpr int kThreads = 512, kRegisters = 128;
 constexpr int kLoadWarp = 8, kIssueWarp = 9, kScaleWarp = 12;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kScaleCol = 480;                   // two stages of 16 columns: 4 for A's scales, up to 8 for W's
@@ -94,7 +95,7 @@ __device__ __forceinline__ bool tile_live(const Matmul8Params& p, int first, int
 enum Epilogue { kPlain, kResidual, kEight };
 
 // t / (1 + 2^x), two at a time with one reciprocal, 1 / a = b / (a b): the special function unit, which forms 16 a cycle, bounds an epilogue
-// with an activation. So that a b stays finite x is held at 63: below 2^-63 t the result is that.
+// with an activation among others. So that a b stays finite x is held at 63: below 2^-63 t the result is that.
 __device__ __forceinline__ uint64_t times_sigmoid2(uint64_t t, uint64_t x) {
     float x0, x1, d0, d1, r;
     unpair(x, x0, x1);
@@ -633,6 +634,12 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
                                                                      : matmul8_tc_kernel<DT, CG, NT, kPlain>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
+    // the warps' shares of the registers rely on what the kernel was built with: with fewer they would wait for ever
+    cudaFuncAttributes attr;
+    static const bool built[3] = {cudaFuncGetAttributes(&attr, matmul8_tc_kernel<DT, CG, NT, kEight>) == cudaSuccess && attr.numRegs >= kRegisters,
+                                  cudaFuncGetAttributes(&attr, matmul8_tc_kernel<DT, CG, NT, kResidual>) == cudaSuccess && attr.numRegs >= kRegisters,
+                                  cudaFuncGetAttributes(&attr, matmul8_tc_kernel<DT, CG, NT, kPlain>) == cudaSuccess && attr.numRegs >= kRegisters};
+    if (!built[0] || !built[1] || !built[2]) return cudaErrorInvalidKernelImage;
     // parts: what the list of tiles holds, and what counts in 32 bits
     constexpr int64_t kMaxN = int64_t(1) << 18;
     for (int64_t m0 = 0; m0 < p.m; m0 += int64_t(kMaxTilesM) * S::kTileM)
