@@ -231,7 +231,7 @@ cudaError_t run_few(const Matmul8Params& p, int sm_count, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     const int64_t tiles = (static_cast<int64_t>(p.n) + kRows - 1) / kRows * ((p.m + NR - 1) / NR);
     const int k_blocks = (p.k + kBlock8 - 1) / kBlock8;
-    const int ranks = few_ranks(tiles, k_blocks, sm_count);
+    const int ranks = max(few_ranks(tiles, k_blocks, sm_count), p.shares);
     return launch_early(kernel, static_cast<unsigned>(tiles * ranks), static_cast<unsigned>(ranks), kFewThreads, smem, stream, p, a, w);
 }
 

@@ -94,8 +94,9 @@ __device__ __forceinline__ bool tile_live(const Matmul8Params& p, int first, int
 // own: the epilogue's code has to stay in the instruction cache (one for all, unrolled over all columns, was three times as slow).
 enum Epilogue { kPlain, kResidual, kEight };
 
-// t / (1 + 2^x), two at a time with one reciprocal, 1 / a = b / (a b): the special function unit, which forms 16 a cycle, bounds an epilogue
-// with an activation among others. So that a b stays finite x is held at 63: below 2^-63 t the result is that.
+// t / (1 + 2^x), two at a time with one reciprocal, 1 / a = b / (a b): the special function unit forms 16 a cycle, and is a quarter busy in a
+// product with GELU (4096 x 4608 x 1152; with half of the exponentials as polynomials instead the product took as long). So that
+// a b stays finite x is held at 63: below 2^-63 t the result is that.
 __device__ __forceinline__ uint64_t times_sigmoid2(uint64_t t, uint64_t x) {
     float x0, x1, d0, d1, r;
     unpair(x, x0, x1);
@@ -687,11 +688,26 @@ cudaError_t dispatch(const Matmul8Params& p, Kind kind, int sm_count, cudaStream
     return kind == kOne ? run<DT, 1, 128>(p, sm_count, stream) : run<DT, 2, 256>(p, sm_count, stream);
 }
 
+// The tensor cores cut what they add to a sum to its last bit instead of rounding it, so that a sum over all of k comes out short: in the kernels for
+// many rows by 6.5e-7 of its size at k = 8192 and by 1.4e-6 at 16384, which bf16 and 8 bits do not see. Outputs in fp32 with more than 8192 elements
+// of k are therefore left to the kernel for few rows, which adds up shares of k with rounding: 2304 x 4096 x 16384 is 3.7e-7 off in place of
+// 1.9e-6, for 193 us in place of 101. At 8192 the pair's 9e-7 stay (58 us; shares would take 134).
+constexpr int kShareBlocks = 32, kLongBlocks = 64;
+int shares_of(const Matmul8Params& p, int dtype) {
+    const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
+    if (dtype != SPECA_F32 || p.out == nullptr || kb <= kLongBlocks) return 1;
+    int shares = 2;
+    while (shares < kFewRanks && shares * kShareBlocks < kb) shares *= 2;
+    return shares;
+}
+
 }  // namespace
 
-cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream) {
-    if (p.m == 0) return cudaSuccess;
-    const Kind kind = choose(p, sm_count);
+cudaError_t launch_matmul8(const Matmul8Params& given, int dtype, int sm_count, cudaStream_t stream) {
+    if (given.m == 0) return cudaSuccess;
+    Matmul8Params p = given;
+    p.shares = shares_of(p, dtype);
+    const Kind kind = p.shares > 1 ? kFew : choose(p, sm_count);
     if (kind == kFew) return launch_matmul8_few(p, dtype, sm_count, stream);
     return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, kind, sm_count, stream) : dispatch<SPECA_F32>(p, kind, sm_count, stream);
 }

@@ -236,6 +236,29 @@ def test_scales_far_from_one(S, m, n, ea, ew):
     assert torch.equal(out.double(), E.values(a) @ E.values(w).T)
 
 
+@pytest.mark.parametrize("m,n,k", [(8, 512, 16384), (300, 512, 8192), (2304, 2048, 4096), (2304, 2048, 8200), (2304, 2048, 16384)])
+def test_fp32_sums_over_long_k(S, m, n, k):
+    # a share of s elements is off by (1.04 s + 73) roundings of its magnitudes at most (eight_util.product has the count for s = k), and shares are at
+    # most 4096 elements from k = 8193 on
+    g = gen(k)
+    a, w = real(g, m, k), real(g, n, k, k ** -0.5)
+    layer = S.SpecaLayer([0, m], S.SPECA_F32, device=DEV)
+    out = torch.zeros(m, n, device=DEV)
+    layer.matmul8(a, w, out)
+    layer.check()
+    t, bt = E.product(a, w)
+    share = (1.04 * (4096 if k > 8192 else k) + 73) / (1.04 * k + 73)
+    L.check(out, t, share * bt)
+    # a bias, an activation, a gate and a residual go with it, and a mask
+    bias, res = torch.randn(n, generator=g, device=DEV), torch.randn(m, n, generator=g, device=DEV)
+    gate = torch.randn(1, n, generator=g, device=DEV)
+    t, bt = E.product(a, w, bias, "silu")
+    want, bound = res.double() + gate.double() * t, gate.double().abs() * (bt + 2 * E.U32 * t.abs())
+    layer.matmul8(a, w, res, bias=bias, activation=S.SPECA_ACT_SILU, residual=res, gate=gate, active=torch.ones(1, dtype=torch.uint8, device=DEV))
+    layer.check()
+    L.check(res, want, bound)
+
+
 def test_the_same_bits_every_time(S):
     g = gen(12)
     for m, n, k in ((4, 512, 8192), (300, 1000, 1152), (2304, 4096, 1152)):
