@@ -212,41 +212,42 @@ __global__ void __launch_bounds__(1024) norm8_long_kernel(const __grid_constant_
     const T *px = row_of(p.x, row, p.x_stride), *pb = row_of(p.branch, row, p.branch_stride), *pw = row_of(p.weight, 0, 0);
     const T *pg = row_of(p.gate, seq, p.mod_stride), *ps = row_of(p.scale, seq, p.mod_stride), *pt = row_of(p.shift, seq, p.mod_stride);
     T* po = p.x_out == nullptr ? nullptr : reinterpret_cast<T*>(p.x_out) + row * p.x_out_stride;
-    constexpr int kStep = 1024 / kLanes * kBlock8;
-    const int l = threadIdx.x % kLanes, start = threadIdx.x / kLanes * kBlock8;
-    auto value = [&](int c) {
+    // without a sign: a step behind the last element passes 2^31
+    constexpr uint32_t kStep = 1024 / kLanes * kBlock8;
+    const uint32_t dim = p.dim, l = threadIdx.x % kLanes, start = threadIdx.x / kLanes * kBlock8;
+    auto value = [&](uint32_t c) {
         const float v = to_float(px[c]);
         return pb == nullptr ? v : fmaf(pg == nullptr ? 1.f : to_float(pg[c]), to_float(pb[c]), v);
     };
     float mean = 0.f;
     if (p.centre) {
         float sum = 0.f;
-        for (int f = start; f < p.dim; f += kStep)
-            for (int c = f + l; c < min(f + kBlock8, p.dim); c += kLanes) sum += value(c);
+        for (uint32_t f = start; f < dim; f += kStep)
+            for (uint32_t c = f + l; c < min(f + kBlock8, dim); c += kLanes) sum += value(c);
         mean = sum_row<1024>(sum, red[0]) / p.dim;
     }
     float sq = 0.f;
-    for (int f = start; f < p.dim; f += kStep)
-        for (int c = f + l; c < min(f + kBlock8, p.dim); c += kLanes) {
+    for (uint32_t f = start; f < dim; f += kStep)
+        for (uint32_t c = f + l; c < min(f + kBlock8, dim); c += kLanes) {
             const float d = value(c) - mean;
             sq = fmaf(d, d, sq);
         }
     const float rstd = 1.f / sqrtf(sum_row<1024>(sq, red[1]) / p.dim + p.eps);
     // the blocks of a warp go through the loop together
-    for (int f = start, first = threadIdx.x / 32 * (32 / kLanes) * kBlock8; first < p.dim; f += kStep, first += kStep) {
+    for (uint32_t f = start, first = threadIdx.x / 32 * (32 / kLanes) * kBlock8; first < dim; f += kStep, first += kStep) {
         float v[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-            const int c = f + l + kLanes * e;
+            const uint32_t c = f + l + kLanes * e;
             v[e] = 0.f;
-            if (c >= p.dim) continue;
+            if (c >= dim) continue;
             v[e] = value(c);
             if (po != nullptr) po[c] = from_float<T>(v[e]);
             float y = (v[e] - mean) * rstd;
             if (pw != nullptr) y *= to_float(pw[c]);
             v[e] = fmaf(y, ps == nullptr ? 1.f : 1.f + to_float(ps[c]), pt == nullptr ? 0.f : to_float(pt[c]));
         }
-        put16<false>(p.out, row, f, l, p.dim, true, v);
+        put16<false>(p.out, row, static_cast<int>(f), l, p.dim, f < dim, v);
     }
 }
 

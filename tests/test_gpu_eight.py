@@ -251,3 +251,27 @@ def test_rows_behind_32_bits(S):
         assert torch.equal(m.codes.view(torch.uint8)[part], first.codes.view(torch.uint8))
         assert torch.equal(m.scales.view(torch.uint8)[:, part], first.scales.view(torch.uint8))
     assert int(m.codes.view(torch.uint8)[rows // 2].max()) == 0 and int(E.bytes_of(m)[rows // 2, 0]) == 127
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+def test_the_longest_row(S, kind):
+    # ones with a two at either end. RMS norm: of mean square 1 + 6 / dim, that is 1 off by 3e-6 with eps: codes of 1 and 2 (a step of e4m3 there is 2^-3
+    # of the value or 2^-4). Layer norm: mean 1 + 2 / dim (rounded to 1: 2^-24 of it, 6e-8, is more), so zeros, and of the two 1 / sqrt(2 / dim + eps)
+    dim = S.SPECA_MAX_ROWS
+    x = torch.ones(1, dim, dtype=torch.bfloat16, device=DEV)
+    x[0, 0], x[0, -1] = 2, 2
+    layer = S.SpecaLayer([0, 1], S.SPECA_BF16, device=DEV)
+    m = S.Matrix8.empty(1, dim, DEV)
+    layer.norm8(x, m, S.SPECA_NORM_RMS if kind == "rms" else S.SPECA_NORM_LAYER)
+    layer.check()
+    got, byte = m.codes.view(torch.uint8)[0], m.scales.view(torch.uint8).view(-1)
+    # e4m3: 256 is 0x78, 128 is 0x70
+    inner, want = (0x78, 119) if kind == "rms" else (0x00, 127)
+    assert bool((byte[1:-1] == want).all())
+    assert bool((got[128:-128] == inner).all())
+    top = 2.0 if kind == "rms" else 1 / (2 / dim + 1e-6) ** 0.5
+    for edge, at in ((slice(0, 128), 0), (slice(dim - 128, dim), -1)):
+        values = got[edge].view(torch.float8_e4m3fn).float() * 2.0 ** (int(byte[at]) - 127)
+        want = torch.full((128,), 1.0 if kind == "rms" else 0.0, device=DEV)
+        want[at] = top
+        assert bool(((values - want).abs() <= want * (0 if kind == "rms" else 2.0 ** -4)).all())
