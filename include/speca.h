@@ -679,11 +679,12 @@ speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_
  *   value(r, c) = e4m3(codes[r * code_stride + c]) * 2^(s - 127),
  *   s = scales[(c / 512) * scale_stride + 4 * r + c / 128 % 4]
  * so the scale bytes of four blocks of a row lie together, rows of such a group of 512 columns one after another; bytes behind
- * the last block are neither read nor written. Writing a block takes the smallest power of two 2^(s - 127), 1 <= s <= 254, that brings
+ * the last block are neither used nor written. Writing a block takes the smallest power of two 2^(s - 127), 1 <= s <= 254, that brings
  * its largest finite magnitude to 448 or less (s = 127 for a block of zeros) and rounds the quotients to nearest even.
  * e4m3 has no infinity: a value that is not finite becomes NaN, and the others of its block keep their scale.
  */
 #define SPECA_BLOCK8 128 /* elements that share a scale */
+#define SPECA_MAX_K8 262144 /* most elements of a row of a product's operands: a bf16 rounding, 2^-9, is lost in a sum of that many of one sign */
 typedef struct {
     void* codes;          /* device, rows of bytes */
     int64_t code_stride;  /* bytes between rows */
@@ -725,8 +726,7 @@ speca_status_t speca_layer_norm8(speca_layer_t* layer, int32_t kind, int32_t dim
                                  const speca_matrix8_t* out, void* stream);
 
 /*
- * Product of the layer's query rows with a weight matrix, both in 8 bits, sums in fp32. (The tensor cores cut a sum's last bit, 32 elements
- * of k at a time; for outputs in fp32 and k from 8193 to 32768 they sum at most 4096 elements, and such shares are added with rounding.)
+ * Product of the layer's query rows with a weight matrix, both in 8 bits, sums in fp32:
  *   t[i, j] = act(sum_k a[i, k] * w[j, k] + bias[j])
  *   out[i, j] = residual[i, j] + gate_s[j] * t[i, j]      in the layer's type, or
  *   out_8bit  = 8 bits of t, a scale for each 128 columns
@@ -736,7 +736,10 @@ speca_status_t speca_layer_norm8(speca_layer_t* layer, int32_t kind, int32_t dim
  *                 same stride.  gate: [n_seqs, n], row stride gate_stride, or NULL (1).
  *   out, out_8bit exactly one of them; nothing else may overlap the output. residual and gate go with out alone.
  * Rows of inactive sequences are not written, and tiles of rows that hold no others are not computed. A NaN (code 0x7f or 0xff, or a scale byte
- * of 255) makes its row or column of the product NaN. A row's result does not depend on the mask: no atomics on values, an order of sums that the
+ * of 255) makes its row or column of the product NaN. The products are exact; the tensor cores add 32 at a time to a sum and cut each at some
+ * 2^-25 of the largest among them and the sum, so that sum_k is off by at most (1.04 s + 73) 2^-24 sum_k |a w| when s elements are summed at once:
+ * k at most, and at most 4096 for outputs in fp32 with k from 8193 to 32768, whose shares are added with rounding (k / 8 beyond). Of terms of one
+ * sign s / 2^27 of the sum gets lost that way, so k ends at SPECA_MAX_K8. A row's result does not depend on the mask: no atomics on values, an order of sums that the
  * sizes fix (the number of rows among them: k is shared out where there are few).
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, UNSUPPORTED (a stride of 2^40 bytes or more), CUDA.
  */

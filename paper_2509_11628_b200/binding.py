@@ -29,7 +29,7 @@ SPECA_MAX_ORDER, SPECA_MAX_BATCH, SPECA_MAX_ENTRIES, SPECA_MAX_HORIZON = 4, 64, 
 SPECA_ROPE_INTERLEAVED, SPECA_ROPE_HALVES = 0, 1
 SPECA_NORM_LAYER, SPECA_NORM_RMS = 0, 1
 SPECA_ACT_NONE, SPECA_ACT_GELU, SPECA_ACT_SILU = 0, 1, 2
-SPECA_BLOCK8 = 128
+SPECA_BLOCK8, SPECA_MAX_K8 = 128, 262144
 SPECA_MAX_SEQS, SPECA_MAX_ROWS, SPECA_MAX_HEAD_DIM, SPECA_MAX_GROUP, SPECA_MAX_AXES = 512, (1 << 31) - (1 << 16), 128, 128, 4
 
 EXPORTS = [

@@ -156,8 +156,8 @@ speca_status_t speca_layer_matmul8(speca_layer_t* c, int32_t n, int32_t k, const
                                    const void* gate, int64_t gate_stride, const uint8_t* dev_active_mask, void* out,
                                    int64_t out_stride, const speca_matrix8_t* out_8bit, void* stream) {
     if (c == nullptr) return SPECA_ERR_INVALID_ARG;
-    if (n < 1 || n > kMaxRows || k < 1 || k > kMaxRows)
-        return fail(c, SPECA_ERR_SHAPE, "matmul8: n or k outside 1 .. %lld", static_cast<long long>(kMaxRows));
+    if (n < 1 || n > kMaxRows) return fail(c, SPECA_ERR_SHAPE, "matmul8: n outside 1 .. %lld", static_cast<long long>(kMaxRows));
+    if (k < 1 || k > SPECA_MAX_K8) return fail(c, SPECA_ERR_SHAPE, "matmul8: k outside 1 .. %d", SPECA_MAX_K8);
     if (activation != SPECA_ACT_NONE && activation != SPECA_ACT_GELU && activation != SPECA_ACT_SILU)
         return fail(c, SPECA_ERR_INVALID_ARG, "matmul8: unknown activation");
     const int64_t m = c->total_q;

@@ -168,6 +168,14 @@ def test_product_refuses(S, lib, dtype):
     assert lib.speca_layer_matmul8(None, 1, 1, None, None, None, 0, None, 0, None, 0, None, None, 0, None, None) == S.SPECA_ERR_INVALID_ARG
 
 
+def test_product_of_the_longest_rows(S, lib):
+    layer, _mem = H.layer(S, lib, [0, 2, ROWS], 1)
+    k = S.SPECA_MAX_K8
+    far = dict(a=(A, k + 16, B, 4 * ROWS), w=(C, k + 16, D, 1024))
+    assert product(S, lib, layer, k=k, **far) == S.SPECA_OK
+    assert product(S, lib, layer, k=k + 1, **far) == S.SPECA_ERR_SHAPE and b"262144" in lib.speca_layer_last_error(layer)
+
+
 def test_the_binding_refuses_what_it_cannot_marshal(S):
     codes = torch.zeros(4, 600, dtype=torch.uint8).view(torch.float8_e4m3fn)
     scales = torch.zeros(2, 4, 4, dtype=torch.uint8).view(torch.float8_e8m0fnu)

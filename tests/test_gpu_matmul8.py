@@ -360,6 +360,77 @@ def test_two_handles_on_two_streams_and_replayed_graphs(S):
         assert torch.equal(out, want.flip(0))
 
 
+@pytest.mark.parametrize("dt", list(DT))
+@pytest.mark.parametrize("m,n", [(1, 1), (5, 200), (300, 700), (2400, 2100)])
+def test_the_longest_k(S, dt, m, n):
+    # ones: below 2^24 their sums are exact
+    k = S.SPECA_MAX_K8
+    a, w = S.Matrix8.empty(m, k, DEV), S.Matrix8.empty(n, k, DEV)
+    for x in (a, w):
+        raw(x)[0].fill_(0x38)
+        raw(x)[1].fill_(127)
+    out = torch.zeros(m, n, dtype=DT[dt], device=DEV)
+    layer = S.SpecaLayer([0, m], code(S, dt), device=DEV)
+    layer.matmul8(a, w, out)
+    layer.check()
+    assert bool((out == k).all())
+
+
+def test_one_handle_on_two_streams_and_in_a_graph_with_branches(S):
+    # kernels may start before the one in front has ended; they wait for it, whichever stream or branch it is on
+    g = gen(17)
+    m, k, n = 700, 1152, 640
+    layer = S.SpecaLayer(L.offsets([300, 0, 400]), S.SPECA_BF16, device=DEV)
+    x = torch.randn(m, k, generator=g, device=DEV).bfloat16()
+    w = real(g, n, k, k ** -0.5)
+    a, b = (S.Matrix8.empty(m, k, DEV) for _ in range(2))
+    one, two, three = (torch.zeros(m, n, dtype=torch.bfloat16, device=DEV) for _ in range(3))
+    side = torch.cuda.Stream()
+
+    def run():
+        main = torch.cuda.current_stream()
+        x.mul_(1)
+        side.wait_stream(main)
+        layer.norm8(x, a)
+        layer.matmul8(a, w, one)
+        with torch.cuda.stream(side):
+            layer.quantize8(x, b)
+            layer.matmul8(b, w, two, activation=S.SPECA_ACT_SILU)
+        main.wait_stream(side)
+        layer.matmul8(a, w, three, residual=two)
+        x.copy_(x.flip(0))
+        layer.quantize8(x, a)
+
+    def alone():
+        y, c = x.clone(), S.Matrix8.empty(m, k, DEV)
+        outs = [torch.zeros_like(one) for _ in range(3)]
+        for step in (lambda: layer.norm8(y, c), lambda: layer.matmul8(c, w, outs[0]), lambda: layer.quantize8(y, c),
+                     lambda: layer.matmul8(c, w, outs[1], activation=S.SPECA_ACT_SILU), lambda: layer.norm8(y, c),
+                     lambda: layer.matmul8(c, w, outs[2], residual=outs[1]), lambda: layer.quantize8(y.flip(0).contiguous(), c)):
+            step()
+            torch.cuda.synchronize()
+        return outs, c
+
+    def check(outs, c):
+        torch.cuda.synchronize()
+        layer.check()
+        for got, want in zip((one, two, three), outs):
+            assert torch.equal(got, want)
+        assert all(torch.equal(p, q) for p, q in zip(raw(a), raw(c)))
+
+    want = alone()
+    run()
+    check(*want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for seed in (1, 2, 3):
+        x.copy_(torch.randn(m, k, generator=gen(seed), device=DEV))
+        want = alone()
+        graph.replay()
+        check(*want)
+
+
 def test_no_rows(S):
     layer = S.SpecaLayer([0, 0, 0], S.SPECA_BF16, device=DEV)
     layer.matmul8(S.Matrix8.empty(0, 64, DEV), S.Matrix8.empty(32, 64, DEV), torch.zeros(0, 32, dtype=torch.bfloat16, device=DEV))
