@@ -547,8 +547,8 @@ speca_status_t speca_cache_launch_count(const speca_cache_t* cache, uint64_t* ou
  *
  * A speculative step computes one block for real -- the verification layer, whose fresh feature
  * speca_verify compares with the forecast -- and a rejected sample computes all of them. The calls
- * below are the parts of such a block that are not plain matrix products: the adaptive layer norm at
- * its entry, the rotary positions of its queries and keys, and its attention. They work on packed
+ * below are the parts of such a block: the adaptive layer norm at its entry, the rotary positions of its
+ * queries and keys, its attention, and (in 8 bits, further down) its matrix products. They work on packed
  * sequences: the samples of a batch lie one after another in one [rows, ...] tensor, sequence s in rows
  * host_q_start[s] .. host_q_start[s + 1] - 1, each of its own length (zero included). As everywhere in
  * this library a device mask says per sequence whether it is active (dev_active_mask, n_seqs bytes, NULL =
@@ -684,7 +684,7 @@ speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_
  * e4m3 has no infinity: a value that is not finite becomes NaN, and the others of its block keep their scale.
  */
 #define SPECA_BLOCK8 128 /* elements that share a scale */
-#define SPECA_MAX_K8 262144 /* most elements of a row of a product's operands: a bf16 rounding, 2^-9, is lost in a sum of that many of one sign */
+#define SPECA_MAX_K8 262144 /* most elements of a row of a product's operands: a sum of that many of one sign may lose a bf16 rounding, 2^-9 */
 typedef struct {
     void* codes;          /* device, rows of bytes */
     int64_t code_stride;  /* bytes between rows */
@@ -739,7 +739,7 @@ speca_status_t speca_layer_norm8(speca_layer_t* layer, int32_t kind, int32_t dim
  * of 255) makes its row or column of the product NaN. The products are exact; the tensor cores add 32 at a time to a sum and cut each at some
  * 2^-25 of the largest among them and the sum, so that sum_k is off by at most (1.04 s + 73) 2^-24 sum_k |a w| when s elements are summed at once:
  * k at most, and at most 4096 for outputs in fp32 with k from 8193 to 32768, whose shares are added with rounding (k / 8 beyond). Of terms of one
- * sign s / 2^27 of the sum gets lost that way, so k ends at SPECA_MAX_K8. A row's result does not depend on the mask: no atomics on values, an order of sums that the
+ * sign up to s / 2^27 of the sum gets lost that way (uniform positive values: 3e-6 at s = 8192), so k ends at SPECA_MAX_K8. A row's result does not depend on the mask: no atomics on values, an order of sums that the
  * sizes fix (the number of rows among them: k is shared out where there are few).
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, UNSUPPORTED (a stride of 2^40 bytes or more), CUDA.
  */

@@ -730,7 +730,7 @@ _NO_STRIDE, _NO_MODULATIONS = (0,), (None, None, None)
 
 
 class SpecaLayer:
-    """The parts of a verification layer that are not plain matrix products, over packed sequences: sequence s of a
+    """The parts of a verification layer, its matrix products in 8 bits among them, over packed sequences: sequence s of a
     ``[rows, ...]`` tensor is rows ``q_start[s]`` to ``q_start[s + 1] - 1``. Owns the workspace and the handle. Tensors
     may be strided views whose last dimension is dense; outputs are the caller's."""
 

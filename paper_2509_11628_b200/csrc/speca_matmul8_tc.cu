@@ -689,9 +689,10 @@ cudaError_t dispatch(const Matmul8Params& p, Kind kind, int sm_count, cudaStream
 }
 
 // The tensor cores cut what they add to a sum, each of 32 products, at about 2^-25 of the sum, so that a sum over all of k comes out short: of terms of
-// either sign by 6.5e-7 of its size at k = 8192 and by 1.4e-6 at 16384 (of one sign by k / 2^27), which bf16 and 8 bits do not see. Outputs in fp32 with
-// more than 8192 elements of k are therefore left to the kernel for few rows, which adds up shares of k with rounding: 2304 x 4096 x 16384 is 3.7e-7
-// off in place of 1.9e-6, for 193 us in place of 101. At 8192 the pair's 9e-7 stay (58 us; shares would take 134).
+// either sign by 6.5e-7 of its size at k = 8192 and by 1.4e-6 at 16384 (of one sign by k / 2^27 at most; uniform positive values by 2.7e-6 at 8192),
+// which bf16 and 8 bits do not see. Outputs in fp32 with more than 8192 elements of k are therefore left to the kernel for few rows, which adds up
+// shares of k with rounding: 2304 x 4096 x 16384 is 3.7e-7 off in place of 1.9e-6, for 193 us in place of 101. At 8192 the pair's 9e-7 stay (58 us;
+// shares would take 134).
 constexpr int kShareBlocks = 32, kLongBlocks = 64;
 int shares_of(const Matmul8Params& p, int dtype) {
     const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
