@@ -6,7 +6,7 @@
 // so its largest magnitude takes three shuffles. y is rounded once, to its code. Bound by memory in the end, by instructions and by the blocks that
 // registers leave room for on the way there: 20926 rows x 4096 bf16 with branch, gate and weight 113 us (5.3 TB/s), as they are 49 us (5.2 TB/s); with 8 elements a
 // lane (four shuffles, one scale and one set of addresses for half as much) 210 and 84. Tried and not kept, 20926 x 4096: weight, scale and shift loaded in
-// front of the sums 155 us (registers), bounds on the registers 114 to 146.
+// front of the sums 155 us (registers), asked into L1 there 117, bounds on the registers 114 to 146, the row map read before the wait 118.
 #include "speca_early.cuh"
 #include "speca_eight_common.cuh"
 #include "speca_rows_common.cuh"
