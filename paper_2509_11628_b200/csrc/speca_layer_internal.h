@@ -138,16 +138,13 @@ struct Matmul8Params {
     uint32_t* gave_up;
 };
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
-// The kernel for few rows: rows of a tile, and how many blocks share the k of a tile of 128 features (a cluster), each with four stages of 128 at
-// least: two or four where all blocks run at once, two to an SM, eight where one to an SM does. 64 rows x 4096 x 4096: 128 blocks of four shares
-// 10.0 us, 256 of eight 11.4; 256 rows x 4096 x 14336: 256 of four 23, 128 of two 30; 16 rows x 1152 x 4608: 72 of eight 6.4, 36 of four 7.4.
+// The kernel for few rows: rows of a tile (16, 32, 64 or 128), and how many blocks share the k of a tile of 128 features (a cluster).
 constexpr int kFewRanks = 8;
-inline int few_rows(int m) { return m <= 16 ? 16 : m <= 32 ? 32 : m <= 64 ? 64 : 128; }
-inline int few_ranks(int64_t tiles, int k_blocks, int sm_count) {
-    int ranks = 1;
-    while (2 * ranks <= kFewRanks && 2 * ranks * tiles <= (2 * ranks < kFewRanks ? 2 : 1) * sm_count && k_blocks >= 8 * ranks) ranks *= 2;
-    return ranks;
-}
-cudaError_t launch_matmul8_few(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
+struct FewPlan {
+    int rows, ranks;
+    double us;  // about
+};
+FewPlan plan_few(const Matmul8Params& p, int sm_count);
+cudaError_t launch_matmul8_few(const Matmul8Params& p, const FewPlan& plan, int dtype, cudaStream_t stream);
 
 }  // namespace speca

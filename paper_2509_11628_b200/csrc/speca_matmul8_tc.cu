@@ -660,25 +660,22 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
 
 // The three kernels' times in us, as fits to what they measured over 1 to 4096 rows, 1152 to 14336 features and elements of k
 // (largest error 25 %; what matters is where they cross). A start, then rounds of tiles over the SMs, each with a step for 128 elements of
-// k and an end. Few rows: bound by the weights' bytes at 6.5 TB/s, or by their steps. In us, rows x features x k, few / one SM / a pair:
+// k and an end, longer where rows do not start on 16 bytes; all read the weights at 6.5 TB/s at best. In us, rows x features x k, few / one SM / a pair:
 // 1 x 4096 x 4096 8.5 / 12.6 / 15.6;  512 x 4096 x 4096 17.7 / 13.3 / 16.6;  384 x 4096 x 14336 34 / 40 / 41;  1024 x 4096 x 14336 63 / 73 / 48;
-// 64 x 4608 x 1152 8.1 / 6.9 / 8.8;  4096 x 1152 x 4608 30 / 27 / 30;  4096 x 14336 x 4096 307 / 252 / 180.
+// 64 x 4608 x 1152 6.2 / 6.9 / 8.8;  4096 x 1152 x 4608 30 / 27 / 30;  4096 x 14336 x 4096 307 / 252 / 180.
 // A mask, which only the device knows, is taken to leave three rows of four where tiles of one SM and of a pair are compared: of 16 samples of 256 rows, 11
 // of them active, x 1152 x 4608 a pair's tiles fill one round in place of two (23.7 us, 31.4). These two add in the same order, so a row's
 // bits do not depend on the mask; shares of k add in another, so few rows are told apart without it.
 enum Kind { kFew, kOne, kPair };
-Kind choose(const Matmul8Params& p, int sm_count) {
+Kind choose(const Matmul8Params& p, const FewPlan& few, int sm_count) {
     const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
     auto tiles = [&](int64_t m, int64_t rows, int64_t features) { return (m + rows - 1) / rows * ((p.n + features - 1) / features); };
     auto rounds = [](int64_t n, int64_t places) { return static_cast<double>((n + places - 1) / places); };
-    const int rows = few_rows(p.m);
     // (tiles of one SM with 16 rows or fewer took half as long again: 22 us for 14336 x 4096, 15.4 from 32 rows on)
-    auto one = [&](int64_t m) { return 4.2 + rounds(tiles(m, kRows, 128), sm_count) * (0.7 + (rows == 16 ? 0.45 : 0.27) * kb); };
+    auto one = [&](int64_t m) { return 4.2 + rounds(tiles(m, kRows, 128), sm_count) * (0.7 + (p.m <= 16 ? 0.45 : 0.27) * kb); };
     auto pair = [&](int64_t m) { return 4.5 + rounds(tiles(m, 2 * kRows, 256), sm_count / 2) * (1.0 + 0.34 * kb); };
-    const int64_t few = tiles(p.m, rows, kRows), ranks = few_ranks(few, static_cast<int>(kb), sm_count);
-    const double start = rows == 16 ? 6.0 : rows == 32 ? 6.8 : rows == 64 ? 8.0 : 10.5;
-    const double t_few = start + std::max(static_cast<double>(p.n) * p.k / 6.5e6, rounds(few * ranks, 2 * sm_count) * rounds(kb, ranks) * 0.5);
-    if (t_few <= one(p.m) && t_few <= pair(p.m)) return kFew;
+    const double least = static_cast<double>(p.n) * p.k / 6.5e6 + (p.m <= 64 ? 8.0 : 6.9), odd = p.vectors ? 0.0 : 3.0;
+    if (few.us <= std::max(std::min(one(p.m), pair(p.m)) + odd, least)) return kFew;
     const int64_t m = p.dev_mask != nullptr ? p.m - p.m / 4 : p.m;
     return one(m) <= pair(m) ? kOne : kPair;
 }
@@ -708,8 +705,9 @@ cudaError_t launch_matmul8(const Matmul8Params& given, int dtype, int sm_count, 
     if (given.m == 0) return cudaSuccess;
     Matmul8Params p = given;
     p.shares = shares_of(p, dtype);
-    const Kind kind = p.shares > 1 ? kFew : choose(p, sm_count);
-    if (kind == kFew) return launch_matmul8_few(p, dtype, sm_count, stream);
+    const FewPlan few = plan_few(p, sm_count);
+    const Kind kind = p.shares > 1 ? kFew : choose(p, few, sm_count);
+    if (kind == kFew) return launch_matmul8_few(p, few, dtype, stream);
     return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, kind, sm_count, stream) : dispatch<SPECA_F32>(p, kind, sm_count, stream);
 }
 

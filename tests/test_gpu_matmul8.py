@@ -53,7 +53,8 @@ def blank(S, rows, n, fill=0x55):
 # rows, features, k
 FEW = [(1, 1, 1), (1, 33, 16), (3, 77, 130), (8, 256, 512), (16, 128, 1152), (17, 1000, 1155), (32, 513, 4608), (64, 640, 2000), (5, 4000, 700),
        (100, 300, 8200), (4, 300, 16384)]
-ONE = [(65, 129, 128), (128, 128, 64), (257, 513, 1000), (300, 1000, 1155), (1000, 77, 31), (640, 640, 640)]
+ONE = [(65, 129, 128), (128, 128, 64), (257, 513, 1000), (300, 1000, 1155), (1000, 77, 31), (640, 640, 640), (1100, 1500, 520), (1100, 1501, 1000), (1150, 1733, 31),
+       (1025, 1280, 640)]
 PAIR = [(2100, 4100, 300), (4099, 2048, 1152), (1025, 14336, 520), (2500, 4000, 17)]
 
 
@@ -81,7 +82,7 @@ def test_whole_numbers_are_exact(S, m, n, k):
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("kind", ["none", "gelu", "silu"])
-@pytest.mark.parametrize("m,n,k", [(7, 300, 1155), (400, 333, 520), (2100, 4096, 384)])
+@pytest.mark.parametrize("m,n,k", [(7, 300, 1155), (400, 333, 520), (1100, 1501, 520), (1100, 1504, 520), (2100, 4096, 384)])
 def test_epilogues(S, dt, kind, m, n, k):
     g = gen(m)
     lens = [m // 3, 0, m - m // 3 - 2, 2]
@@ -120,7 +121,8 @@ def test_epilogues(S, dt, kind, m, n, k):
 
 
 # the third goes to tiles of one SM without a mask and to a pair's with one
-@pytest.mark.parametrize("m,n,k", [(12, 200, 300), (500, 300, 256), (4096, 1152, 4608), (4608, 2304, 256), (100, 300, 8200)])
+@pytest.mark.parametrize("m,n,k", [(12, 200, 300), (500, 300, 256), (4096, 1152, 4608), (4608, 2304, 256), (100, 300, 8200), (1100, 1501, 520),
+                                   (1100, 1504, 520)])
 def test_masked_samples_are_left_alone_and_others_do_not_see_it(S, m, n, k):
     g = gen(1)
     lens = [m // 4, 0, 1, m // 2, m - m // 4 - 1 - m // 2]
@@ -157,7 +159,7 @@ def test_masked_samples_are_left_alone_and_others_do_not_see_it(S, m, n, k):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-@pytest.mark.parametrize("m,n,k", [(9, 130, 200), (300, 264, 200), (2304, 4099, 130)])
+@pytest.mark.parametrize("m,n,k", [(9, 130, 200), (300, 264, 200), (1100, 1501, 200), (1100, 1504, 200), (2304, 4099, 130)])
 def test_strides_offsets_and_in_place(S, dt, m, n, k):
     g = gen(4)
     a, w = real(g, m, k), real(g, 2 * n + 3, k, k ** -0.5)
@@ -198,7 +200,7 @@ def test_strides_offsets_and_in_place(S, dt, m, n, k):
     assert bool((buf[:, :5] == 0x44).all() and (buf[:, 5 + n:] == 0x44).all() and (sc[:, :5] == 0x44).all() and (sc[:, 5 + m:] == 0x44).all())
 
 
-@pytest.mark.parametrize("m,n,k", [(6, 140, 300), (300, 264, 300), (2304, 4100, 300)])
+@pytest.mark.parametrize("m,n,k", [(6, 140, 300), (300, 264, 300), (1100, 1504, 300), (2304, 4100, 300)])
 def test_nan_stays_in_its_row_and_column(S, m, n, k):
     g = gen(6)
     a, w = whole(g, m, k), whole(g, n, k)
@@ -221,7 +223,7 @@ def test_nan_stays_in_its_row_and_column(S, m, n, k):
     assert torch.equal(m8.codes.double()[~nan], codes[~nan]) and torch.equal(E.bytes_of(m8).long(), byte)
 
 
-@pytest.mark.parametrize("m,n", [(5, 140), (300, 264), (2304, 4100)])
+@pytest.mark.parametrize("m,n", [(5, 140), (300, 264), (1100, 1504), (2304, 4100)])
 @pytest.mark.parametrize("ea,ew", [(27, 227), (227, 27), (77, 177), (67, 67), (187, 180)])
 def test_scales_far_from_one(S, m, n, ea, ew):
     # products of scales from 2^-120 to 2^113, of factors up to 2^100
