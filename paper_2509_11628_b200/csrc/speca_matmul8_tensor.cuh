@@ -140,9 +140,12 @@ __device__ __forceinline__ void mma8(uint32_t d, uint64_t a, uint64_t b, uint32_
             : "memory");
 }
 
-// Scales of four blocks of a row; those of rows that do not exist: 1.
+// Scales of four blocks of a row; those of rows that do not exist: 1. An ordinary load behind the wait for the kernel in front, which may be writing them
+// when this one begins: the read-only path (__ldg) is for what nobody writes while a kernel runs.
 __device__ __forceinline__ uint32_t scale_word(const uint8_t* scales, int64_t stride, int group, int row, int rows) {
-    return row < rows ? __ldg(reinterpret_cast<const uint32_t*>(scales + group * stride) + row) : 0x7f7f7f7fu;
+    uint32_t word = 0x7f7f7f7fu;
+    if (row < rows) asm volatile("ld.global.b32 %0, [%1];" : "=r"(word) : "l"(reinterpret_cast<const uint32_t*>(scales + group * stride) + row) : "memory");
+    return word;
 }
 
 }  // namespace
