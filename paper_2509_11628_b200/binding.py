@@ -793,7 +793,9 @@ class SpecaLayer:
 
     def _stream(self, stream):
         """The stream's address; of the device's current stream without the Stream object around it (2 us a call)."""
-        return torch._C._cuda_getCurrentRawStream(self.index) if stream is None else stream
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self.index)
+        return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream
 
     def _modulations(self, tensors, dim):
         """Addresses of gate, scale and shift ([n_seqs, dim] or None) and their one row stride."""
