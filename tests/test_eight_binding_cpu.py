@@ -35,9 +35,8 @@ def layer_of(S, monkeypatch, rows=6):
     """A layer over `rows` rows whose tensors are the host's, with a library that only listens."""
     lib = Library()
     layer = object.__new__(S.SpecaLayer)
-    layer.handle, layer.lib, layer.index, layer.device = 1234, lib, -1, torch.device("cpu")
+    layer.handle, layer.lib, layer.index, layer.device = None, lib, -1, torch.device("cpu")
     layer.n_seqs, layer.rows, layer.torch_dtype = 2, rows, torch.bfloat16
-    monkeypatch.setattr(S.SpecaLayer, "close", lambda self: None)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 77, raising=False)
     return layer, lib
 
