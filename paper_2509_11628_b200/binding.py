@@ -193,6 +193,13 @@ def _stream_ptr(stream) -> Optional[int]:
     return int(stream) or None
 
 
+def _stream_object(stream, device) -> Optional[torch.cuda.Stream]:
+    """The stream as an object of torch's; None for the current one."""
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(int(stream), device) if int(stream) else torch.cuda.default_stream(device)
+
+
 def _doubles(xs: Sequence[float]):
     return (ctypes.c_double * len(xs))(*[float(x) for x in xs])
 
@@ -708,7 +715,8 @@ class Matrix8:
 
 
 def quantize8(x: torch.Tensor, out: Optional[Matrix8] = None, stream=None) -> Matrix8:
-    """Weights ``[rows, dim]`` (fp32 or bf16, on a GPU) into 8 bits."""
+    """Weights ``[rows, dim]`` (fp32 or bf16, on a GPU) into 8 bits. Without ``out`` the matrix is made on ``stream``, as under
+    ``torch.cuda.stream``."""
     dtype = {t: code for code, t in _TORCH_DTYPES.items()}.get(x.dtype)
     if dtype is None:
         raise TypeError("fp32 or bf16 is expected, not %s" % x.dtype)
@@ -716,7 +724,10 @@ def quantize8(x: torch.Tensor, out: Optional[Matrix8] = None, stream=None) -> Ma
         raise TypeError("a tensor on a GPU is expected")
     if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
         raise ValueError("a matrix with a dense last dimension is expected")
-    out = Matrix8.empty(*x.shape, x.device) if out is None else out
+    if out is None:
+        # its zeros are written on the stream that the codes are, or they could come behind them
+        with torch.cuda.stream(_stream_object(stream, x.device)):
+            out = Matrix8.empty(*x.shape, x.device)
     if out.shape != x.shape:
         raise ValueError("out: shape %s is expected, not %s" % (tuple(x.shape), tuple(out.shape)))
     if out.index != x.get_device():
