@@ -689,7 +689,8 @@ class SpecaCache:
 class Matrix8:
     """A matrix in 8 bits: ``codes`` float8_e4m3fn ``[rows, dim]`` (rows may be strided, the last dimension is dense) and
     ``scales`` float8_e8m0fnu ``[ceil(dim / 512), rows, 4]``: the scale of column c of row r is ``scales[c // 512, r, c // 128 % 4]``.
-    Rows of codes that start on multiples of 16 bytes, as ``empty`` lays them out, can enter a product."""
+    Rows of codes that start on multiples of 16 bytes, as ``empty`` lays them out, can enter a product. A matrix stands for the memory it was
+    made of: ``codes`` and ``scales`` cannot be assigned, and one whose tensors have been moved (``set_``, a storage resized) is refused."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
         if codes.dtype is not torch.float8_e4m3fn or scales.dtype is not torch.float8_e8m0fnu:
@@ -701,10 +702,24 @@ class Matrix8:
         rows, dim = codes.shape
         if (dim > 1 and codes.stride(1) != 1) or (rows > 0 and scales.shape[0] > 0 and (scales.stride(2) != 1 or (rows > 1 and scales.stride(1) != 4))):
             raise TypeError("the last dimension of codes, and the last two of scales, must be dense")
-        self.codes, self.scales, self.shape, self.device = codes, scales, codes.shape, codes.device
-        self.index = codes.get_device()
-        self.desc = Matrix8Desc(codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0))
+        # tensors of its own, so that what is done to the caller's (transposed or resized in place) is not done to these
+        codes, scales = codes.detach(), scales.detach()
+        self.__dict__.update(codes=codes, scales=scales)
+        self.shape, self.device, self.index = codes.shape, codes.device, codes.get_device()
+        self.codes_now, self.scales_now = codes.data_ptr, scales.data_ptr
+        self.codes_at, self.scales_at = codes.data_ptr(), scales.data_ptr()
+        self.desc = Matrix8Desc(self.codes_at, codes.stride(0), self.scales_at, scales.stride(0))
         self.ref = ctypes.byref(self.desc)
+
+    def __setattr__(self, name, value):   # (properties would cost each reader 0.1 us)
+        if name in ("codes", "scales"):
+            raise AttributeError("%s of a Matrix8 cannot be assigned: make another from the tensors" % name)
+        object.__setattr__(self, name, value)
+
+    def stand(self, name: str) -> None:
+        """Refuses a matrix whose memory has gone."""
+        if self.codes_now() != self.codes_at or self.scales_now() != self.scales_at:
+            raise ValueError("%s: the matrix's tensors no longer have the memory it was made of" % name)
 
     @classmethod
     def empty(cls, rows: int, dim: int, device="cuda:0") -> "Matrix8":
@@ -732,6 +747,7 @@ def quantize8(x: torch.Tensor, out: Optional[Matrix8] = None, stream=None) -> Ma
         raise ValueError("out: shape %s is expected, not %s" % (tuple(x.shape), tuple(out.shape)))
     if out.index != x.get_device():
         raise TypeError("out: a matrix on %s is expected" % x.device)
+    out.stand("out")
     speca_quantize8(x.shape[0], x.shape[1], x.data_ptr(), x.stride(0), dtype, out.desc, out.index,
                     torch._C._cuda_getCurrentRawStream(out.index) if stream is None else stream)
     return out
@@ -860,23 +876,28 @@ class SpecaLayer:
 
     def _matrix8(self, m, name, shape):
         """What the library takes for a Matrix8 of this shape."""
+        if type(m) is Matrix8 and m.shape == shape and m.index == self.index and m.codes_now() == m.codes_at and m.scales_now() == m.scales_at:
+            return m.ref
         if not isinstance(m, Matrix8):
             raise TypeError("%s: a Matrix8 is expected" % name)
         if m.index != self.index:
             raise TypeError("%s: a matrix on %s is expected" % (name, self.device))
         if m.shape != shape:
             raise ValueError("%s: shape %s is expected, not %s" % (name, tuple(shape), tuple(m.shape)))
+        m.stand(name)
         return m.ref
 
     def _active(self, active):
-        return None if active is None else self._tensor(active, "active", (self.n_seqs,), torch.uint8)[0]
+        return self._tensor(active, "active", (self.n_seqs,), torch.uint8)[0]
 
     def quantize8(self, x, out, active=None, stream=None):
         """The rows of x in 8 bits."""
         dim = x.shape[-1]
         shape = (self.rows, dim)
         px, sx = self._tensor(x, "x", shape, self.torch_dtype)
-        status = self.lib.speca_layer_quantize8(self.handle, dim, px, sx[0], self._active(active), self._matrix8(out, "out", shape), self._stream(stream))
+        status = self.lib.speca_layer_quantize8(self.handle, dim, px, sx[0], None if active is None else self._active(active),
+                                                self._matrix8(out, "out", shape),
+                                                torch._C._cuda_getCurrentRawStream(self.index) if stream is None else self._stream(stream))
         if status:
             _check_layer(status, self.handle)
 
@@ -893,8 +914,10 @@ class SpecaLayer:
             (pg, ps, pt), mod_stride = _NO_MODULATIONS, 0
         else:
             (pg, ps, pt), mod_stride = self._modulations((gate, scale, shift), dim)
-        status = self.lib.speca_layer_norm8(self.handle, kind, dim, px, sx[0], pb, sb[0], pg, ps, pt, mod_stride, pw, self._active(active), po, so[0],
-                                            self._matrix8(out, "out", shape), self._stream(stream))
+        status = self.lib.speca_layer_norm8(self.handle, kind, dim, px, sx[0], pb, sb[0], pg, ps, pt, mod_stride, pw,
+                                            None if active is None else self._active(active), po, so[0],
+                                            self._matrix8(out, "out", shape),
+                                            torch._C._cuda_getCurrentRawStream(self.index) if stream is None else self._stream(stream))
         if status:
             _check_layer(status, self.handle)
 
@@ -905,7 +928,8 @@ class SpecaLayer:
             raise TypeError("w: a Matrix8 is expected")
         (n, k), dt, tensor = w.shape, self.torch_dtype, self._tensor
         shape = (self.rows, n)
-        ra, rw = self._matrix8(a, "a", (self.rows, k)), self._matrix8(w, "w", w.shape)
+        ra = self._matrix8(a, "a", (self.rows, k))
+        rw = w.ref if w.index == self.index and w.codes_now() == w.codes_at and w.scales_now() == w.scales_at else self._matrix8(w, "w", (n, k))
         if isinstance(out, Matrix8):
             eight, po, so = self._matrix8(out, "out", shape), None, _NO_STRIDE
         else:
@@ -913,8 +937,9 @@ class SpecaLayer:
         pb = None if bias is None else tensor(bias, "bias", (n,), dt)[0]
         pr, sr = (None, _NO_STRIDE) if residual is None else tensor(residual, "residual", shape, dt)
         pg, sg = (None, _NO_STRIDE) if gate is None else tensor(gate, "gate", (self.n_seqs, n), dt)
-        status = self.lib.speca_layer_matmul8(self.handle, n, k, ra, rw, pb, activation, pr, sr[0], pg, sg[0], self._active(active), po, so[0], eight,
-                                              self._stream(stream))
+        status = self.lib.speca_layer_matmul8(self.handle, n, k, ra, rw, pb, activation, pr, sr[0], pg, sg[0],
+                                              None if active is None else self._active(active), po, so[0], eight,
+                                              torch._C._cuda_getCurrentRawStream(self.index) if stream is None else self._stream(stream))
         if status:
             _check_layer(status, self.handle)
 

@@ -59,3 +59,41 @@ def test_streams_reach_the_library_as_addresses(S, monkeypatch, make, address):
     for _, args in lib.calls:
         assert args[-1] == address
         ctypes.c_void_p(args[-1])   # what the library's own argument takes
+
+
+def product(S, monkeypatch, break_it):
+    layer, lib = layer_of(S, monkeypatch)
+    codes = torch.zeros(6, 256, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    scales = torch.zeros(1, 6, 4, dtype=torch.uint8).view(torch.float8_e8m0fnu)
+    a, w, out = S.Matrix8(codes, scales), S.Matrix8.empty(32, 256, "cpu"), torch.zeros(6, 32, dtype=torch.bfloat16)
+    at = a.desc.codes, a.desc.scales
+    break_it(a, codes, scales)
+    try:
+        layer.matmul8(a, w, out)
+    finally:
+        assert (a.desc.codes, a.desc.scales) == at
+    return lib.calls
+
+
+def other():
+    return torch.zeros(6, 256, dtype=torch.uint8).view(torch.float8_e4m3fn)
+
+
+def test_a_matrix_keeps_its_tensors(S, monkeypatch):
+    m = S.Matrix8.empty(6, 256, "cpu")
+    with pytest.raises(AttributeError):
+        m.codes = other()
+    with pytest.raises(AttributeError):
+        m.scales = m.scales.clone()
+    # what the caller does to tensors of its own is nothing to the matrix, which keeps the memory
+    assert len(product(S, monkeypatch, lambda a, codes, scales: codes.set_(other()))) == 1
+    assert len(product(S, monkeypatch, lambda a, codes, scales: scales.transpose_(0, 1))) == 1
+
+
+@pytest.mark.parametrize("break_it", [lambda a, codes, scales: a.codes.set_(other()),
+                                      lambda a, codes, scales: a.scales.set_(a.scales.clone()),
+                                      lambda a, codes, scales: a.codes.untyped_storage().resize_(0),
+                                      lambda a, codes, scales: scales.untyped_storage().resize_(0)])
+def test_a_matrix_whose_memory_has_gone_is_refused(S, monkeypatch, break_it):
+    with pytest.raises(ValueError, match="a: the matrix"):
+        product(S, monkeypatch, break_it)
