@@ -693,8 +693,8 @@ typedef struct {
 } speca_matrix8_t;
 
 typedef enum { SPECA_NORM_LAYER = 0, SPECA_NORM_RMS = 1 } speca_norm_t;
-/* GELU is the tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))); SILU is x / (1 + exp(-x)). A factor of x below 2^-63 may be taken
- * as 2^-63. */
+/* GELU is the tanh form, x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))); SILU is x / (1 + exp(-x)). A factor of x may be 2^-62 too
+ * low, but not below zero. */
 typedef enum { SPECA_ACT_NONE = 0, SPECA_ACT_GELU = 1, SPECA_ACT_SILU = 2 } speca_activation_t;
 
 /*

@@ -96,13 +96,19 @@ enum Epilogue { kPlain, kResidual, kEight };
 
 // t / (1 + 2^x), two at a time with one reciprocal, 1 / a = b / (a b): the special function unit forms 16 a cycle, and is a quarter busy in a
 // product with GELU (4096 x 4608 x 1152; with half of the exponentials as polynomials instead the product took as long). So that
-// a b stays finite x is held at 63: below 2^-63 t the result is that.
+// a b stays finite, also next to a NaN, x is held at 63, where the factor is 2^-63. A little more than that is taken off every factor and none goes below
+// zero, so that from there on it is zero, whatever t (NaN of one that is not finite). (Choosing between factor and zero instead took 1.5 % longer.)
+__device__ __forceinline__ float factor(float other, float r) {
+    float f;
+    asm("fma.rn.sat.f32 %0, %1, %2, %3;" : "=f"(f) : "f"(other), "f"(r), "f"(-0x1.0001p-63f));
+    return f;
+}
 __device__ __forceinline__ uint64_t times_sigmoid2(uint64_t t, uint64_t x) {
     float x0, x1, d0, d1, r;
     unpair(x, x0, x1);
     unpair(add2(pair(ex2(fminf(x0, 63.f)), ex2(fminf(x1, 63.f))), pair(1.f, 1.f)), d0, d1);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
-    return mul2(t, mul2(pair(d1, d0), pair(r, r)));
+    return mul2(t, pair(factor(d1, r), factor(d0, r)));
 }
 __device__ __forceinline__ void activate32(float (&v)[32], int act) {
     if (act == SPECA_ACT_GELU) {
