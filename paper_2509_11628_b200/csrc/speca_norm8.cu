@@ -199,11 +199,24 @@ __global__ void __launch_bounds__(NT) norm8_kernel(const __grid_constant__ Norm8
     }
 }
 
-// Rows too long for the registers of one block: passes over memory, the later ones out of L2. A thread meets the same elements in each.
+// Sum of what the row's 1024 threads hold in 64 bits.
+__device__ __forceinline__ double sum_long(double x, double* red) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = x;
+    __syncthreads();
+    x = red[threadIdx.x % 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// Rows too long for the registers of one block: passes over memory, the later ones out of L2. A thread meets the same elements in each. It adds up to 2^21
+// of them: those of one block of 128 (16) in 32 bits, the blocks in 64. (All in 32 bits, squares of like size came out 1.4e-4 off at 2^24 elements and 2e-2 at 2^31.)
 template <int DT>
 __global__ void __launch_bounds__(1024) norm8_long_kernel(const __grid_constant__ Norm8Params p) {
     using T = typename Type<DT>::T;
-    __shared__ float red[2][32];
+    __shared__ double red[2][32];
     const int row = blockIdx.x;
     wait_for_stream();
     const int seq = p.row_seq[row];
@@ -221,18 +234,24 @@ __global__ void __launch_bounds__(1024) norm8_long_kernel(const __grid_constant_
     };
     float mean = 0.f;
     if (p.centre) {
-        float sum = 0.f;
-        for (uint32_t f = start; f < dim; f += kStep)
-            for (uint32_t c = f + l; c < min(f + kBlock8, dim); c += kLanes) sum += value(c);
-        mean = sum_row<1024>(sum, red[0]) / p.dim;
+        double sum = 0;
+        for (uint32_t f = start; f < dim; f += kStep) {
+            float part = 0.f;
+            for (uint32_t c = f + l; c < min(f + kBlock8, dim); c += kLanes) part += value(c);
+            sum += part;
+        }
+        mean = static_cast<float>(sum_long(sum, red[0]) / p.dim);
     }
-    float sq = 0.f;
-    for (uint32_t f = start; f < dim; f += kStep)
+    double sq = 0;
+    for (uint32_t f = start; f < dim; f += kStep) {
+        float part = 0.f;
         for (uint32_t c = f + l; c < min(f + kBlock8, dim); c += kLanes) {
             const float d = value(c) - mean;
-            sq = fmaf(d, d, sq);
+            part = fmaf(d, d, part);
         }
-    const float rstd = 1.f / sqrtf(sum_row<1024>(sq, red[1]) / p.dim + p.eps);
+        sq += part;
+    }
+    const float rstd = 1.f / sqrtf(static_cast<float>(sum_long(sq, red[1]) / p.dim) + p.eps);
     // the blocks of a warp go through the loop together
     for (uint32_t f = start, first = threadIdx.x / 32 * (32 / kLanes) * kBlock8; first < dim; f += kStep, first += kStep) {
         float v[kPer];
