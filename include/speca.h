@@ -684,7 +684,7 @@ speca_status_t speca_layer_attention(speca_layer_t* layer, const void* q, int64_
  * e4m3 has no infinity: a value that is not finite becomes NaN, and the others of its block keep their scale.
  */
 #define SPECA_BLOCK8 128 /* elements that share a scale */
-#define SPECA_MAX_K8 262144 /* most elements of a row of a product's operands: a sum of that many of one sign may lose a bf16 rounding, 2^-9 */
+#define SPECA_MAX_K8 262144 /* most elements of a row of a product's operands: eight shares of as many as may be summed at once, 32768 */
 typedef struct {
     void* codes;          /* device, rows of bytes */
     int64_t code_stride;  /* bytes between rows */
@@ -738,10 +738,11 @@ speca_status_t speca_layer_norm8(speca_layer_t* layer, int32_t kind, int32_t dim
  * Rows of inactive sequences are not written, and tiles of rows that hold no others are not computed. A NaN (code 0x7f or 0xff, or a scale byte
  * of 255) makes its row or column of the product NaN. The products are exact; the tensor cores add 32 at a time to a sum and cut each at some
  * 2^-25 of the largest among them and the sum, so that sum_k is off by at most (1.04 s + 73) 2^-24 sum_k |a w| when s elements are summed at once:
- * k at most, and at most 4096 for outputs in fp32 with k from 8193 to 32768, whose shares are added with rounding (k / 8 beyond). Of terms of one
- * sign up to s / 2^27 of the sum gets lost that way (uniform positive values: 3e-6 at s = 8192), so k ends at SPECA_MAX_K8. A row's result does
- * not depend on the mask: no atomics on values, an order of sums that the sizes and the rows' alignment fix (the number of rows among them: k is
- * shared out where there are few).
+ * k or 32768 at most, and at most 4096 for outputs in fp32 with k from 8193 to 32768 (k / 8 beyond); shares are added with rounding. Of s terms
+ * next to a large one of their sign, each below 2^-25 of it, up to s / 2^25 of the sum may be lost (uniform positive values: 3e-6 at s = 8192). In 8 bits a sum that
+ * is a few roundings off moves its code by a step at most; where it is its block's largest magnitude and next to 448 2^e, the scale, and with it all codes of
+ * the block, may be those of the next power of two. A row's result does not depend on the mask: no atomics on values, an order of sums that the
+ * sizes and the rows' alignment fix (the number of rows among them: k is shared out where there are few).
  * Errors: INVALID_ARG, SHAPE, ALIGNMENT, UNSUPPORTED (a stride of 2^40 bytes or more), CUDA.
  */
 speca_status_t speca_layer_matmul8(speca_layer_t* layer, int32_t n, int32_t k, const speca_matrix8_t* a, const speca_matrix8_t* w,

@@ -134,7 +134,7 @@ struct Matmul8Params {
     int32_t vectors;  // rows of bias, residual, gate and out (or the codes) start on 16 bytes
     int32_t wide;     // those of the codes on 32
     int32_t boxes;    // the copy engine can address the output (set by the launch)
-    int32_t shares;   // of k that fp32 sums are added up from at least (set by the launch)
+    int32_t shares;   // of k that sums are added up from at least (set by the launch)
     uint32_t* gave_up;
 };
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);

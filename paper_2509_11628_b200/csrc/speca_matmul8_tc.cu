@@ -691,19 +691,21 @@ cudaError_t dispatch(const Matmul8Params& p, Kind kind, int sm_count, cudaStream
     return kind == kOne ? run<DT, 1, 128>(p, sm_count, stream) : run<DT, 2, 256>(p, sm_count, stream);
 }
 
-// The tensor cores cut what they add to a sum, each of 32 products, at about 2^-25 of the sum, so that a sum over all of k comes out short: of terms of
-// either sign by 6.5e-7 of its size at k = 8192 and by 1.4e-6 at 16384 (of one sign by k / 2^27 at most; uniform positive values by 2.7e-6 at 8192),
-// which bf16 and 8 bits do not see. Outputs in fp32 with more than 8192 elements of k are therefore left to the kernel for few rows, which adds up
-// shares of k with rounding: 2304 x 4096 x 16384 is 3.7e-7 off in place of 1.9e-6, for 193 us in place of 101. At 8192 the pair's 9e-7 stay (58 us;
-// shares would take 134).
-constexpr int kShareBlocks = 32, kLongBlocks = 64;
+// The tensor cores cut what they add to a sum, each step of 32 products, at about 2^-25 of the largest of the step's terms and the sum, so that a sum over all of k
+// comes out short: of normal values by 2.2e-7 of its size at k = 4096 and 5.0e-7 at 8192 (twice that in rows with a value 20 times the others), of uniform positive
+// ones by 9.4e-7 and 2.7e-6. At worst, of s terms next to a large one, each just below 2^-25 of it, s 2^-25 of the sum are lost (half of them were, where tried).
+// bf16 and 8 bits see that where it passes half a rounding, 2^-10: so at most 32768 elements are summed at once. Outputs in fp32 with more than 8192
+// elements take shares of 4096 (k / 8 beyond 32768): 2304 x 4096 x 16384 is 3.7e-7 off in place of 1.9e-6, for 193 us in place of 101. At 8192 the pair's 9e-7 stay
+// (58 us; shares would take 134). Shares of k are added up with rounding, by the kernel for few rows.
 int shares_of(const Matmul8Params& p, int dtype) {
     const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
-    if (dtype != SPECA_F32 || p.out == nullptr || kb <= kLongBlocks) return 1;
+    const bool exact = dtype == SPECA_F32 && p.out != nullptr;
+    if (kb <= (exact ? 64 : 256)) return 1;
     int shares = 2;
-    while (shares < kFewRanks && shares * kShareBlocks < kb) shares *= 2;
+    while (shares < kFewRanks && shares * (exact ? 32 : 256) < kb) shares *= 2;
     return shares;
 }
+static_assert(SPECA_MAX_K8 <= kFewRanks * 32768, "no share is longer");
 
 }  // namespace
 
