@@ -15,7 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libspeca.so")
 SOURCES = ["speca_kernels.cu", "speca_static.cu", "speca_layer_rows.cu", "speca_attention_bf16.cu", "speca_attention_f32.cu", "speca_attention_join.cu",
-           "speca_norm8.cu", "speca_matmul8_tc.cu", "speca_matmul8_few.cu", "speca_api.cpp", "speca_layer.cpp", "speca_layer8.cpp"]
+           "speca_norm8.cu", "speca_matmul8_tc.cu", "speca_matmul8_few.cu", "speca_matmul8_plan.cpp", "speca_api.cpp", "speca_layer.cpp", "speca_layer8.cpp"]
 HEADERS = [os.path.join(CSRC, "speca_internal.h"), os.path.join(CSRC, "speca_layer_internal.h"),
            os.path.join(CSRC, "speca_layer_handle.h"), os.path.join(CSRC, "speca_rows_common.cuh"),
            os.path.join(CSRC, "speca_eight_common.cuh"), os.path.join(CSRC, "speca_tc.cuh"), os.path.join(CSRC, "speca_early.cuh"), os.path.join(CSRC, "speca_matmul8_common.cuh"), os.path.join(CSRC, "speca_matmul8_tensor.cuh"),

@@ -134,7 +134,6 @@ struct Matmul8Params {
     int32_t vectors;  // rows of bias, residual, gate and out (or the codes) start on 16 bytes
     int32_t wide;     // those of the codes on 32
     int32_t boxes;    // the copy engine can address the output (set by the launch)
-    int32_t shares;   // of k that sums are added up from at least (set by the launch)
     uint32_t* gave_up;
 };
 cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream);
@@ -144,7 +143,13 @@ struct FewPlan {
     int rows, ranks;
     double us;  // about
 };
-FewPlan plan_few(const Matmul8Params& p, int sm_count);
+// Tiles for few rows, of one SM (128 x 128), of a pair (256 x 256).
+enum Matmul8Kernel { kFew, kOne, kPair };
+struct Matmul8Plan {
+    Matmul8Kernel kernel;
+    FewPlan few;  // that kernel's, whichever runs
+};
+Matmul8Plan plan_matmul8(const Matmul8Params& p, int dtype, int sm_count);
 cudaError_t launch_matmul8_few(const Matmul8Params& p, const FewPlan& plan, int dtype, cudaStream_t stream);
 
 }  // namespace speca

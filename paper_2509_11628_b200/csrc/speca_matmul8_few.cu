@@ -10,9 +10,6 @@
 // 14.7, 64 rows 10.0 and 17.1. Tried and not kept: shares sent to the row's block instead of fetched by it (equal or slower), one block an SM with
 // twice the stages (17 us for 4096 x 4096 of two shares, 8 us as it is). (With mma.sync in place of the tensor memory's products, 8 rows by 14336 x 4096 took
 // 17 us and 32 rows 37.)
-#include <algorithm>
-#include <cmath>
-
 #include "speca_matmul8_tensor.cuh"
 
 namespace speca {
@@ -246,40 +243,7 @@ cudaError_t dispatch_few(const Matmul8Params& p, const FewPlan& plan, cudaStream
     }
 }
 
-// Shares of k, of four stages of 128 at least: as many as run at once. Two blocks share an SM, and a cluster's SMs lie together, so that only 66 clusters of
-// four fit 148 SMs (72 took 14.4 us for 4 rows x 9216 x 4096, where two shares take 10.7); eight are worth it one to an SM (15 clusters): 4 rows x
-// 1152 x 4096 5.2 us, 6.3 with four; 4096 x 4096 as 256 blocks of eight 8.2, as 128 of four 7.7.
-int ranks_few(int64_t tiles, int k_blocks, int sm_count) {
-    int ranks = 1;
-    for (const double room : {2.0, 1.8, 0.82}) {
-        if (2 * ranks * tiles > room * sm_count || k_blocks < 8 * ranks) break;
-        ranks *= 2;
-    }
-    return ranks;
-}
-
 }  // namespace
-
-// Smaller tiles start and end sooner but read the weights more often, out of L2; blocks that share an SM share its way to L2. Fitted to 21 sizes of
-// each, within some 10 %: 211 rows x 333 x 1155 5.8 us in tiles of 16 rows, 10.4 in tiles of 128; 128 x 4096 x 4096 10.4 of 64, 10.8 of 128,
-// 12.0 of 32; 256 x 1152 x 4608 9.5 of 64, 11.4 of 128.
-FewPlan plan_few(const Matmul8Params& p, int sm_count) {
-    const int k_blocks = (p.k + kBlock8 - 1) / kBlock8;
-    FewPlan best{0, 0, 0.0};
-    for (const int rows : {16, 32, 64, 128}) {
-        if (rows > 16 && rows / 2 >= p.m) break;
-        const int64_t m_tiles = (p.m + rows - 1) / rows, tiles = (static_cast<int64_t>(p.n) + kRows - 1) / kRows * m_tiles;
-        const int ranks = std::max(ranks_few(tiles, k_blocks, sm_count), p.shares);
-        const double blocks = static_cast<double>(tiles) * ranks, sms = sm_count;
-        const double together = blocks <= sms ? 1.0 : blocks <= 2 * sms ? std::max(ranks > 2 ? 1.7 : 1.0, blocks / sms) : 2 * std::ceil(blocks / (2 * sms));
-        const double weights = static_cast<double>(p.n) * p.k / 6.5e6 * (0.75 + 0.25 * static_cast<double>(m_tiles));
-        const double steps = together * ((k_blocks + ranks - 1) / ranks) * (0.137 + 0.0013 * rows);
-        const double start = rows == 16 ? 6.0 : rows == 32 ? 6.4 : rows == 64 ? 7.3 : 9.1;
-        const double us = start + std::max(weights, steps) + 1.5 * (together - 1);
-        if (best.rows == 0 || us < best.us) best = FewPlan{rows, ranks, us};
-    }
-    return best;
-}
 
 cudaError_t launch_matmul8_few(const Matmul8Params& p, const FewPlan& plan, int dtype, cudaStream_t stream) {
     return dtype == SPECA_BF16 ? dispatch_few<SPECA_BF16>(p, plan, stream) : dispatch_few<SPECA_F32>(p, plan, stream);

@@ -664,59 +664,18 @@ cudaError_t run(Matmul8Params p, int sm_count, cudaStream_t stream) {
     return cudaSuccess;
 }
 
-// The three kernels' times in us, as fits to what they measured over 1 to 4096 rows, 1152 to 14336 features and elements of k
-// (largest error 25 %; what matters is where they cross). A start, then rounds of tiles over the SMs, each with a step for 128 elements of
-// k and an end, longer where rows do not start on 16 bytes; all read the weights at 6.5 TB/s at best. In us, rows x features x k, few / one SM / a pair:
-// 1 x 4096 x 4096 8.5 / 12.6 / 15.6;  512 x 4096 x 4096 17.7 / 13.3 / 16.6;  384 x 4096 x 14336 34 / 40 / 41;  1024 x 4096 x 14336 63 / 73 / 48;
-// 64 x 4608 x 1152 6.2 / 6.9 / 8.8;  4096 x 1152 x 4608 30 / 27 / 30;  4096 x 14336 x 4096 307 / 252 / 180.
-// A mask, which only the device knows, is taken to leave three rows of four where tiles of one SM and of a pair are compared: of 16 samples of 256 rows, 11
-// of them active, x 1152 x 4608 a pair's tiles fill one round in place of two (23.7 us, 31.4). These two add in the same order, so a row's
-// bits do not depend on the mask; shares of k add in another, so few rows are told apart without it.
-enum Kind { kFew, kOne, kPair };
-Kind choose(const Matmul8Params& p, const FewPlan& few, int sm_count) {
-    const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
-    auto tiles = [&](int64_t m, int64_t rows, int64_t features) { return (m + rows - 1) / rows * ((p.n + features - 1) / features); };
-    auto rounds = [](int64_t n, int64_t places) { return static_cast<double>((n + places - 1) / places); };
-    // (tiles of one SM with 16 rows or fewer took half as long again: 22 us for 14336 x 4096, 15.4 from 32 rows on)
-    auto one = [&](int64_t m) { return 4.2 + rounds(tiles(m, kRows, 128), sm_count) * (0.7 + (p.m <= 16 ? 0.45 : 0.27) * kb); };
-    auto pair = [&](int64_t m) { return 4.5 + rounds(tiles(m, 2 * kRows, 256), sm_count / 2) * (1.0 + 0.34 * kb); };
-    const double least = static_cast<double>(p.n) * p.k / 6.5e6 + (p.m <= 64 ? 8.0 : 6.9), odd = p.vectors ? 0.0 : 3.0;
-    if (few.us <= std::max(std::min(one(p.m), pair(p.m)) + odd, least)) return kFew;
-    const int64_t m = p.dev_mask != nullptr ? p.m - p.m / 4 : p.m;
-    return one(m) <= pair(m) ? kOne : kPair;
-}
-
 template <int DT>
-cudaError_t dispatch(const Matmul8Params& p, Kind kind, int sm_count, cudaStream_t stream) {
+cudaError_t dispatch(const Matmul8Params& p, Matmul8Kernel kind, int sm_count, cudaStream_t stream) {
     return kind == kOne ? run<DT, 1, 128>(p, sm_count, stream) : run<DT, 2, 256>(p, sm_count, stream);
 }
 
-// The tensor cores cut what they add to a sum, each step of 32 products, at about 2^-25 of the largest of the step's terms and the sum, so that a sum over all of k
-// comes out short: of normal values by 2.2e-7 of its size at k = 4096 and 5.0e-7 at 8192 (twice that in rows with a value 20 times the others), of uniform positive
-// ones by 9.4e-7 and 2.7e-6. At worst, of s terms next to a large one, each just below 2^-25 of it, s 2^-25 of the sum are lost (half of them were, where tried).
-// bf16 and 8 bits see that where it passes half a rounding, 2^-10: so at most 32768 elements are summed at once. Outputs in fp32 with more than 8192
-// elements take shares of 4096 (k / 8 beyond 32768): 2304 x 4096 x 16384 is 3.7e-7 off in place of 1.9e-6, for 193 us in place of 101. At 8192 the pair's 9e-7 stay
-// (58 us; shares would take 134). Shares of k are added up with rounding, by the kernel for few rows.
-int shares_of(const Matmul8Params& p, int dtype) {
-    const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;
-    const bool exact = dtype == SPECA_F32 && p.out != nullptr;
-    if (kb <= (exact ? 64 : 256)) return 1;
-    int shares = 2;
-    while (shares < kFewRanks && shares * (exact ? 32 : 256) < kb) shares *= 2;
-    return shares;
-}
-static_assert(SPECA_MAX_K8 <= kFewRanks * 32768, "no share is longer");
-
 }  // namespace
 
-cudaError_t launch_matmul8(const Matmul8Params& given, int dtype, int sm_count, cudaStream_t stream) {
-    if (given.m == 0) return cudaSuccess;
-    Matmul8Params p = given;
-    p.shares = shares_of(p, dtype);
-    const FewPlan few = plan_few(p, sm_count);
-    const Kind kind = p.shares > 1 ? kFew : choose(p, few, sm_count);
-    if (kind == kFew) return launch_matmul8_few(p, few, dtype, stream);
-    return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, kind, sm_count, stream) : dispatch<SPECA_F32>(p, kind, sm_count, stream);
+cudaError_t launch_matmul8(const Matmul8Params& p, int dtype, int sm_count, cudaStream_t stream) {
+    if (p.m == 0) return cudaSuccess;
+    const Matmul8Plan plan = plan_matmul8(p, dtype, sm_count);
+    if (plan.kernel == kFew) return launch_matmul8_few(p, plan.few, dtype, stream);
+    return dtype == SPECA_BF16 ? dispatch<SPECA_BF16>(p, plan.kernel, sm_count, stream) : dispatch<SPECA_F32>(p, plan.kernel, sm_count, stream);
 }
 
 }  // namespace speca
