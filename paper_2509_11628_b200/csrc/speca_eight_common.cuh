@@ -6,13 +6,12 @@ namespace speca {
 namespace {
 
 // Scale byte of a block whose largest finite magnitude is `top`: the smallest e with top <= 448 * 2^e, biased by 127, within
-// 1..254. 448 = 1.75 * 2^8: eight binades below top's, one more where top's significand exceeds 1.75. Zeros: 1.
+// 1..254. 448 = 1.75 * 2^8: eight binades below top's, one more where top's significand exceeds 1.75. Of zeros: 127, a scale of 1.
 __device__ __forceinline__ uint32_t scale_byte(float top) {
     const uint32_t u = __float_as_uint(top);
     const int e = static_cast<int>(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);
     return top == 0.f ? 127u : static_cast<uint32_t>(max(e, 1));
 }
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 // 1 / scale, exact: 2^(127 - byte). (A byte is at most 254 - 8 + 1 here.)
 __device__ __forceinline__ float inverse_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
