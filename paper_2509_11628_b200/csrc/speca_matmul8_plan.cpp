@@ -48,7 +48,8 @@ FewPlan plan_few(const Matmul8Params& p, int shares, int sm_count) {
 // 1 x 4096 x 4096 8.5 / 12.6 / 15.6;  512 x 4096 x 4096 17.7 / 13.3 / 16.6;  384 x 4096 x 14336 34 / 40 / 41;  1024 x 4096 x 14336 63 / 73 / 48;
 // 64 x 4608 x 1152 6.2 / 6.9 / 8.8;  4096 x 1152 x 4608 30 / 27 / 30;  4096 x 14336 x 4096 307 / 252 / 180.
 // A mask, which only the device knows, is taken to leave three rows of four where tiles of one SM and of a pair are compared: of 16 samples of 256 rows, 11
-// of them active, x 1152 x 4608 a pair's tiles fill one round in place of two (23.7 us, 31.4). These two add in the same order, so a row's
+// of them active, x 1152 x 4608 a pair's tiles fill one round in place of two (23.7 us, 31.4). In a graph the pair then takes 18.2 us with one sample active, 20.1 with 8 to
+// 14 and 29.9 with all 16, where tiles of one SM take 23.7. These two add in the same order, so a row's
 // bits do not depend on the mask; shares of k add in another, so few rows are told apart without it.
 Matmul8Kernel choose(const Matmul8Params& p, const FewPlan& few, int sm_count) {
     const int64_t kb = (p.k + kBlock8 - 1) / kBlock8;

@@ -15,7 +15,8 @@
 // products. Between tiles some 1300 cycles pass while the last sums are read. In a loop the card runs into its power limit (1000 W, 1.4 GHz).
 // Measured, e4m3 with bf16 out, in a loop: 4096 x 4608 x 1152 22.9 us (1.90 PFLOP/s; a library's block-scaled product 23.3), 4096 x 1152 x 4608 26.8 (1.62;
 // 28.0), 8352 x 14336 x 4096 399 (2.46; 390), 8192^3 422 (2.61; 470), 20928 x 16384 x 4096 1100 (2.55; 1277); 8352 x 14336 x 4096 in a short run 357 (2.74).
-// Short k with an activation is bound by the epilogue: 4096 x 4608 x 1152 with bias and GELU into 8 bits 28 us, 20 without them. Tried there and
+// Short k with an activation waits for the epilogue: 4096 x 4608 x 1152 in a graph 19.2 us into bf16, 20 into 8 bits, 22 with GELU into bf16, 27 to 29 with bias and GELU into
+// 8 bits; what in it takes the time is not known (the special function unit is busy a quarter of it). Tried there and
 // not kept: 16 epilogue warps in place of 8 (28.1 us), exponentials of one pair in 4, 3 or 2 by polynomial (28.3 to 28.9), what the next tile needs asked
 // for a tile ahead (30.8 then, 30.1).
 #include <algorithm>

@@ -26,8 +26,9 @@ __device__ __forceinline__ uint32_t leaders(uint64_t* bar) {
     if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(a));
     return a;
 }
-// Tells the first SM that this warp's accesses to tensor memory are done. They are (the warp waited for them) and no other memory is
-// handed over, so nothing has to be released: a release to the cluster waits 1200 cycles for the thread's stores.
+// Tells the first SM that this warp's accesses to tensor memory are done. They are (the warp waited for them), and tensor memory is ordered between threads by the
+// tcgen05 fences in front of an arrival and behind a wait, whatever the arrival's own strength. No other memory is handed over, so nothing has to be
+// released: a release to the cluster waits 1200 cycles for the thread's stores.
 template <int CG>
 __device__ __forceinline__ void hand_over(uint64_t* bar, int lane) {
     tc_fence_before();
