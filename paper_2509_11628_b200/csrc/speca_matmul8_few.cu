@@ -111,11 +111,9 @@ __global__ void __launch_bounds__(kFewThreads, 2)
                 if (!ok) break;
                 load(kb);
             }
-            if (!ok) {
-                sm.abort = 1;
-                // copies in flight must land before the block gives its shared memory back
-                for (int i = 0; i < S::kStages; ++i) bar_wait(&sm.full[i], i < stage ? phase : phase ^ 1);
-            }
+            if (!ok) sm.abort = 1;
+            // Copies in flight must land before the block gives its shared memory back, also where another warp's wait ran out.
+            for (int i = 0; i < S::kStages; ++i) bar_wait(&sm.full[i], i < stage ? phase : phase ^ 1);
         }
     } else if (warp == kIssuer) {
         if (elect_one()) {

@@ -19,8 +19,6 @@
 // 8 bits; what in it takes the time is not known (the special function unit is busy a quarter of it). Tried there and
 // not kept: 16 epilogue warps in place of 8 (28.1 us), exponentials of one pair in 4, 3 or 2 by polynomial (28.3 to 28.9), what the next tile needs asked
 // for a tile ahead (30.8 then, 30.1).
-#include <algorithm>
-
 #include "speca_matmul8_tensor.cuh"
 
 namespace speca {
@@ -372,14 +370,13 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
                     if (++stage == S::kStages) stage = 0, phase ^= 1;
                 }
             }
-            if (!ok) {
-                sm.abort = 1;
-                // copies in flight must land before the block gives its shared memory back
-                if (rank == 0)
-                    for (int i = 0; i < S::kStages; ++i) bar_wait(&sm.full[i], i < stage ? phase : phase ^ 1);
-                else
-                    for (int i = 0; i < 1000; ++i) __nanosleep(1000);
-            }
+            if (!ok) sm.abort = 1;
+            // Copies in flight, those of both SMs, must land before the block gives its shared memory back, also where another warp's wait ran out. The second
+            // SM, which cannot wait for the first one's barriers, leaves no sooner than that one does.
+            if (rank == 0)
+                for (int i = 0; i < S::kStages; ++i) bar_wait(&sm.full[i], i < stage ? phase : phase ^ 1);
+            else if (!ok)
+                for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         }
     } else if (warp == kIssueWarp) {
         // ---- products: one thread of the first SM. It looks for the next stage before it issues this one's: a wait that is
