@@ -49,7 +49,7 @@ def test_codes_next_to_a_border_tell_sums_apart(S, kind):
     z = x.double()
     mean = z.mean() if kind == "layer" else 0.0
     unit = ((z - mean) / torch.sqrt(((z - mean) ** 2).mean() + 1e-6)).abs().mean()
-    # codes of 1 and 1.125: their border is 1.0625. Weights on either side of it, and a 1.75 in every block that sets the scale
+    # codes of 1 and 1.125: their border is 1.0625. Weights on either side of it, and a 1.7 in every block, so that its scale is the one of values up to 1.75
     weight = torch.full((dim,), 1.0625, dtype=torch.float64, device=DEV)
     weight[0::2] *= 1 + 2e-5
     weight[1::2] *= 1 - 2e-5
